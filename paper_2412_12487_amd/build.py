@@ -31,10 +31,14 @@ def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     kobj = os.path.join(BUILD, "echo_kernels.o")
     hobj = os.path.join(BUILD, "echo_host.o")
+    okobj = os.path.join(BUILD, "echo_ops.o")
+    ohobj = os.path.join(BUILD, "echo_ops_host.o")
     _run(["hipcc", "-c", *DEVICE_FLAGS, *COMMON, os.path.join(CSRC, "echo_kernels.hip"), "-o", kobj], verbose)
     _run(["hipcc", "-c", *COMMON, os.path.join(CSRC, "echo_host.cpp"), "-o", hobj], verbose)
+    _run(["hipcc", "-c", *DEVICE_FLAGS, *COMMON, os.path.join(CSRC, "echo_ops.hip"), "-o", okobj], verbose)
+    _run(["hipcc", "-c", *COMMON, os.path.join(CSRC, "echo_ops_host.cpp"), "-o", ohobj], verbose)
     tmp = LIB + ".tmp"
-    _run(["hipcc", "-shared", "-fPIC", "--offload-arch=" + ARCH, kobj, hobj, "-o", tmp], verbose)
+    _run(["hipcc", "-shared", "-fPIC", "--offload-arch=" + ARCH, kobj, hobj, okobj, ohobj, "-o", tmp], verbose)
     os.replace(tmp, LIB)
     return LIB
 

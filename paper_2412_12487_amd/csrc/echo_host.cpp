@@ -1357,6 +1357,21 @@ int walk_chain(echo_graph g, const int64_t w[3], int64_t out[4]) {
 
 }  // namespace
 
+namespace echo {
+
+int set_error(int code, const char *fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    return fail(code, "%s", buf);
+}
+
+void clear_error() { g_last_error.clear(); }
+
+}  // namespace echo
+
 extern "C" {
 
 int echo_load_graph_ex(const echo_graph_desc *desc, int hip_device, int32_t ranks_per_walker, echo_graph *out) {

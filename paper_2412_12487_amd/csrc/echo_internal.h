@@ -26,6 +26,10 @@
 
 namespace echo {
 
+// The calling thread's last error (echo_last_error): set_error returns `code`.
+int set_error(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+void clear_error();
+
 constexpr int kStreams = 8;
 constexpr int kClasses = 8;
 constexpr int kTypes = 4;

@@ -1,0 +1,312 @@
+// echo_ops_host.cpp -- C entry points of the training-step operators (echo_ops.h): argument checks,
+// the device guard and the launches.  Nothing here allocates device memory or waits.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <initializer_list>
+
+#include "echo.h"
+#include "echo_internal.h"
+#include "echo_ops.h"
+#include "echo_ops_internal.h"
+
+using namespace echo;
+
+namespace {
+
+constexpr int64_t kMaxRows = INT32_MAX;
+constexpr int64_t kMaxCols = int64_t(1) << 24;
+constexpr int64_t kMaxStride = int64_t(1) << 28;   // 2^31 rows of 4-byte elements stay below 2^62 bytes
+
+int64_t elem(int32_t type) { return type == ECHO_F32 ? 4 : 2; }
+bool is_type(int32_t t) { return t == ECHO_F32 || t == ECHO_F16 || t == ECHO_BF16; }
+
+// The bytes that an argument spans.  `same`: an output that may be exactly an input of the same
+// layout; such pairs carry the same nonzero number.
+struct Span {
+    const char *name;
+    const void *p;
+    int64_t bytes;
+    int same;
+};
+int64_t span_of(int64_t rows, int64_t cols, int64_t stride, int64_t e) {
+    return rows ? ((rows - 1) * stride + cols) * e : 0;
+}
+bool meet(const Span &a, const Span &b) {
+    if (!a.p || !b.p || a.bytes <= 0 || b.bytes <= 0) return false;
+    const uintptr_t p = (uintptr_t)a.p, q = (uintptr_t)b.p;
+    return p < q + (uintptr_t)b.bytes && q < p + (uintptr_t)a.bytes;
+}
+// Every output against every input and every other output.
+int check_spans(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+    for (const Span *o = outs.begin(); o != outs.end(); ++o) {
+        for (const Span *q = outs.begin(); q != o; ++q)
+            if (meet(*o, *q)) return set_error(ECHO_ERR_ARG, "%s and %s overlap", o->name, q->name);
+        for (const Span &i : ins)
+            if (meet(*o, i) && !(o->same && (o->same & i.same) && o->p == i.p && o->bytes == i.bytes))
+                return set_error(ECHO_ERR_ARG, "%s overlaps %s", o->name, i.name);
+    }
+    return ECHO_OK;
+}
+
+int check_matrix(const char *name, const void *p, int64_t rows, int64_t stride, int64_t e) {
+    if (rows && !p) return set_error(ECHO_ERR_ARG, "%s is null", name);
+    if (stride < 0 || stride > kMaxStride)
+        return set_error(ECHO_ERR_ARG, "%s: row stride %lld outside [0, 2^28]", name, (long long)stride);
+    if ((uintptr_t)p % (uintptr_t)e) return set_error(ECHO_ERR_ARG, "%s is not aligned to its elements", name);
+    return ECHO_OK;
+}
+int check_vector(const char *name, const void *p, int64_t e, bool required) {
+    if (required && !p) return set_error(ECHO_ERR_ARG, "%s is null", name);
+    if ((uintptr_t)p % (uintptr_t)e) return set_error(ECHO_ERR_ARG, "%s is not aligned to its elements", name);
+    return ECHO_OK;
+}
+int check_sizes(int64_t rows, int64_t cols) {
+    if (rows < 0 || rows > kMaxRows) return set_error(ECHO_ERR_ARG, "rows = %lld outside [0, 2^31)", (long long)rows);
+    if (cols < 1 || cols > kMaxCols) return set_error(ECHO_ERR_ARG, "cols = %lld outside [1, 2^24]", (long long)cols);
+    return ECHO_OK;
+}
+int check_types(int32_t type, int32_t other, const char *what) {
+    if (!is_type(type)) return set_error(ECHO_ERR_ARG, "unknown element type %d", type);
+    if (other != type && other != ECHO_F32)
+        return set_error(ECHO_ERR_ARG, "%s must be the activations' type or 32 bits (got %d)", what, other);
+    return ECHO_OK;
+}
+int check_index(int32_t index_type) {
+    if (index_type != ECHO_I32 && index_type != ECHO_I64)
+        return set_error(ECHO_ERR_ARG, "unknown index type %d", index_type);
+    return ECHO_OK;
+}
+int check_shard(int64_t start, int64_t n, int64_t whole) {
+    if (start < 0 || n < 0 || n > kMaxRows || start > INT64_MAX - n)
+        return set_error(ECHO_ERR_ARG, "vocabulary shard [%lld, +%lld) out of range", (long long)start, (long long)n);
+    if (whole >= 0 && start + n > whole)
+        return set_error(ECHO_ERR_ARG, "vocabulary shard [%lld, +%lld) passes the vocabulary of %lld",
+                         (long long)start, (long long)n, (long long)whole);
+    return ECHO_OK;
+}
+int check_workspace(const void *p, int64_t bytes, int64_t need) {
+    if (need && (!p || bytes < need))
+        return set_error(ECHO_ERR_ARG, "workspace holds %lld bytes, needs %lld", (long long)(p ? bytes : 0),
+                         (long long)need);
+    if ((uintptr_t)p % 16) return set_error(ECHO_ERR_ARG, "workspace is not aligned to 16 bytes");
+    return ECHO_OK;
+}
+
+// Runs f on GPU `device` and leaves the thread's current device as it was.
+template <class F>
+int on_device(int device, const char *what, F f) {
+    int before = -1;
+    hipError_t e = hipGetDevice(&before);
+    if (e != hipSuccess) return set_error(ECHO_ERR_HIP, "hipGetDevice: %s", hipGetErrorString(e));
+    if (before != device && (e = hipSetDevice(device)) != hipSuccess)
+        return set_error(ECHO_ERR_HIP, "hipSetDevice(%d): %s", device, hipGetErrorString(e));
+    e = f();
+    if (before != device) (void)hipSetDevice(before);
+    if (e != hipSuccess) return set_error(ECHO_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+    return ECHO_OK;
+}
+
+#define ECHO_TRY(call)                 \
+    do {                               \
+        const int rc_ = (call);        \
+        if (rc_ != ECHO_OK) return rc_; \
+    } while (0)
+
+}  // namespace
+
+extern "C" {
+
+int echo_layer_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride,
+                    const void *weight, const void *bias, int32_t type, int32_t weight_type, int64_t rows,
+                    int64_t cols, float eps, void *y, void *sum, float *mean, float *rstd, int hip_device,
+                    void *hip_stream) {
+    clear_error();
+    ECHO_TRY(check_types(type, weight_type, "weight_type"));
+    ECHO_TRY(check_sizes(rows, cols));
+    if (!(eps >= 0.0f) || !std::isfinite(eps)) return set_error(ECHO_ERR_ARG, "eps must be finite and >= 0");
+    const int64_t e = elem(type), we = elem(weight_type);
+    const int64_t live = residual ? rows : 0;
+    ECHO_TRY(check_matrix("x", x, rows, x_stride, e));
+    ECHO_TRY(check_matrix("residual", residual, live, residual ? residual_stride : 0, e));
+    ECHO_TRY(check_vector("weight", weight, we, rows > 0));
+    ECHO_TRY(check_vector("bias", bias, we, false));
+    ECHO_TRY(check_matrix("y", y, rows, cols, e));
+    if (rows && !residual != !sum) return set_error(ECHO_ERR_ARG, "sum is given exactly when residual is");
+    ECHO_TRY(check_matrix("sum", sum, live, cols, e));
+    ECHO_TRY(check_vector("mean", mean, 4, rows > 0));
+    ECHO_TRY(check_vector("rstd", rstd, 4, rows > 0));
+    ECHO_TRY(check_spans({{"y", y, rows * cols * e, 0}, {"sum", sum, live * cols * e, 1}, {"mean", mean, rows * 4, 0},
+                          {"rstd", rstd, rows * 4, 0}},
+                         {{"x", x, span_of(rows, cols, x_stride, e), rows < 2 || x_stride == cols},
+                          {"residual", residual, span_of(live, cols, residual_stride, e),
+                           rows < 2 || residual_stride == cols},
+                          {"weight", weight, cols * we, 0}, {"bias", bias, cols * we, 0}}));
+    if (!rows) return ECHO_OK;
+    const NormArgs a{x, residual, weight, bias, x_stride, residual_stride, rows, (int)cols, eps, y, sum, mean, rstd};
+    return on_device(hip_device, "layer norm", [&] {
+        return launch_norm(a, type, weight_type, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+int64_t echo_layer_norm_grad_workspace(int64_t rows, int64_t cols) {
+    if (rows < 0 || rows > kMaxRows || cols < 1 || cols > kMaxCols) return 0;
+    return (int64_t)norm_grad_parts(rows, cols) * 2 * cols * 4;
+}
+
+int echo_layer_norm_grad(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, const void *weight,
+                         const float *mean, const float *rstd, const void *grad_residual,
+                         int64_t grad_residual_stride, int32_t type, int32_t weight_type, int64_t rows, int64_t cols,
+                         void *dx, void *dweight, void *dbias, int32_t grad_type, int32_t accumulate,
+                         void *workspace, int64_t workspace_bytes, int hip_device, void *hip_stream) {
+    clear_error();
+    ECHO_TRY(check_types(type, weight_type, "weight_type"));
+    if (grad_type != weight_type && grad_type != ECHO_F32)
+        return set_error(ECHO_ERR_ARG, "grad_type must be the weight's type or 32 bits (got %d)", grad_type);
+    ECHO_TRY(check_sizes(rows, cols));
+    const int64_t e = elem(type), we = elem(weight_type), ge = elem(grad_type);
+    const int64_t live = grad_residual ? rows : 0;
+    ECHO_TRY(check_matrix("dy", dy, rows, dy_stride, e));
+    ECHO_TRY(check_matrix("x", x, rows, x_stride, e));
+    ECHO_TRY(check_matrix("grad_residual", grad_residual, live, grad_residual ? grad_residual_stride : 0, e));
+    ECHO_TRY(check_vector("weight", weight, we, rows > 0));
+    ECHO_TRY(check_vector("mean", mean, 4, rows > 0));
+    ECHO_TRY(check_vector("rstd", rstd, 4, rows > 0));
+    ECHO_TRY(check_matrix("dx", dx, rows, cols, e));
+    ECHO_TRY(check_vector("dweight", dweight, ge, true));
+    ECHO_TRY(check_vector("dbias", dbias, ge, false));
+    const int64_t need = echo_layer_norm_grad_workspace(rows, cols);
+    ECHO_TRY(check_workspace(workspace, workspace_bytes, need));
+    ECHO_TRY(check_spans({{"dx", dx, rows * cols * e, 1}, {"dweight", dweight, cols * ge, 0},
+                          {"dbias", dbias, cols * ge, 0}, {"workspace", workspace, need, 0}},
+                         {{"dy", dy, span_of(rows, cols, dy_stride, e), rows < 2 || dy_stride == cols},
+                          {"x", x, span_of(rows, cols, x_stride, e), 0},
+                          {"grad_residual", grad_residual, span_of(live, cols, grad_residual_stride, e),
+                           rows < 2 || grad_residual_stride == cols},
+                          {"weight", weight, cols * we, 0}, {"mean", mean, rows * 4, 0}, {"rstd", rstd, rows * 4, 0}}));
+    const NormGradArgs a{dy, x, weight, grad_residual, mean, rstd, dy_stride, x_stride, grad_residual_stride, rows,
+                         (int)cols, dx, dweight, dbias, static_cast<float *>(workspace), norm_grad_parts(rows, cols),
+                         accumulate != 0};
+    return on_device(hip_device, "layer norm gradient", [&] {
+        return launch_norm_grad(a, type, weight_type, grad_type, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+int echo_embedding(const void *ids, int32_t index_type, const void *weight, int64_t weight_stride, int32_t type,
+                   int64_t rows, int64_t cols, int64_t vocab_start, int64_t vocab, float scale, void *out,
+                   int hip_device, void *hip_stream) {
+    clear_error();
+    ECHO_TRY(check_types(type, type, "type"));
+    ECHO_TRY(check_index(index_type));
+    ECHO_TRY(check_sizes(rows, cols));
+    ECHO_TRY(check_shard(vocab_start, vocab, -1));
+    const int64_t e = elem(type), ie = index_type == ECHO_I64 ? 8 : 4;
+    ECHO_TRY(check_vector("ids", ids, ie, rows > 0));
+    ECHO_TRY(check_matrix("weight", weight, rows ? vocab : 0, weight_stride, e));
+    ECHO_TRY(check_matrix("out", out, rows, cols, e));
+    ECHO_TRY(check_spans({{"out", out, rows * cols * e, 0}},
+                         {{"ids", ids, rows * ie, 0}, {"weight", weight, span_of(vocab, cols, weight_stride, e), 0}}));
+    if (!rows) return ECHO_OK;
+    const EmbedArgs a{ids, weight, weight_stride, rows, vocab_start, (int)cols, (int)vocab, scale, out};
+    return on_device(hip_device, "embedding", [&] {
+        return launch_embed(a, type, index_type, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+int64_t echo_embedding_grad_workspace(int64_t rows, int64_t cols, int64_t vocab) {
+    if (rows < 0 || rows > kMaxRows || cols < 1 || cols > kMaxCols || vocab < 0 || vocab > kMaxRows) return 0;
+    return embed_grad_bytes(rows, cols, vocab);
+}
+
+int echo_embedding_grad(const void *ids, int32_t index_type, const void *dy, int64_t dy_stride, int32_t type,
+                        int64_t rows, int64_t cols, int64_t vocab_start, int64_t vocab, float scale, void *dweight,
+                        int32_t grad_type, int32_t accumulate, void *workspace, int64_t workspace_bytes,
+                        int hip_device, void *hip_stream) {
+    clear_error();
+    ECHO_TRY(check_types(type, grad_type, "grad_type"));
+    ECHO_TRY(check_index(index_type));
+    ECHO_TRY(check_sizes(rows, cols));
+    ECHO_TRY(check_shard(vocab_start, vocab, -1));
+    const int64_t e = elem(type), ge = elem(grad_type), ie = index_type == ECHO_I64 ? 8 : 4;
+    ECHO_TRY(check_vector("ids", ids, ie, rows > 0));
+    ECHO_TRY(check_matrix("dy", dy, rows, dy_stride, e));
+    ECHO_TRY(check_matrix("dweight", dweight, vocab, cols, ge));
+    const int64_t need = echo_embedding_grad_workspace(rows, cols, vocab);
+    ECHO_TRY(check_workspace(workspace, workspace_bytes, need));
+    ECHO_TRY(check_spans({{"dweight", dweight, vocab * cols * ge, 0}, {"workspace", workspace, need, 0}},
+                         {{"ids", ids, rows * ie, 0}, {"dy", dy, span_of(rows, cols, dy_stride, e), 0}}));
+    if (!vocab || (!rows && accumulate)) return ECHO_OK;
+    const EmbedGradArgs a{ids, dy, dy_stride, rows, vocab_start, (int)cols, (int)vocab, scale, dweight,
+                          accumulate != 0, workspace};
+    return on_device(hip_device, "embedding gradient", [&] {
+        return launch_embed_grad(a, type, index_type, grad_type, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+int echo_cross_entropy(const void *logits, int64_t logits_stride, int32_t type, const void *targets,
+                       int32_t index_type, int64_t rows, int64_t cols, int64_t vocab_start, int64_t vocab_size,
+                       float *lse, float *target, float *loss, const float *grad_loss, void *grad,
+                       int64_t grad_stride, int hip_device, void *hip_stream) {
+    clear_error();
+    ECHO_TRY(check_types(type, type, "type"));
+    ECHO_TRY(check_index(index_type));
+    ECHO_TRY(check_sizes(rows, cols));
+    ECHO_TRY(check_shard(vocab_start, cols, vocab_size));
+    const bool whole = vocab_start == 0 && vocab_size == cols;
+    if (!whole && (loss || grad))
+        return set_error(ECHO_ERR_ARG, "loss and grad need the whole vocabulary; a shard gives lse and target");
+    if (rows && !lse && !target && !loss && !grad) return set_error(ECHO_ERR_ARG, "no output is asked for");
+    if (rows && !grad != !grad_loss) return set_error(ECHO_ERR_ARG, "grad_loss is given exactly when grad is");
+    const int64_t e = elem(type), ie = index_type == ECHO_I64 ? 8 : 4, live = grad ? rows : 0;
+    ECHO_TRY(check_matrix("logits", logits, rows, logits_stride, e));
+    ECHO_TRY(check_vector("targets", targets, ie, rows > 0));
+    ECHO_TRY(check_vector("lse", lse, 4, false));
+    ECHO_TRY(check_vector("target", target, 4, false));
+    ECHO_TRY(check_vector("loss", loss, 4, false));
+    ECHO_TRY(check_vector("grad_loss", grad_loss, 4, false));
+    ECHO_TRY(check_matrix("grad", grad, live, grad ? grad_stride : 0, e));
+    if (live > 1 && grad_stride < cols) return set_error(ECHO_ERR_ARG, "rows of grad overlap");
+    const bool dense = rows < 2 || logits_stride == grad_stride;
+    ECHO_TRY(check_spans({{"grad", grad, span_of(live, cols, grad_stride, e), 1}, {"lse", lse, rows * 4, 0},
+                          {"target", target, rows * 4, 0}, {"loss", loss, rows * 4, 0}},
+                         {{"logits", logits, span_of(rows, cols, logits_stride, e), dense},
+                          {"targets", targets, rows * ie, 0}, {"grad_loss", grad_loss, rows * 4, 0}}));
+    if (!rows) return ECHO_OK;
+    const LossArgs a{logits, targets, logits_stride, rows, vocab_start, vocab_size, (int)cols, lse, target, loss,
+                     nullptr, grad_loss, grad, grad_stride};
+    return on_device(hip_device, "cross entropy", [&] {
+        return launch_loss(a, type, index_type, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+int echo_cross_entropy_grad(const void *logits, int64_t logits_stride, int32_t type, const void *targets,
+                            int32_t index_type, int64_t rows, int64_t cols, int64_t vocab_start, int64_t vocab_size,
+                            const float *lse, const float *grad_loss, void *grad, int64_t grad_stride,
+                            int hip_device, void *hip_stream) {
+    clear_error();
+    ECHO_TRY(check_types(type, type, "type"));
+    ECHO_TRY(check_index(index_type));
+    ECHO_TRY(check_sizes(rows, cols));
+    ECHO_TRY(check_shard(vocab_start, cols, vocab_size));
+    const int64_t e = elem(type), ie = index_type == ECHO_I64 ? 8 : 4;
+    ECHO_TRY(check_matrix("logits", logits, rows, logits_stride, e));
+    ECHO_TRY(check_vector("targets", targets, ie, rows > 0));
+    ECHO_TRY(check_vector("lse", lse, 4, rows > 0));
+    ECHO_TRY(check_vector("grad_loss", grad_loss, 4, rows > 0));
+    ECHO_TRY(check_matrix("grad", grad, rows, grad_stride, e));
+    if (rows > 1 && grad_stride < cols) return set_error(ECHO_ERR_ARG, "rows of grad overlap");
+    const bool dense = rows < 2 || logits_stride == grad_stride;
+    ECHO_TRY(check_spans({{"grad", grad, span_of(rows, cols, grad_stride, e), 1}},
+                         {{"logits", logits, span_of(rows, cols, logits_stride, e), dense},
+                          {"targets", targets, rows * ie, 0}, {"lse", lse, rows * 4, 0},
+                          {"grad_loss", grad_loss, rows * 4, 0}}));
+    if (!rows) return ECHO_OK;
+    const LossArgs a{logits, targets, logits_stride, rows, vocab_start, vocab_size, (int)cols, nullptr, nullptr,
+                     nullptr, lse, grad_loss, grad, grad_stride};
+    return on_device(hip_device, "cross entropy gradient", [&] {
+        return launch_loss_grad(a, type, index_type, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+}  // extern "C"

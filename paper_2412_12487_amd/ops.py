@@ -1,0 +1,343 @@
+"""Operators of a training step (include/echo_ops.h): embedding, layer norm and cross entropy, each
+with its gradient, as HIP kernels of libecho.so.
+
+The composer plans a job from its operators' durations; these are the operators of a pipeline
+stage outside its matrix products, on the GPU at hand (`workloads.measured` times them for a graph).
+
+    y = layer_norm(x, weight, bias)["y"]
+    h = embedding(ids, table, scale)
+    r = cross_entropy(logits, targets, grad_loss=g)          # loss, lse and the logits' gradient
+
+Activations are float32, float16 or bfloat16 matrices whose rows are contiguous (leading dimensions in
+one stride; nothing is copied into order behind the caller's back: another layout raises EchoError).
+Sums and statistics are in 32 bits and each result is rounded once.  Work is enqueued on the
+current stream of the tensors' GPU; outputs and workspaces not passed in come from torch's allocator on
+that stream.  Every call can be captured in a HIP graph.  Results do not vary from run to run.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from .echo import ECHO_ERR_ARG, EchoError, _check, lib
+
+EXPORTS = ("echo_layer_norm", "echo_layer_norm_grad", "echo_layer_norm_grad_workspace", "echo_embedding",
+           "echo_embedding_grad", "echo_embedding_grad_workspace", "echo_cross_entropy", "echo_cross_entropy_grad")
+
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+_INDEX = {torch.int32: 0, torch.int64: 1}
+
+_fns = None
+
+
+def _ops():
+    """The library with the operators' signatures set."""
+    global _fns
+    if _fns is None:
+        L = lib()
+        P, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+        L.echo_layer_norm.argtypes = [P, i64, P, i64, P, P, i32, i32, i64, i64, f32, P, P, P, P, i32, P]
+        L.echo_layer_norm_grad.argtypes = [P, i64, P, i64, P, P, P, P, i64, i32, i32, i64, i64, P, P, P, i32, i32,
+                                           P, i64, i32, P]
+        L.echo_embedding.argtypes = [P, i32, P, i64, i32, i64, i64, i64, i64, f32, P, i32, P]
+        L.echo_embedding_grad.argtypes = [P, i32, P, i64, i32, i64, i64, i64, i64, f32, P, i32, i32, P, i64, i32, P]
+        L.echo_cross_entropy.argtypes = [P, i64, i32, P, i32, i64, i64, i64, i64, P, P, P, P, P, i64, i32, P]
+        L.echo_cross_entropy_grad.argtypes = [P, i64, i32, P, i32, i64, i64, i64, i64, P, P, P, i64, i32, P]
+        for name in EXPORTS:
+            getattr(L, name).restype = i32
+        L.echo_layer_norm_grad_workspace.argtypes = [i64, i64]
+        L.echo_layer_norm_grad_workspace.restype = i64
+        L.echo_embedding_grad_workspace.argtypes = [i64, i64, i64]
+        L.echo_embedding_grad_workspace.restype = i64
+        _fns = L
+    return _fns
+
+
+def _bad(msg):
+    return EchoError(ECHO_ERR_ARG, msg)
+
+
+def _gpu(t, name):
+    """Device index of the call's first tensor."""
+    if not isinstance(t, torch.Tensor):
+        raise _bad(f"{name} must be a torch tensor")
+    if not t.is_cuda:
+        raise _bad(f"{name} is on {t.device}: the operators run on the GPU")
+    return t.device
+
+
+def _matrix(t, name, dev, types):
+    """(rows, cols, row stride) of a tensor read as rows of its last dimension."""
+    if not isinstance(t, torch.Tensor):
+        raise _bad(f"{name} must be a torch tensor")
+    if t.device != dev:
+        raise _bad(f"{name} is on {t.device}, the call on {dev}")
+    if t.dtype not in types:
+        raise _bad(f"{name} must be {' or '.join(str(x) for x in types)} (got {t.dtype})")
+    if t.dim() < 1:
+        raise _bad(f"{name} must have at least one dimension")
+    cols = t.shape[-1]
+    if cols < 1:
+        raise _bad(f"{name} has rows of no elements")
+    rows = t.numel() // cols
+    if rows <= 1 or t.is_contiguous():
+        if rows and cols > 1 and t.stride(-1) != 1:
+            raise _bad(f"{name}: the elements of a row must be contiguous (stride {t.stride(-1)})")
+        return rows, cols, cols
+    if cols > 1 and t.stride(-1) != 1:
+        raise _bad(f"{name}: the elements of a row must be contiguous (stride {t.stride(-1)})")
+    stride = n = None
+    for size, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if stride is None:
+            stride, n = step, size
+        elif step != stride * n:
+            raise _bad(f"{name}: the leading dimensions {tuple(t.shape[:-1])} are not one run of rows "
+                       f"(strides {t.stride()[:-1]})")
+        else:
+            n *= size
+    return rows, cols, stride
+
+
+def _vector(t, name, dev, n, types):
+    if not isinstance(t, torch.Tensor):
+        raise _bad(f"{name} must be a torch tensor")
+    if t.device != dev:
+        raise _bad(f"{name} is on {t.device}, the call on {dev}")
+    if t.dtype not in types:
+        raise _bad(f"{name} must be {' or '.join(str(x) for x in types)} (got {t.dtype})")
+    if t.numel() != n:
+        raise _bad(f"{name} has {t.numel()} elements, needs {n}")
+    if not t.is_contiguous():
+        raise _bad(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _dense(t, name, dev, shape, dtype):
+    """An output: the caller's tensor, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    if not isinstance(t, torch.Tensor):
+        raise _bad(f"{name} must be a torch tensor")
+    if t.device != dev:
+        raise _bad(f"{name} is on {t.device}, the call on {dev}")
+    if t.dtype != dtype:
+        raise _bad(f"{name} must be {dtype} (got {t.dtype})")
+    if t.shape != torch.Size(shape):
+        raise _bad(f"{name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
+    if not t.is_contiguous():
+        raise _bad(f"{name} must be contiguous")
+    return t
+
+
+def _space(workspace, need, dev):
+    """Scratch of at least `need` bytes: the caller's, or a new one."""
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    if not isinstance(workspace, torch.Tensor) or workspace.device != dev or not workspace.is_contiguous():
+        raise _bad(f"workspace must be a contiguous tensor on {dev}")
+    return workspace
+
+
+def _space_args(space):
+    return (None, 0) if space is None else (space.data_ptr(), space.numel() * space.element_size())
+
+
+def _stream(dev):
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+def _only(out, names):
+    out = dict(out or {})
+    for k in out:
+        if k not in names:
+            raise _bad(f"out has no entry {k!r} here (entries: {', '.join(names)})")
+    return out
+
+
+def layer_norm(x, weight, bias=None, eps=1e-5, *, residual=None, out=None):
+    """Layer norm over the last dimension, of x or of x + residual.
+
+    Returns a dict: 'y' and, with a residual, 'sum' (x + residual, what is normalised), both like x;
+    'mean' and 'rstd' float32 of x's leading shape, for layer_norm_grad.  `out` may supply tensors of
+    those names ('sum' may be x or residual itself).  weight and bias: x's type or float32."""
+    dev = _gpu(x, "x")
+    rows, cols, xs = _matrix(x, "x", dev, _TYPES)
+    w = _vector(weight, "weight", dev, cols, (x.dtype, torch.float32))
+    b = None if bias is None else _vector(bias, "bias", dev, cols, (weight.dtype,))
+    res = _only(out, ("y", "sum", "mean", "rstd") if residual is not None else ("y", "mean", "rstd"))
+    r, rs = None, 0
+    if residual is not None:
+        if not isinstance(residual, torch.Tensor) or residual.shape != x.shape:
+            raise _bad("residual must be a tensor of x's shape")
+        _, _, rs = _matrix(residual, "residual", dev, (x.dtype,))
+        r = residual.data_ptr()
+        res["sum"] = _dense(res.get("sum"), "sum", dev, x.shape, x.dtype)
+    res["y"] = _dense(res.get("y"), "y", dev, x.shape, x.dtype)
+    for k in ("mean", "rstd"):
+        res[k] = _dense(res.get(k), k, dev, x.shape[:-1], torch.float32)
+    _check(_ops().echo_layer_norm(
+        x.data_ptr(), xs, r, rs, w, b, _TYPES[x.dtype], _TYPES[weight.dtype], rows, cols, float(eps),
+        res["y"].data_ptr(), None if r is None else res["sum"].data_ptr(), res["mean"].data_ptr(),
+        res["rstd"].data_ptr(), dev.index, _stream(dev)))
+    return res
+
+
+def layer_norm_grad(dy, x, weight, mean, rstd, *, grad_residual=None, bias=True, dtype=None, out=None,
+                    accumulate=False, workspace=None):
+    """Gradients of layer_norm from that of y; x is what was normalised ('sum' where a residual was added).
+
+    Returns a dict: 'dx' like x (plus grad_residual, the gradient that reaches x past the norm), 'dweight' and, unless
+    bias=False, 'dbias', of weight's type or of `dtype` (float32).  `out` may supply tensors of those names
+    ('dx' may be dy or grad_residual itself); with accumulate=True it has to supply 'dweight' (and 'dbias'),
+    which are added to."""
+    dev = _gpu(dy, "dy")
+    rows, cols, ds = _matrix(dy, "dy", dev, _TYPES)
+    if not isinstance(x, torch.Tensor) or x.shape != dy.shape:
+        raise _bad("x must be a tensor of dy's shape")
+    _, _, xs = _matrix(x, "x", dev, (dy.dtype,))
+    w = _vector(weight, "weight", dev, cols, (dy.dtype, torch.float32))
+    m = _vector(mean, "mean", dev, rows, (torch.float32,))
+    k = _vector(rstd, "rstd", dev, rows, (torch.float32,))
+    r, rs = None, 0
+    if grad_residual is not None:
+        if not isinstance(grad_residual, torch.Tensor) or grad_residual.shape != dy.shape:
+            raise _bad("grad_residual must be a tensor of dy's shape")
+        _, _, rs = _matrix(grad_residual, "grad_residual", dev, (dy.dtype,))
+        r = grad_residual.data_ptr()
+    names = ("dweight", "dbias") if bias else ("dweight",)
+    res = _only(out, ("dx",) + names)
+    if accumulate and any(n not in res for n in names):
+        raise _bad(f"accumulate adds to out's {' and '.join(names)}")
+    if dtype is None:
+        dtype = res["dweight"].dtype if isinstance(res.get("dweight"), torch.Tensor) else weight.dtype
+    if dtype not in (weight.dtype, torch.float32):
+        raise _bad(f"dtype must be {weight.dtype} or torch.float32 (got {dtype})")
+    res["dx"] = _dense(res.get("dx"), "dx", dev, dy.shape, dy.dtype)
+    for n in names:
+        res[n] = _dense(res.get(n), n, dev, (cols,), dtype)
+    L = _ops()
+    space = _space(workspace, L.echo_layer_norm_grad_workspace(rows, cols), dev)
+    _check(L.echo_layer_norm_grad(
+        dy.data_ptr(), ds, x.data_ptr(), xs, w, m, k, r, rs, _TYPES[dy.dtype], _TYPES[weight.dtype], rows, cols,
+        res["dx"].data_ptr(), res["dweight"].data_ptr(), res["dbias"].data_ptr() if bias else None, _TYPES[dtype],
+        int(bool(accumulate)), *_space_args(space), dev.index, _stream(dev)))
+    return res
+
+
+def embedding(ids, weight, scale=1.0, *, vocab_start=0, out=None):
+    """Rows scale * weight[ids - vocab_start], of shape ids.shape + (cols,) and weight's type.
+
+    weight holds the rows vocab_start .. vocab_start + len(weight) - 1 of the vocabulary; an id
+    outside them (another rank's, or a negative one for padding) gives a row of zeros."""
+    dev = _gpu(ids, "ids")
+    t = _vector(ids, "ids", dev, ids.numel(), _INDEX)
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
+        raise _bad("weight must be a matrix")
+    vocab, cols, ws = _matrix(weight, "weight", dev, _TYPES)
+    res = _dense(out, "out", dev, tuple(ids.shape) + (cols,), weight.dtype)
+    _check(_ops().echo_embedding(t, _INDEX[ids.dtype], weight.data_ptr(), ws, _TYPES[weight.dtype], ids.numel(), cols,
+                                 int(vocab_start), vocab, float(scale), res.data_ptr(), dev.index, _stream(dev)))
+    return res
+
+
+def embedding_grad(ids, dy, vocab, scale=1.0, *, vocab_start=0, dtype=None, out=None, accumulate=False,
+                   workspace=None):
+    """Gradient of embedding's table: [vocab, cols], of dy's type or of `dtype` (float32).
+
+    dy has the shape ids.shape + (cols,).  With accumulate=True the rows that ids name are added to `out` and its
+    other rows are left alone; otherwise every row is written."""
+    dev = _gpu(ids, "ids")
+    t = _vector(ids, "ids", dev, ids.numel(), _INDEX)
+    if not isinstance(dy, torch.Tensor) or dy.dim() != ids.dim() + 1 or dy.shape[:-1] != ids.shape:
+        raise _bad("dy must have the shape of ids and one dimension more")
+    rows, cols, ds = _matrix(dy, "dy", dev, _TYPES)
+    if accumulate and out is None:
+        raise _bad("accumulate adds to out")
+    if dtype is None:
+        dtype = out.dtype if isinstance(out, torch.Tensor) else dy.dtype
+    if dtype not in (dy.dtype, torch.float32):
+        raise _bad(f"dtype must be {dy.dtype} or torch.float32 (got {dtype})")
+    vocab = int(vocab)
+    if vocab < 0:
+        raise _bad("vocab must be >= 0")
+    res = _dense(out, "out", dev, (vocab, cols), dtype)
+    L = _ops()
+    space = _space(workspace, L.echo_embedding_grad_workspace(rows, cols, vocab), dev)
+    _check(L.echo_embedding_grad(
+        t, _INDEX[ids.dtype], dy.data_ptr(), ds, _TYPES[dy.dtype], rows, cols, int(vocab_start), vocab, float(scale),
+        res.data_ptr(), _TYPES[dtype], int(bool(accumulate)), *_space_args(space), dev.index, _stream(dev)))
+    return res
+
+
+def _loss_args(logits, targets):
+    dev = _gpu(logits, "logits")
+    rows, cols, ls = _matrix(logits, "logits", dev, _TYPES)
+    if not isinstance(targets, torch.Tensor) or targets.shape != logits.shape[:-1]:
+        raise _bad("targets must have the leading shape of logits")
+    return dev, rows, cols, ls, _vector(targets, "targets", dev, rows, _INDEX)
+
+
+def _grad_out(t, logits, dev, rows, cols):
+    """(tensor, row stride) of a gradient of logits: new and dense, or the caller's, of any row stride."""
+    if t is None:
+        return torch.empty(logits.shape, dtype=logits.dtype, device=dev), cols
+    n, c, stride = _matrix(t, "grad", dev, (logits.dtype,))
+    if t.shape != logits.shape:
+        raise _bad(f"grad has shape {tuple(t.shape)}, needs {tuple(logits.shape)}")
+    return t, stride
+
+
+def cross_entropy(logits, targets, *, vocab_start=0, vocab_size=None, grad_loss=None, out=None):
+    """Cross entropy of rows of logits; a target outside the vocabulary (-100) marks a row not trained on.
+
+    Whole vocabulary (vocab_size not given): a dict with 'loss' (0 for rows not trained on), 'lse' (log of the sum
+    of exponentials), float32, and, if grad_loss (float32, the gradient of each row's loss) is given, 'grad': that of the
+    logits, in the same pass.  `out` may supply tensors of those names; 'grad' may be logits itself.
+
+    The rows vocab_start .. vocab_start + cols - 1 of a vocabulary of vocab_size, as one tensor-parallel rank holds
+    them: a dict with 'lse' over these rows and 'target', the target's logit or 0 where it is another
+    rank's.  The whole lse is the logarithm of the ranks' sum of exp(lse), the target's logit their sum, and
+    loss = lse - target; cross_entropy_grad then gives each rank its gradient."""
+    dev, rows, cols, ls, t = _loss_args(logits, targets)
+    shape = logits.shape[:-1]
+    if vocab_size is None:
+        if vocab_start:
+            raise _bad("vocab_start needs vocab_size")
+        vocab_size, names = cols, ("loss", "lse")
+    else:
+        if grad_loss is not None:
+            raise _bad("a shard's gradient needs the whole vocabulary's lse: use cross_entropy_grad")
+        names = ("lse", "target")
+    res = _only(out, names + (("grad",) if grad_loss is not None else ()))
+    for n in names:
+        res[n] = _dense(res.get(n), n, dev, shape, torch.float32)
+    g, gs, gl = None, 0, None
+    if grad_loss is not None:
+        gl = _vector(grad_loss, "grad_loss", dev, rows, (torch.float32,))
+        res["grad"], gs = _grad_out(res.get("grad"), logits, dev, rows, cols)
+        g = res["grad"].data_ptr()
+    _check(_ops().echo_cross_entropy(
+        logits.data_ptr(), ls, _TYPES[logits.dtype], t, _INDEX[targets.dtype], rows, cols, int(vocab_start),
+        int(vocab_size), res["lse"].data_ptr(), res["target"].data_ptr() if "target" in res else None,
+        res["loss"].data_ptr() if "loss" in res else None, gl, g, gs, dev.index, _stream(dev)))
+    return res
+
+
+def cross_entropy_grad(logits, targets, lse, grad_loss, *, vocab_start=0, vocab_size=None, out=None):
+    """(exp(logits - lse) - onehot(targets)) * grad_loss, like logits: the gradient of cross entropy for the
+    columns held here, with lse and grad_loss float32 of targets' shape.  `out` may be logits itself."""
+    dev, rows, cols, ls, t = _loss_args(logits, targets)
+    if vocab_size is None:
+        if vocab_start:
+            raise _bad("vocab_start needs vocab_size")
+        vocab_size = cols
+    e = _vector(lse, "lse", dev, rows, (torch.float32,))
+    gl = _vector(grad_loss, "grad_loss", dev, rows, (torch.float32,))
+    res, gs = _grad_out(out, logits, dev, rows, cols)
+    _check(_ops().echo_cross_entropy_grad(
+        logits.data_ptr(), ls, _TYPES[logits.dtype], t, _INDEX[targets.dtype], rows, cols, int(vocab_start),
+        int(vocab_size), e, gl, res.data_ptr(), gs, dev.index, _stream(dev)))
+    return res
