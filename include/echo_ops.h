@@ -14,7 +14,8 @@
  *     softmax statistics are in 32 bits and each output is rounded once;
  *   - a matrix argument is `rows` rows of `cols` contiguous elements, `*_stride` elements apart
  *     (0 to 2^28; 0 repeats one row).  Elements need the alignment of their type only.  Outputs without a
- *     stride argument are dense.  0 <= rows < 2^31, 1 <= cols <= 2^24;
+ *     stride argument are dense.  0 <= rows < 2^31, 1 <= cols <= 2^24, and rows * cols <= 2^38 (else
+ *     ECHO_ERR_RANGE);
  *   - outputs may not overlap inputs or each other unless a call says so (ECHO_ERR_ARG);
  *   - workspaces are scratch: their contents need no initialisation and mean nothing after the call,
  *     so calls on one stream may share one.  Nothing is allocated, cleared by memset or waited for, so
@@ -80,7 +81,7 @@ int echo_embedding(const void *ids, int32_t index_type, const void *weight, int6
  *   dweight[v] = scale * sum of dy[t] over the t with ids[t] = vocab_start + v
  * for every row of the shard (zeros where no token has the id), or with accumulate != 0 added to
  * dweight, whose other rows are then left alone.  dy is of `type`, dweight [vocab][cols] of grad_type
- * (`type` or ECHO_F32).  Tokens are sorted by id first; a row's tokens are summed in ascending order.
+ * (`type` or ECHO_F32); vocab <= 2^26 (else ECHO_ERR_RANGE).  Tokens are sorted by id first; a row's tokens are summed in ascending order.
  * workspace: at least echo_embedding_grad_workspace(rows, cols, vocab) bytes, aligned to 16.
  */
 int64_t echo_embedding_grad_workspace(int64_t rows, int64_t cols, int64_t vocab);

@@ -249,87 +249,253 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
     }
 }
 
-// Workspace of the gradient: where each row's tokens begin, and the tokens sorted by row.
+// Tokens are sorted by their row's slot: 2^bits sorting workgroups take 64 slots each, and a row's
+// workgroup is its low bits, so that the frequent ids, which vocabularies number first, do not meet in one.
+__host__ __device__ __forceinline__ int slot_of(int row, int bits) { return ((row & ((1 << bits) - 1)) << 6) + (row >> bits); }
+int sort_bits(int64_t vocab) {
+    int b = 0;
+    while ((int64_t(kWave) << b) < vocab) ++b;
+    return b;
+}
+
+// Workspace of the gradient: where each slot's tokens begin, the tokens sorted by slot, the row of
+// each sorted place, and two rows of 32-bit sums for every chunk of sorted places: of the run of one row that
+// reaches in from the chunk before, and of the one that goes on into the next.
 struct EmbedSpace {
-    int *begin, *token;
+    int *begin, *token, *row;
+    float *part;
 };
 int64_t round16(int64_t n) { return (n + 15) & ~int64_t(15); }
-EmbedSpace embed_space(void *p, int64_t vocab) {
+EmbedSpace embed_space(void *p, int64_t rows, int64_t vocab) {
     char *c = static_cast<char *>(p);
-    return EmbedSpace{reinterpret_cast<int *>(c), reinterpret_cast<int *>(c + round16((vocab + 1) * 4))};
+    EmbedSpace w;
+    w.begin = reinterpret_cast<int *>(c);
+    w.token = reinterpret_cast<int *>(c += round16(((int64_t(kWave) << sort_bits(vocab)) + 1) * 4));
+    w.row = reinterpret_cast<int *>(c += round16(rows * 4));
+    w.part = reinterpret_cast<float *>(c += round16(rows * 4));
+    return w;
+}
+constexpr int kTile = kWave * kVec;      // columns that a wavefront takes at a time
+int64_t tiles_of(int64_t cols) { return (cols + kTile - 1) / kTile; }
+
+// Sorted places of a chunk: few enough to give the chip wavefronts, and no fewer.
+int embed_chunk(int64_t rows, int64_t cols) {
+    int c = 4;
+    while (c < kWave && (rows + c - 1) / c * tiles_of(cols) > 16384) c *= 2;
+    return c;
 }
 
-// Tokens sorted by row of the shard, ascending within a row.  Each wavefront owns 64 rows (one a lane)
-// and reads every id twice: it counts its rows' tokens and those of the rows before them, which
-// says where its rows begin, and then places its tokens in order.  Lanes whose ids name the same row
-// are placed together, in the order of the lanes.
-template <class I>
-__global__ __launch_bounds__(64) void k_embed_sort(EmbedGradArgs a, EmbedSpace ws) {
-    const int lane = threadIdx.x, first = blockIdx.x * kWave;
+// Tokens sorted by slot, ascending within one.  A workgroup owns 64 slots and reads every
+// id, each wavefront its share of the tokens: they count their rows' tokens (in LDS) and those of the slots
+// before them, which says where each row and each wavefront's part of it begins, and then
+// place the tokens in order.  A lane's place among those of its 64 tokens with the same row follows from six
+// ballots, one for each bit of the row's number in the workgroup.  No scan over workgroups and no atomics whose
+// order matters: one launch sorts.  A lane reads LOADS ids at a time, and a share of as many only once.
+constexpr int kSortWaves = 16;
+template <class I, int LOADS>
+__global__ __launch_bounds__(kSortWaves * kWave) void k_embed_sort(EmbedGradArgs a, EmbedSpace ws, int bits) {
+    __shared__ int counts[kSortWaves][kWave], befores[kSortWaves];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+    const int block = blockIdx.x, mask = (1 << bits) - 1;
     const uint64_t below = (uint64_t(1) << lane) - 1;
-    int count = 0, before = 0;
-    for (int64_t t = 0; t < a.rows; t += kWave) {
-        const int v = t + lane < a.rows ? shard_row(id_at<I>(a.ids, t + lane), a.vocab_start, a.vocab) : -1;
-        before += __popcll(__ballot(v >= 0 && v < first));
-        uint64_t mine = __ballot(v >= first && v - first < kWave);
-        while (mine) {
-            const int row = __shfl(v, __ffsll((unsigned long long)mine) - 1);
-            const uint64_t same = __ballot(v == row);
-            if (lane == row - first) count += __popcll(same);
-            mine &= ~same;
+    const int64_t share = (a.rows + waves * kWave - 1) / (waves * kWave) * kWave;
+    const int64_t lo = share * wave, hi = lo + share < a.rows ? lo + share : a.rows;
+    const bool once = share <= LOADS * kWave;
+    // a token's slot in this workgroup; negative for slots before its own, 64 for others
+    const auto slots_at = [&](int64_t t, int (&v)[LOADS]) {
+        I id[LOADS];
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) {
+            const int64_t u = t + k * kWave + lane;
+            id[k] = static_cast<const I *>(a.ids)[u < hi ? u : hi - 1];
+        }
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) {
+            const int row = shard_row((int64_t)id[k], a.vocab_start, a.vocab), own = row & mask;
+            v[k] = t + k * kWave + lane >= hi || row < 0 || own > block ? kWave : own < block ? -1 : row >> bits;
+        }
+    };
+    counts[wave][lane] = 0;
+    int before = 0, v[LOADS];
+    for (int64_t t = lo; t < hi; t += LOADS * kWave) {
+        slots_at(t, v);
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) {
+            if (t + k * kWave >= hi) break;
+            before += __popcll(__ballot(v[k] < 0));
+            if ((unsigned)v[k] < kWave) atomicAdd(&counts[wave][v[k]], 1);
         }
     }
-    int at = count;      // exclusive prefix sum over the lanes
+    if (lane == 0) befores[wave] = before;
+    __syncthreads();
+    int total = 0, at = 0;      // at: tokens of row `lane` in the wavefronts before this one
+    before = 0;
+    for (int w = 0; w < waves; ++w) {
+        if (w == wave) at = total;
+        total += counts[w][lane];
+        before += befores[w];
+    }
+    int start = total;          // inclusive prefix sum over the lanes, made exclusive
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) {
-        const int up = __shfl_up(at, d);
-        if (lane >= d) at += up;
+        const int up = __shfl_up(start, d);
+        if (lane >= d) start += up;
     }
-    at += before - count;
-    if (first + lane < a.vocab) ws.begin[first + lane] = at;
-    if (first + lane == a.vocab - 1) ws.begin[a.vocab] = at + count;
-    for (int64_t t = 0; t < a.rows; t += kWave) {
-        const int v = t + lane < a.rows ? shard_row(id_at<I>(a.ids, t + lane), a.vocab_start, a.vocab) : -1;
-        uint64_t mine = __ballot(v >= first && v - first < kWave);
-        while (mine) {
-            const int row = __shfl(v, __ffsll((unsigned long long)mine) - 1);
-            const uint64_t same = __ballot(v == row);
-            const int base = __shfl(at, row - first);
-            if (v == row) ws.token[base + __popcll(same & below)] = (int)(t + lane);
-            if (lane == row - first) at += __popcll(same);
-            mine &= ~same;
+    start += before - total;
+    if (wave == 0) {
+        ws.begin[block * kWave + lane] = start;
+        if (block == mask && lane == kWave - 1) ws.begin[block * kWave + kWave] = start + total;
+    }
+    __syncthreads();            // every wavefront has read the counts: they become the next free places
+    volatile int *next = counts[wave];
+    next[lane] = start + at;
+    for (int64_t t = lo; t < hi; t += LOADS * kWave) {
+        if (!once) slots_at(t, v);
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) {
+            if (t + k * kWave >= hi) break;
+            const bool mine = (unsigned)v[k] < kWave;
+            uint64_t same = __ballot(mine);
+            if (!same) continue;
+#pragma unroll
+            for (int b = 0; b < 6; ++b) {
+                const uint64_t set = __ballot(v[k] >> b & 1);
+                same &= v[k] >> b & 1 ? set : ~set;
+            }
+            if (!mine) continue;
+            const int place = next[v[k]] + __popcll(same & below);
+            ws.token[place] = (int)(t + k * kWave + lane);
+            ws.row[place] = block + (v[k] << bits);
+            if (!(same & below)) next[v[k]] = place + __popcll(same);
         }
     }
 }
 
-// One workgroup a row of the table.
+template <class G>
+__device__ __forceinline__ G *row_of(const EmbedGradArgs &a, int row) {
+    return static_cast<G *>(a.dweight) + (int64_t)row * a.cols;
+}
+
+// A wavefront sums one chunk of sorted places over one tile of columns: the rows of the table whose
+// tokens all lie in the chunk are finished, the sums of a run that crosses its ends are left in ws.part.
+// Work is split by tokens, so an id that many tokens share costs no more than many ids.  The wavefronts
+// after those write zeros to the rows that no token names (accumulate: there are none).
 template <class T, class G>
-__global__ __launch_bounds__(256) void k_embed_dw(EmbedGradArgs a, EmbedSpace ws) {
-    for (int v = blockIdx.x; v < a.vocab; v += gridDim.x) {
-        const int lo = a.rows ? ws.begin[v] : 0, hi = a.rows ? ws.begin[v + 1] : 0;
-        if (a.accumulate && lo == hi) continue;
-        G *out = static_cast<G *>(a.dweight) + (int64_t)v * a.cols;
-        for (int c = threadIdx.x * kVec; c < a.cols; c += 256 * kVec) {
-            F8 s = 0.0f;
-            for (int k = lo; k < hi; ++k)
-                s += widen<T>(load8(static_cast<const T *>(a.dy) + (int64_t)ws.token[k] * a.dy_stride, c, a.cols));
-            s *= a.scale;
-            if (a.accumulate) s += widen<G>(load8(out, c, a.cols));
-            store8(out, c, a.cols, round_to<G>(s));
+__global__ __launch_bounds__(256) void k_embed_sum(EmbedGradArgs a, EmbedSpace ws, int bits, int chunk, int64_t sums) {
+    constexpr int kAhead = 4;
+    const int lane = threadIdx.x % kWave;
+    const int64_t id = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave, tiles = (a.cols + kTile - 1) / kTile;
+    if (id >= sums) {
+        for (int64_t v = id - sums; v < a.vocab; v += (int64_t)gridDim.x * 4 - sums) {
+            const int slot = slot_of((int)v, bits);
+            if (a.rows && ws.begin[slot] != ws.begin[slot + 1]) continue;
+            G *out = static_cast<G *>(a.dweight) + v * a.cols;
+            for (int c = lane * kVec; c < a.cols; c += kTile) store8(out, c, a.cols, V8<G>(G(0)));
+        }
+        return;
+    }
+    const int64_t j = id / tiles, base = j * chunk;
+    const int c = (int)(id % tiles) * kTile + lane * kVec;
+    const int64_t n = ws.begin[kWave << bits];
+    if (base >= n) return;
+    const int m = (int)(n - base < chunk ? n - base : chunk);
+    const int row = lane < m ? ws.row[base + lane] : -1, token = lane < m ? ws.token[base + lane] : 0;
+    const int next = base + m < n ? ws.row[base + m] : -1;
+    int after = __shfl_down(row, 1);
+    if (lane == m - 1) after = next;
+    const uint64_t ends = __ballot(lane < m && after != row);
+    bool in = base > 0 && ws.row[base - 1] == __builtin_amdgcn_readlane(row, 0);      // the first run reaches in
+    F8 s = 0.0f;
+    for (int i = 0; i < m; i += kAhead) {
+        V8<T> r[kAhead];
+        V8<G> old[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (i + k >= m || c >= a.cols) continue;
+            r[k] = load8(static_cast<const T *>(a.dy) + (int64_t)__builtin_amdgcn_readlane(token, i + k) * a.dy_stride,
+                         c, a.cols);
+            if (a.accumulate && ends >> (i + k) & 1)
+                old[k] = load8(row_of<G>(a, __builtin_amdgcn_readlane(row, i + k)), c, a.cols);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (i + k >= m || c >= a.cols) continue;
+            s += widen<T>(r[k]);
+            if (!(ends >> (i + k) & 1)) continue;
+            if (in) {
+                store8(ws.part + j * 2 * a.cols, c, a.cols, s);
+            } else {
+                s *= a.scale;
+                if (a.accumulate) s += widen<G>(old[k]);
+                store8(row_of<G>(a, __builtin_amdgcn_readlane(row, i + k)), c, a.cols, round_to<G>(s));
+            }
+            in = false;
+            s = 0.0f;
         }
     }
+    if (c < a.cols && !(ends >> (m - 1) & 1)) store8(ws.part + (j * 2 + !in) * a.cols, c, a.cols, s);
+}
+
+// Finishes the runs that leave the chunk they begin in: the sums of its chunks, four wavefronts taking
+// turns, joined in order.
+template <class G>
+__global__ __launch_bounds__(256) void k_embed_join(EmbedGradArgs a, EmbedSpace ws, int bits, int chunk) {
+    __shared__ F8 lds[3][kWave];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t tiles = (a.cols + kTile - 1) / kTile, j = blockIdx.x / tiles, last = (j + 1) * chunk - 1;
+    // places past the tokens hold no row: they are not looked at, but all three are read at once
+    const int n = ws.begin[kWave << bits], row = ws.row[last], next = ws.row[last + 1];
+    if (last + 1 >= n || row != next) return;
+    const int slot = slot_of(row, bits), lo = ws.begin[slot], hi = ws.begin[slot + 1];
+    if (lo < j * chunk) return;
+    const int c = (int)(blockIdx.x % tiles) * kTile + lane * kVec;
+    const int64_t ends = (hi - 1) / chunk;
+    G *out = row_of<G>(a, row);
+    F8 s = 0.0f;
+    V8<G> old = G(0);
+    if (c < a.cols) {
+        if (wave == 0) {
+            s = load8(ws.part + (j * 2 + 1) * a.cols, c, a.cols);
+            if (a.accumulate) old = load8(out, c, a.cols);
+        }
+#pragma unroll 4
+        for (int64_t k = j + 1 + wave; k <= ends; k += 4) s += load8(ws.part + k * 2 * a.cols, c, a.cols);
+    }
+    if (wave) lds[wave - 1][lane] = s;
+    __syncthreads();
+    if (wave || c >= a.cols) return;
+    for (int w = 0; w < 3; ++w) s += lds[w][lane];
+    s *= a.scale;
+    if (a.accumulate) s += widen<G>(old);
+    store8(out, c, a.cols, round_to<G>(s));
+}
+
+template <class I>
+hipError_t embed_sort(const EmbedGradArgs &a, const EmbedSpace &ws, int bits, hipStream_t s) {
+    const int64_t rounds = (a.rows + kWave - 1) / kWave;
+    const int waves = rounds < kSortWaves ? (int)rounds : kSortWaves;
+    const dim3 grid(1u << bits), block(waves * kWave);
+    return launch(rounds <= kSortWaves       ? k_embed_sort<I, 1>
+                  : rounds <= 4 * kSortWaves ? k_embed_sort<I, 4>
+                                             : k_embed_sort<I, 16>,
+                  grid, block, s, a, ws, bits);
 }
 
 template <class T, class G>
 hipError_t embed_grad(const EmbedGradArgs &a, int index_type, hipStream_t s) {
-    const EmbedSpace ws = embed_space(a.workspace, a.vocab);
-    const dim3 sorters((unsigned)((a.vocab + kWave - 1) / kWave));
+    const EmbedSpace ws = embed_space(a.workspace, a.rows, a.vocab);
+    const int bits = sort_bits(a.vocab), chunk = embed_chunk(a.rows, a.cols);
+    const int64_t chunks = (a.rows + chunk - 1) / chunk, tiles = tiles_of(a.cols);
+    const int64_t sums = (chunks * tiles + 3) / 4 * 4;
     hipError_t e = hipSuccess;
-    if (a.rows)
-        e = index_type == ECHO_I64 ? launch(k_embed_sort<int64_t>, sorters, dim3(kWave), s, a, ws)
-                                   : launch(k_embed_sort<int32_t>, sorters, dim3(kWave), s, a, ws);
-    if (e) return e;
-    return launch(k_embed_dw<T, G>, dim3(grid_of(a.vocab)), dim3(256), s, a, ws);
+    if (a.rows) {
+        e = index_type == ECHO_I64 ? embed_sort<int64_t>(a, ws, bits, s) : embed_sort<int32_t>(a, ws, bits, s);
+        if (e) return e;
+    }
+    const int64_t fills = a.accumulate ? 0 : grid_of((a.vocab + 3) / 4);
+    if ((e = launch(k_embed_sum<T, G>, dim3((unsigned)(sums / 4 + fills)), dim3(256), s, a, ws, bits, chunk, sums))) return e;
+    if (chunks > 1) e = launch(k_embed_join<G>, dim3((unsigned)((chunks - 1) * tiles)), dim3(256), s, a, ws, bits, chunk);
+    return e;
 }
 
 // ---------------------------------------------------------------- cross entropy
@@ -412,8 +578,10 @@ __global__ __launch_bounds__(256) void k_loss_grad(LossArgs a) {
 }  // namespace
 
 int norm_grad_parts(int64_t rows, int64_t) { return (int)(rows < 64 ? rows : 64); }
-int64_t embed_grad_bytes(int64_t rows, int64_t, int64_t vocab) {
-    return rows ? round16((vocab + 1) * 4) + round16(rows * 4) : 0;
+int64_t embed_grad_bytes(int64_t rows, int64_t cols, int64_t vocab) {
+    if (!rows) return 0;
+    const int chunk = embed_chunk(rows, cols);
+    return round16(((int64_t(kWave) << sort_bits(vocab)) + 1) * 4) + 2 * round16(rows * 4) + (rows + chunk - 1) / chunk * 2 * cols * 4;
 }
 
 hipError_t launch_norm(const NormArgs &a, int type, int weight_type, hipStream_t s) {

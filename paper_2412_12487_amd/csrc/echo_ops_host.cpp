@@ -17,6 +17,8 @@ namespace {
 
 constexpr int64_t kMaxRows = INT32_MAX;
 constexpr int64_t kMaxCols = int64_t(1) << 24;
+constexpr int64_t kMaxElements = int64_t(1) << 38; // grids stay below 2^32 work-items
+constexpr int64_t kMaxSorted = int64_t(1) << 26;   // rows of a table whose gradient's tokens are sorted
 constexpr int64_t kMaxStride = int64_t(1) << 28;   // 2^31 rows of 4-byte elements stay below 2^62 bytes
 
 int64_t elem(int32_t type) { return type == ECHO_F32 ? 4 : 2; }
@@ -65,6 +67,8 @@ int check_vector(const char *name, const void *p, int64_t e, bool required) {
 int check_sizes(int64_t rows, int64_t cols) {
     if (rows < 0 || rows > kMaxRows) return set_error(ECHO_ERR_ARG, "rows = %lld outside [0, 2^31)", (long long)rows);
     if (cols < 1 || cols > kMaxCols) return set_error(ECHO_ERR_ARG, "cols = %lld outside [1, 2^24]", (long long)cols);
+    if (rows * cols > kMaxElements)
+        return set_error(ECHO_ERR_RANGE, "%lld rows of %lld pass 2^38 elements", (long long)rows, (long long)cols);
     return ECHO_OK;
 }
 int check_types(int32_t type, int32_t other, const char *what) {
@@ -215,7 +219,7 @@ int echo_embedding(const void *ids, int32_t index_type, const void *weight, int6
 }
 
 int64_t echo_embedding_grad_workspace(int64_t rows, int64_t cols, int64_t vocab) {
-    if (rows < 0 || rows > kMaxRows || cols < 1 || cols > kMaxCols || vocab < 0 || vocab > kMaxRows) return 0;
+    if (rows < 0 || rows > kMaxRows || cols < 1 || cols > kMaxCols || vocab < 0 || vocab > kMaxSorted) return 0;
     return embed_grad_bytes(rows, cols, vocab);
 }
 
@@ -232,6 +236,7 @@ int echo_embedding_grad(const void *ids, int32_t index_type, const void *dy, int
     ECHO_TRY(check_vector("ids", ids, ie, rows > 0));
     ECHO_TRY(check_matrix("dy", dy, rows, dy_stride, e));
     ECHO_TRY(check_matrix("dweight", dweight, vocab, cols, ge));
+    if (vocab > kMaxSorted) return set_error(ECHO_ERR_RANGE, "vocab = %lld passes 2^26", (long long)vocab);
     const int64_t need = echo_embedding_grad_workspace(rows, cols, vocab);
     ECHO_TRY(check_workspace(workspace, workspace_bytes, need));
     ECHO_TRY(check_spans({{"dweight", dweight, vocab * cols * ge, 0}, {"workspace", workspace, need, 0}},

@@ -125,6 +125,13 @@ def test_refusals_come_before_the_device(E, L, i):
     assert msg in L.echo_last_error().decode()
 
 
+def test_more_elements_than_a_grid_holds_are_out_of_range(E, L):
+    for call in (_norm, _norm_grad, _embed, _embed_grad, _loss_grad):
+        kw = {} if call is not _loss_grad else dict(whole=1 << 20)
+        assert call(L, rows=(1 << 18) + 1, cols=1 << 20, **kw) == E.ECHO_ERR_RANGE
+    assert _embed_grad(L, vocab=(1 << 26) + 1) == E.ECHO_ERR_RANGE
+
+
 def test_calls_without_work_succeed_and_clear_the_error(E, L):
     assert _norm(L, cols=0) == E.ECHO_ERR_ARG and L.echo_last_error()
     assert _norm(L, rows=0, x=None, y=None, w=None, b=None, mean=None, rstd=None) == E.ECHO_OK
@@ -142,5 +149,5 @@ def test_workspace_sizes(L):
     assert norm(-1, 8) == norm(8, 0) == embed(8, 0, 8) == embed(-1, 8, 8) == embed(8, 8, -1) == embed(0, 8, 8) == 0
     assert norm(8, 64) >= 8 * 64 and embed(8, 64, 100) >= 4 * 108
     assert 0 < norm((1 << 31) - 1, 1 << 24) < 1 << 50
-    assert 0 < embed((1 << 31) - 1, 1 << 24, (1 << 31) - 1)
+    assert 0 < embed((1 << 31) - 1, 1 << 24, 1 << 26) < 1 << 56 and embed(8, 8, (1 << 26) + 1) == 0
     assert ctypes.sizeof(ctypes.c_int64) == 8
