@@ -43,6 +43,25 @@ __device__ __forceinline__ void store8(T *row, int col, int cols, V8<T> v) {
     for (int j = 0; j < kVec; ++j)
         if (col + j < cols) row[col + j] = v[j];
 }
+// load8 of data that nothing reads again soon.
+template <class T>
+__device__ __forceinline__ V8<T> stream8(const T *row, int col, int cols, T fill = T(0)) {
+    if (col + kVec <= cols) return __builtin_nontemporal_load(reinterpret_cast<const V8<T> *>(row + col));
+    return load8(row, col, cols, fill);
+}
+// A wavefront writes zeros to a row, 16 bytes a lane.
+template <class T>
+__device__ __forceinline__ void zero_row(T *row, int cols) {
+    constexpr int n = 16 / sizeof(T);
+    typedef T Z __attribute__((ext_vector_type(n), aligned(sizeof(T))));
+    for (int c = threadIdx.x % kWave * n; c < cols; c += kWave * n) {
+        if (c + n <= cols) {
+            *reinterpret_cast<Z *>(row + c) = Z(T(0));
+        } else {
+            for (int j = c; j < cols; ++j) row[j] = T(0);
+        }
+    }
+}
 template <class T>
 __device__ __forceinline__ F8 widen(V8<T> v) {
     return __builtin_convertvector(v, F8);
@@ -260,19 +279,22 @@ int sort_bits(int64_t vocab) {
 
 // Workspace of the gradient: where each slot's tokens begin, the tokens sorted by slot, the row of
 // each sorted place, and two rows of 32-bit sums for every chunk of sorted places: of the run of one row that
-// reaches in from the chunk before, and of the one that goes on into the next.
+// reaches in from the chunk before, and of the one that goes on into the next.  runs[0].x counts the runs
+// that leave the chunk they begin in, runs[1 ..] are those: row, first and last chunk, in any order.
 struct EmbedSpace {
     int *begin, *token, *row;
+    int4 *runs;
     float *part;
 };
 int64_t round16(int64_t n) { return (n + 15) & ~int64_t(15); }
-EmbedSpace embed_space(void *p, int64_t rows, int64_t vocab) {
+EmbedSpace embed_space(void *p, int64_t rows, int64_t vocab, int64_t chunks) {
     char *c = static_cast<char *>(p);
     EmbedSpace w;
     w.begin = reinterpret_cast<int *>(c);
     w.token = reinterpret_cast<int *>(c += round16(((int64_t(kWave) << sort_bits(vocab)) + 1) * 4));
     w.row = reinterpret_cast<int *>(c += round16(rows * 4));
-    w.part = reinterpret_cast<float *>(c += round16(rows * 4));
+    w.runs = reinterpret_cast<int4 *>(c += round16(rows * 4));
+    w.part = reinterpret_cast<float *>(c + (chunks + 1) * 16);
     return w;
 }
 constexpr int kTile = kWave * kVec;      // columns that a wavefront takes at a time
@@ -301,31 +323,31 @@ __global__ __launch_bounds__(kSortWaves * kWave) void k_embed_sort(EmbedGradArgs
     const int64_t share = (a.rows + waves * kWave - 1) / (waves * kWave) * kWave;
     const int64_t lo = share * wave, hi = lo + share < a.rows ? lo + share : a.rows;
     const bool once = share <= LOADS * kWave;
-    // a token's slot in this workgroup; negative for slots before its own, 64 for others
-    const auto slots_at = [&](int64_t t, int (&v)[LOADS]) {
+    // A token's row with the workgroup's number taken out of its low bits and those bits turned to the
+    // top: its slot here if that is below 64.  No row (~0) is of the last group and of no slot.
+    int before = 0;
+    unsigned v[LOADS];
+    const auto slots_at = [&](int64_t t, bool count) {
         I id[LOADS];
+        const bool all = t + LOADS * kWave <= hi;
 #pragma unroll
         for (int k = 0; k < LOADS; ++k) {
             const int64_t u = t + k * kWave + lane;
-            id[k] = static_cast<const I *>(a.ids)[u < hi ? u : hi - 1];
+            id[k] = static_cast<const I *>(a.ids)[all || u < hi ? u : hi - 1];
         }
 #pragma unroll
         for (int k = 0; k < LOADS; ++k) {
-            const int row = shard_row((int64_t)id[k], a.vocab_start, a.vocab), own = row & mask;
-            v[k] = t + k * kWave + lane >= hi || row < 0 || own > block ? kWave : own < block ? -1 : row >> bits;
+            unsigned row = (unsigned)shard_row((int64_t)id[k], a.vocab_start, a.vocab);
+            if (!all && t + k * kWave + lane >= hi) row = ~0u;
+            const unsigned x = row ^ (unsigned)block;
+            v[k] = __builtin_amdgcn_alignbit(x, x, bits);
+            if (!count) continue;
+            before += __popcll(__ballot((int)(row & mask) < block));
+            if (v[k] < kWave) atomicAdd(&counts[wave][v[k]], 1);
         }
     };
     counts[wave][lane] = 0;
-    int before = 0, v[LOADS];
-    for (int64_t t = lo; t < hi; t += LOADS * kWave) {
-        slots_at(t, v);
-#pragma unroll
-        for (int k = 0; k < LOADS; ++k) {
-            if (t + k * kWave >= hi) break;
-            before += __popcll(__ballot(v[k] < 0));
-            if ((unsigned)v[k] < kWave) atomicAdd(&counts[wave][v[k]], 1);
-        }
-    }
+    for (int64_t t = lo; t < hi; t += LOADS * kWave) slots_at(t, true);
     if (lane == 0) befores[wave] = before;
     __syncthreads();
     int total = 0, at = 0;      // at: tokens of row `lane` in the wavefronts before this one
@@ -344,28 +366,31 @@ __global__ __launch_bounds__(kSortWaves * kWave) void k_embed_sort(EmbedGradArgs
     start += before - total;
     if (wave == 0) {
         ws.begin[block * kWave + lane] = start;
+        if (block == 0 && lane == 0) ws.runs[0].x = 0;
         if (block == mask && lane == kWave - 1) ws.begin[block * kWave + kWave] = start + total;
     }
     __syncthreads();            // every wavefront has read the counts: they become the next free places
     volatile int *next = counts[wave];
     next[lane] = start + at;
     for (int64_t t = lo; t < hi; t += LOADS * kWave) {
-        if (!once) slots_at(t, v);
+        if (!once) slots_at(t, false);
 #pragma unroll
         for (int k = 0; k < LOADS; ++k) {
-            if (t + k * kWave >= hi) break;
-            const bool mine = (unsigned)v[k] < kWave;
+            const bool mine = v[k] < kWave;
             uint64_t same = __ballot(mine);
             if (!same) continue;
+            if (same & (same - 1)) {      // more than one: who else has this lane's slot
 #pragma unroll
-            for (int b = 0; b < 6; ++b) {
-                const uint64_t set = __ballot(v[k] >> b & 1);
-                same &= v[k] >> b & 1 ? set : ~set;
+                for (int b = 0; b < 6; ++b) {
+                    const bool bit = v[k] >> b & 1;
+                    const uint64_t set = __ballot(bit);
+                    same &= bit ? set : ~set;
+                }
             }
             if (!mine) continue;
             const int place = next[v[k]] + __popcll(same & below);
             ws.token[place] = (int)(t + k * kWave + lane);
-            ws.row[place] = block + (v[k] << bits);
+            ws.row[place] = block + (int)(v[k] << bits);
             if (!(same & below)) next[v[k]] = place + __popcll(same);
         }
     }
@@ -389,8 +414,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedGradArgs a, EmbedSpace w
         for (int64_t v = id - sums; v < a.vocab; v += (int64_t)gridDim.x * 4 - sums) {
             const int slot = slot_of((int)v, bits);
             if (a.rows && ws.begin[slot] != ws.begin[slot + 1]) continue;
-            G *out = static_cast<G *>(a.dweight) + v * a.cols;
-            for (int c = lane * kVec; c < a.cols; c += kTile) store8(out, c, a.cols, V8<G>(G(0)));
+            zero_row(row_of<G>(a, (int)v), a.cols);
         }
         return;
     }
@@ -412,7 +436,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedGradArgs a, EmbedSpace w
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (i + k >= m || c >= a.cols) continue;
-            r[k] = load8(static_cast<const T *>(a.dy) + (int64_t)__builtin_amdgcn_readlane(token, i + k) * a.dy_stride,
+            r[k] = stream8(static_cast<const T *>(a.dy) + (int64_t)__builtin_amdgcn_readlane(token, i + k) * a.dy_stride,
                          c, a.cols);
             if (a.accumulate && ends >> (i + k) & 1)
                 old[k] = load8(row_of<G>(a, __builtin_amdgcn_readlane(row, i + k)), c, a.cols);
@@ -433,41 +457,46 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedGradArgs a, EmbedSpace w
             s = 0.0f;
         }
     }
-    if (c < a.cols && !(ends >> (m - 1) & 1)) store8(ws.part + (j * 2 + !in) * a.cols, c, a.cols, s);
+    if (ends >> (m - 1) & 1) return;
+    if (c < a.cols) store8(ws.part + (j * 2 + !in) * a.cols, c, a.cols, s);
+    if (!in && c == 0) {
+        const int own = __builtin_amdgcn_readlane(row, m - 1), end = ws.begin[slot_of(own, bits) + 1];
+        ws.runs[1 + atomicAdd(&ws.runs[0].x, 1)] = make_int4(own, (int)j, (end - 1) / chunk, 0);
+    }
 }
 
-// Finishes the runs that leave the chunk they begin in: the sums of its chunks, four wavefronts taking
-// turns, joined in order.
+// Finishes the runs that leave the chunk they begin in: the sums of a run's chunks, four wavefronts
+// taking turns, joined in order.
 template <class G>
-__global__ __launch_bounds__(256) void k_embed_join(EmbedGradArgs a, EmbedSpace ws, int bits, int chunk) {
+__global__ __launch_bounds__(256) void k_embed_join(EmbedGradArgs a, EmbedSpace ws) {
     __shared__ F8 lds[3][kWave];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int64_t tiles = (a.cols + kTile - 1) / kTile, j = blockIdx.x / tiles, last = (j + 1) * chunk - 1;
-    // places past the tokens hold no row: they are not looked at, but all three are read at once
-    const int n = ws.begin[kWave << bits], row = ws.row[last], next = ws.row[last + 1];
-    if (last + 1 >= n || row != next) return;
-    const int slot = slot_of(row, bits), lo = ws.begin[slot], hi = ws.begin[slot + 1];
-    if (lo < j * chunk) return;
-    const int c = (int)(blockIdx.x % tiles) * kTile + lane * kVec;
-    const int64_t ends = (hi - 1) / chunk;
-    G *out = row_of<G>(a, row);
-    F8 s = 0.0f;
-    V8<G> old = G(0);
-    if (c < a.cols) {
-        if (wave == 0) {
-            s = load8(ws.part + (j * 2 + 1) * a.cols, c, a.cols);
-            if (a.accumulate) old = load8(out, c, a.cols);
+    const int64_t tiles = (a.cols + kTile - 1) / kTile, n = ws.runs[0].x * tiles;
+    for (int64_t id = blockIdx.x; id < n; id += gridDim.x) {
+        const int4 run = ws.runs[1 + id / tiles];
+        const int64_t j = run.y;
+        const int c = (int)(id % tiles) * kTile + lane * kVec;
+        G *out = row_of<G>(a, run.x);
+        F8 s = 0.0f;
+        V8<G> old = G(0);
+        if (c < a.cols) {
+            if (wave == 0) {
+                s = load8(ws.part + (j * 2 + 1) * a.cols, c, a.cols);
+                if (a.accumulate) old = load8(out, c, a.cols);
+            }
+#pragma unroll 8
+            for (int64_t k = j + 1 + wave; k <= run.z; k += 4) s += load8(ws.part + k * 2 * a.cols, c, a.cols);
         }
-#pragma unroll 4
-        for (int64_t k = j + 1 + wave; k <= ends; k += 4) s += load8(ws.part + k * 2 * a.cols, c, a.cols);
+        if (wave) lds[wave - 1][lane] = s;
+        __syncthreads();
+        if (!wave && c < a.cols) {
+            for (int w = 0; w < 3; ++w) s += lds[w][lane];
+            s *= a.scale;
+            if (a.accumulate) s += widen<G>(old);
+            store8(out, c, a.cols, round_to<G>(s));
+        }
+        __syncthreads();
     }
-    if (wave) lds[wave - 1][lane] = s;
-    __syncthreads();
-    if (wave || c >= a.cols) return;
-    for (int w = 0; w < 3; ++w) s += lds[w][lane];
-    s *= a.scale;
-    if (a.accumulate) s += widen<G>(old);
-    store8(out, c, a.cols, round_to<G>(s));
 }
 
 template <class I>
@@ -483,10 +512,10 @@ hipError_t embed_sort(const EmbedGradArgs &a, const EmbedSpace &ws, int bits, hi
 
 template <class T, class G>
 hipError_t embed_grad(const EmbedGradArgs &a, int index_type, hipStream_t s) {
-    const EmbedSpace ws = embed_space(a.workspace, a.rows, a.vocab);
     const int bits = sort_bits(a.vocab), chunk = embed_chunk(a.rows, a.cols);
     const int64_t chunks = (a.rows + chunk - 1) / chunk, tiles = tiles_of(a.cols);
     const int64_t sums = (chunks * tiles + 3) / 4 * 4;
+    const EmbedSpace ws = embed_space(a.workspace, a.rows, a.vocab, chunks);
     hipError_t e = hipSuccess;
     if (a.rows) {
         e = index_type == ECHO_I64 ? embed_sort<int64_t>(a, ws, bits, s) : embed_sort<int32_t>(a, ws, bits, s);
@@ -494,7 +523,9 @@ hipError_t embed_grad(const EmbedGradArgs &a, int index_type, hipStream_t s) {
     }
     const int64_t fills = a.accumulate ? 0 : grid_of((a.vocab + 3) / 4);
     if ((e = launch(k_embed_sum<T, G>, dim3((unsigned)(sums / 4 + fills)), dim3(256), s, a, ws, bits, chunk, sums))) return e;
-    if (chunks > 1) e = launch(k_embed_join<G>, dim3((unsigned)((chunks - 1) * tiles)), dim3(256), s, a, ws, bits, chunk);
+    // as many workgroups as the chip holds: how many runs there are to join is not known here
+    const int64_t joins = (chunks - 1) * tiles;
+    if (joins > 0) e = launch(k_embed_join<G>, dim3((unsigned)(joins < 2048 ? joins : 2048)), dim3(256), s, a, ws);
     return e;
 }
 
@@ -581,7 +612,8 @@ int norm_grad_parts(int64_t rows, int64_t) { return (int)(rows < 64 ? rows : 64)
 int64_t embed_grad_bytes(int64_t rows, int64_t cols, int64_t vocab) {
     if (!rows) return 0;
     const int chunk = embed_chunk(rows, cols);
-    return round16(((int64_t(kWave) << sort_bits(vocab)) + 1) * 4) + 2 * round16(rows * 4) + (rows + chunk - 1) / chunk * 2 * cols * 4;
+    return round16(((int64_t(kWave) << sort_bits(vocab)) + 1) * 4) + 2 * round16(rows * 4) +
+           ((rows + chunk - 1) / chunk + 1) * 16 + (rows + chunk - 1) / chunk * 2 * cols * 4;
 }
 
 hipError_t launch_norm(const NormArgs &a, int type, int weight_type, hipStream_t s) {
