@@ -278,9 +278,10 @@ int sort_bits(int64_t vocab) {
 }
 
 // Workspace of the gradient: where each slot's tokens begin, the tokens sorted by slot, the row of
-// each sorted place, and two rows of 32-bit sums for every chunk of sorted places: of the run of one row that
-// reaches in from the chunk before, and of the one that goes on into the next.  runs[0].x counts the runs
-// that leave the chunk they begin in, runs[1 ..] are those: row, first and last chunk, in any order.
+// each sorted place, and two rows of 32-bit sums for every chunk of sorted places, for the runs of tokens of one
+// row that are longer than a chunk: of the run that reaches in from the chunk before, and of the one that goes
+// on into the next.  runs[0].x counts those runs, runs[1 ..] are they: row, first and last chunk, in any
+// order.
 struct EmbedSpace {
     int *begin, *token, *row;
     int4 *runs;
@@ -300,10 +301,11 @@ EmbedSpace embed_space(void *p, int64_t rows, int64_t vocab, int64_t chunks) {
 constexpr int kTile = kWave * kVec;      // columns that a wavefront takes at a time
 int64_t tiles_of(int64_t cols) { return (cols + kTile - 1) / kTile; }
 
-// Sorted places of a chunk: few enough to give the chip wavefronts, and no fewer.
+// Sorted places of a chunk: few enough to give the chip wavefronts, and no fewer.  A wavefront looks at two
+// chunks, one place a lane.
 int embed_chunk(int64_t rows, int64_t cols) {
     int c = 4;
-    while (c < kWave && (rows + c - 1) / c * tiles_of(cols) > 16384) c *= 2;
+    while (c < kWave / 2 && (rows + c - 1) / c * tiles_of(cols) > 16384) c *= 2;
     return c;
 }
 
@@ -401,10 +403,11 @@ __device__ __forceinline__ G *row_of(const EmbedGradArgs &a, int row) {
     return static_cast<G *>(a.dweight) + (int64_t)row * a.cols;
 }
 
-// A wavefront sums one chunk of sorted places over one tile of columns: the rows of the table whose
-// tokens all lie in the chunk are finished, the sums of a run that crosses its ends are left in ws.part.
-// Work is split by tokens, so an id that many tokens share costs no more than many ids.  The wavefronts
-// after those write zeros to the rows that no token names (accumulate: there are none).
+// A wavefront sums the runs that begin in one chunk of sorted places over one tile of columns.  Runs
+// of up to a chunk are finished, past the chunk's end where they go on; of a longer run every chunk's
+// wavefront leaves the sum of its places in ws.part.  Work is split by tokens, so an id that many tokens
+// share costs no more than many ids.  The wavefronts after those write zeros to the rows that no token names
+// (accumulate: there are none).
 template <class T, class G>
 __global__ __launch_bounds__(256) void k_embed_sum(EmbedGradArgs a, EmbedSpace ws, int bits, int chunk, int64_t sums) {
     constexpr int kAhead = 4;
@@ -422,51 +425,59 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedGradArgs a, EmbedSpace w
     const int c = (int)(id % tiles) * kTile + lane * kVec;
     const int64_t n = ws.begin[kWave << bits];
     if (base >= n) return;
-    const int m = (int)(n - base < chunk ? n - base : chunk);
-    const int row = lane < m ? ws.row[base + lane] : -1, token = lane < m ? ws.token[base + lane] : 0;
-    const int next = base + m < n ? ws.row[base + m] : -1;
-    int after = __shfl_down(row, 1);
-    if (lane == m - 1) after = next;
-    const uint64_t ends = __ballot(lane < m && after != row);
-    bool in = base > 0 && ws.row[base - 1] == __builtin_amdgcn_readlane(row, 0);      // the first run reaches in
+    const int m = (int)(n - base < chunk ? n - base : chunk);      // places of this chunk
+    const int64_t at = base + lane;
+    const bool seen = lane < 2 * chunk && at < n;                  // places of this one and the next
+    const int row = seen ? ws.row[at] : -1, token = seen ? ws.token[at] : 0;
+    const int past = j > 0 && lane < chunk ? ws.row[at - chunk] : -1;
+    const int first = __builtin_amdgcn_readlane(row, 0), last = __builtin_amdgcn_readlane(row, m - 1);
+    // the run that reaches in: places before the chunk, and in it (as far as is seen)
+    const int before = __popcll(__ballot(past == first)), head = __popcll(__ballot(row == first));
+    const bool in = before > 0, in_long = in && before + head > chunk;
+    // the run at the chunk's end, if it begins here
+    const uint64_t same = __ballot(row == last);
+    const int tail = __ffsll((unsigned long long)same) - 1, length = __popcll(same);
+    const bool out_long = !(in && tail == 0) && length > chunk;
+    const int begin = in && !in_long ? head : 0;
+    const int end = out_long || (in && tail == 0) ? m : tail + length;
+    const int after = __shfl_down(row, 1);
+    const uint64_t ends = __ballot(lane < end && (lane == end - 1 || after != row));
+    bool inner = !in_long;
     F8 s = 0.0f;
-    for (int i = 0; i < m; i += kAhead) {
+    for (int i = begin; i < end; i += kAhead) {
         V8<T> r[kAhead];
         V8<G> old[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            if (i + k >= m || c >= a.cols) continue;
+            if (i + k >= end || c >= a.cols) continue;
             r[k] = stream8(static_cast<const T *>(a.dy) + (int64_t)__builtin_amdgcn_readlane(token, i + k) * a.dy_stride,
-                         c, a.cols);
+                           c, a.cols);
             if (a.accumulate && ends >> (i + k) & 1)
                 old[k] = load8(row_of<G>(a, __builtin_amdgcn_readlane(row, i + k)), c, a.cols);
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            if (i + k >= m || c >= a.cols) continue;
+            if (i + k >= end || c >= a.cols) continue;
             s += widen<T>(r[k]);
             if (!(ends >> (i + k) & 1)) continue;
-            if (in) {
-                store8(ws.part + j * 2 * a.cols, c, a.cols, s);
+            if (!inner || (out_long && i + k >= tail)) {
+                store8(ws.part + (j * 2 + inner) * a.cols, c, a.cols, s);
             } else {
                 s *= a.scale;
                 if (a.accumulate) s += widen<G>(old[k]);
                 store8(row_of<G>(a, __builtin_amdgcn_readlane(row, i + k)), c, a.cols, round_to<G>(s));
             }
-            in = false;
+            inner = true;
             s = 0.0f;
         }
     }
-    if (ends >> (m - 1) & 1) return;
-    if (c < a.cols) store8(ws.part + (j * 2 + !in) * a.cols, c, a.cols, s);
-    if (!in && c == 0) {
-        const int own = __builtin_amdgcn_readlane(row, m - 1), end = ws.begin[slot_of(own, bits) + 1];
-        ws.runs[1 + atomicAdd(&ws.runs[0].x, 1)] = make_int4(own, (int)j, (end - 1) / chunk, 0);
-    }
+    if (out_long && c == 0)
+        ws.runs[1 + atomicAdd(&ws.runs[0].x, 1)] =
+            make_int4(last, (int)j, (ws.begin[slot_of(last, bits) + 1] - 1) / chunk, 0);
 }
 
-// Finishes the runs that leave the chunk they begin in: the sums of a run's chunks, four wavefronts
-// taking turns, joined in order.
+// Finishes the runs longer than a chunk: the sums of a run's chunks, four wavefronts taking turns, joined in
+// order.
 template <class G>
 __global__ __launch_bounds__(256) void k_embed_join(EmbedGradArgs a, EmbedSpace ws) {
     __shared__ F8 lds[3][kWave];
