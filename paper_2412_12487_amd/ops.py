@@ -115,10 +115,13 @@ def _vector(t, name, dev, n, types):
     return t.data_ptr()
 
 
+def _like(t):
+    """A new dense tensor like t."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 def _dense(t, name, dev, shape, dtype):
-    """An output: the caller's tensor, checked, or a new one."""
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
+    """An output that the caller supplies, checked."""
     if not isinstance(t, torch.Tensor):
         raise _bad(f"{name} must be a torch tensor")
     if t.device != dev:
@@ -145,12 +148,16 @@ def _space_args(space):
     return (None, 0) if space is None else (space.data_ptr(), space.numel() * space.element_size())
 
 
-def _stream(dev):
-    return torch.cuda.current_stream(dev).cuda_stream
+# Handle of the current stream of GPU `index`: torch.cuda.current_stream(...).cuda_stream without the
+# Stream object around it (1.7 us, a tenth of a small call)
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _only(out, names):
-    out = dict(out or {})
+    if not out:
+        return {}
+    out = dict(out)
     for k in out:
         if k not in names:
             raise _bad(f"out has no entry {k!r} here (entries: {', '.join(names)})")
@@ -174,14 +181,16 @@ def layer_norm(x, weight, bias=None, eps=1e-5, *, residual=None, out=None):
             raise _bad("residual must be a tensor of x's shape")
         _, _, rs = _matrix(residual, "residual", dev, (x.dtype,))
         r = residual.data_ptr()
-        res["sum"] = _dense(res.get("sum"), "sum", dev, x.shape, x.dtype)
-    res["y"] = _dense(res.get("y"), "y", dev, x.shape, x.dtype)
+        res["sum"] = _dense(res["sum"], "sum", dev, x.shape, x.dtype) if "sum" in res else _like(x)
+    res["y"] = _dense(res["y"], "y", dev, x.shape, x.dtype) if "y" in res else _like(x)
+    lead = x.shape[:-1]
     for k in ("mean", "rstd"):
-        res[k] = _dense(res.get(k), k, dev, x.shape[:-1], torch.float32)
+        res[k] = (_dense(res[k], k, dev, lead, torch.float32) if k in res
+                  else x.new_empty(lead, dtype=torch.float32))
     _check(_ops().echo_layer_norm(
         x.data_ptr(), xs, r, rs, w, b, _TYPES[x.dtype], _TYPES[weight.dtype], rows, cols, float(eps),
         res["y"].data_ptr(), None if r is None else res["sum"].data_ptr(), res["mean"].data_ptr(),
-        res["rstd"].data_ptr(), dev.index, _stream(dev)))
+        res["rstd"].data_ptr(), dev.index, _stream(dev.index)))
     return res
 
 
@@ -215,15 +224,15 @@ def layer_norm_grad(dy, x, weight, mean, rstd, *, grad_residual=None, bias=True,
         dtype = res["dweight"].dtype if isinstance(res.get("dweight"), torch.Tensor) else weight.dtype
     if dtype not in (weight.dtype, torch.float32):
         raise _bad(f"dtype must be {weight.dtype} or torch.float32 (got {dtype})")
-    res["dx"] = _dense(res.get("dx"), "dx", dev, dy.shape, dy.dtype)
+    res["dx"] = _dense(res["dx"], "dx", dev, dy.shape, dy.dtype) if "dx" in res else _like(dy)
     for n in names:
-        res[n] = _dense(res.get(n), n, dev, (cols,), dtype)
+        res[n] = _dense(res[n], n, dev, (cols,), dtype) if n in res else weight.new_empty((cols,), dtype=dtype)
     L = _ops()
     space = _space(workspace, L.echo_layer_norm_grad_workspace(rows, cols), dev)
     _check(L.echo_layer_norm_grad(
         dy.data_ptr(), ds, x.data_ptr(), xs, w, m, k, r, rs, _TYPES[dy.dtype], _TYPES[weight.dtype], rows, cols,
         res["dx"].data_ptr(), res["dweight"].data_ptr(), res["dbias"].data_ptr() if bias else None, _TYPES[dtype],
-        int(bool(accumulate)), *_space_args(space), dev.index, _stream(dev)))
+        int(bool(accumulate)), *_space_args(space), dev.index, _stream(dev.index)))
     return res
 
 
@@ -237,9 +246,10 @@ def embedding(ids, weight, scale=1.0, *, vocab_start=0, out=None):
     if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
         raise _bad("weight must be a matrix")
     vocab, cols, ws = _matrix(weight, "weight", dev, _TYPES)
-    res = _dense(out, "out", dev, tuple(ids.shape) + (cols,), weight.dtype)
+    shape = ids.shape + (cols,)
+    res = weight.new_empty(shape) if out is None else _dense(out, "out", dev, shape, weight.dtype)
     _check(_ops().echo_embedding(t, _INDEX[ids.dtype], weight.data_ptr(), ws, _TYPES[weight.dtype], ids.numel(), cols,
-                                 int(vocab_start), vocab, float(scale), res.data_ptr(), dev.index, _stream(dev)))
+                                 int(vocab_start), vocab, float(scale), res.data_ptr(), dev.index, _stream(dev.index)))
     return res
 
 
@@ -263,12 +273,12 @@ def embedding_grad(ids, dy, vocab, scale=1.0, *, vocab_start=0, dtype=None, out=
     vocab = int(vocab)
     if vocab < 0:
         raise _bad("vocab must be >= 0")
-    res = _dense(out, "out", dev, (vocab, cols), dtype)
+    res = dy.new_empty((vocab, cols), dtype=dtype) if out is None else _dense(out, "out", dev, (vocab, cols), dtype)
     L = _ops()
     space = _space(workspace, L.echo_embedding_grad_workspace(rows, cols, vocab), dev)
     _check(L.echo_embedding_grad(
         t, _INDEX[ids.dtype], dy.data_ptr(), ds, _TYPES[dy.dtype], rows, cols, int(vocab_start), vocab, float(scale),
-        res.data_ptr(), _TYPES[dtype], int(bool(accumulate)), *_space_args(space), dev.index, _stream(dev)))
+        res.data_ptr(), _TYPES[dtype], int(bool(accumulate)), *_space_args(space), dev.index, _stream(dev.index)))
     return res
 
 
@@ -283,7 +293,7 @@ def _loss_args(logits, targets):
 def _grad_out(t, logits, dev, rows, cols):
     """(tensor, row stride) of a gradient of logits: new and dense, or the caller's, of any row stride."""
     if t is None:
-        return torch.empty(logits.shape, dtype=logits.dtype, device=dev), cols
+        return _like(logits), cols
     n, c, stride = _matrix(t, "grad", dev, (logits.dtype,))
     if t.shape != logits.shape:
         raise _bad(f"grad has shape {tuple(t.shape)}, needs {tuple(logits.shape)}")
@@ -313,7 +323,8 @@ def cross_entropy(logits, targets, *, vocab_start=0, vocab_size=None, grad_loss=
         names = ("lse", "target")
     res = _only(out, names + (("grad",) if grad_loss is not None else ()))
     for n in names:
-        res[n] = _dense(res.get(n), n, dev, shape, torch.float32)
+        res[n] = (_dense(res[n], n, dev, shape, torch.float32) if n in res
+                  else logits.new_empty(shape, dtype=torch.float32))
     g, gs, gl = None, 0, None
     if grad_loss is not None:
         gl = _vector(grad_loss, "grad_loss", dev, rows, (torch.float32,))
@@ -322,7 +333,7 @@ def cross_entropy(logits, targets, *, vocab_start=0, vocab_size=None, grad_loss=
     _check(_ops().echo_cross_entropy(
         logits.data_ptr(), ls, _TYPES[logits.dtype], t, _INDEX[targets.dtype], rows, cols, int(vocab_start),
         int(vocab_size), res["lse"].data_ptr(), res["target"].data_ptr() if "target" in res else None,
-        res["loss"].data_ptr() if "loss" in res else None, gl, g, gs, dev.index, _stream(dev)))
+        res["loss"].data_ptr() if "loss" in res else None, gl, g, gs, dev.index, _stream(dev.index)))
     return res
 
 
@@ -339,5 +350,5 @@ def cross_entropy_grad(logits, targets, lse, grad_loss, *, vocab_start=0, vocab_
     res, gs = _grad_out(out, logits, dev, rows, cols)
     _check(_ops().echo_cross_entropy_grad(
         logits.data_ptr(), ls, _TYPES[logits.dtype], t, _INDEX[targets.dtype], rows, cols, int(vocab_start),
-        int(vocab_size), e, gl, res.data_ptr(), gs, dev.index, _stream(dev)))
+        int(vocab_size), e, gl, res.data_ptr(), gs, dev.index, _stream(dev.index)))
     return res
