@@ -20,25 +20,29 @@ DEVICE_FLAGS = ["--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-I", INCLUDE, "-I", CSRC]
 
 
-def _run(cmd, verbose):
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+SOURCES = ("echo_kernels.hip", "echo_norm.hip", "echo_embed.hip", "echo_loss.hip", "echo_host.cpp", "echo_ops_host.cpp")
+
+
+def _run(cmds, verbose):
+    """Run the commands side by side; raise if one of them fails."""
+    running = []
+    for cmd in cmds:
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        running.append((cmd, subprocess.Popen(cmd)))
+    failed = [(cmd, p.returncode) for cmd, p in running if p.wait()]
+    if failed:
+        raise subprocess.CalledProcessError(failed[0][1], failed[0][0])
 
 
 def build(verbose: bool = False) -> str:
     """Compile every source and link libecho.so; always rebuilds."""
     os.makedirs(BUILD, exist_ok=True)
-    kobj = os.path.join(BUILD, "echo_kernels.o")
-    hobj = os.path.join(BUILD, "echo_host.o")
-    okobj = os.path.join(BUILD, "echo_ops.o")
-    ohobj = os.path.join(BUILD, "echo_ops_host.o")
-    _run(["hipcc", "-c", *DEVICE_FLAGS, *COMMON, os.path.join(CSRC, "echo_kernels.hip"), "-o", kobj], verbose)
-    _run(["hipcc", "-c", *COMMON, os.path.join(CSRC, "echo_host.cpp"), "-o", hobj], verbose)
-    _run(["hipcc", "-c", *DEVICE_FLAGS, *COMMON, os.path.join(CSRC, "echo_ops.hip"), "-o", okobj], verbose)
-    _run(["hipcc", "-c", *COMMON, os.path.join(CSRC, "echo_ops_host.cpp"), "-o", ohobj], verbose)
+    objects = {src: os.path.join(BUILD, os.path.splitext(src)[0] + ".o") for src in SOURCES}
+    _run([["hipcc", "-c", *(DEVICE_FLAGS if src.endswith(".hip") else []), *COMMON, os.path.join(CSRC, src), "-o", obj]
+          for src, obj in objects.items()], verbose)
     tmp = LIB + ".tmp"
-    _run(["hipcc", "-shared", "-fPIC", "--offload-arch=" + ARCH, kobj, hobj, okobj, ohobj, "-o", tmp], verbose)
+    _run([["hipcc", "-shared", "-fPIC", "--offload-arch=" + ARCH, *objects.values(), "-o", tmp]], verbose)
     os.replace(tmp, LIB)
     return LIB
 

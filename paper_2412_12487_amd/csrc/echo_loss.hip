@@ -1,0 +1,227 @@
+// echo_loss.hip -- cross entropy over a vocabulary or a shard of one, and its gradient, on gfx950.
+#include "echo_ops_device.h"
+
+namespace echo {
+namespace {
+
+// What a row's loss and gradient are computed with.
+struct LossRow {
+    bool trained;      // the target is an id of the vocabulary
+    int at;            // its column here, or -1
+};
+template <class I>
+__device__ __forceinline__ LossRow loss_row(const LossArgs &a, int64_t row) {
+    const int64_t t = id_at<I>(a.targets, row);
+    const bool trained = t >= 0 && t < a.vocab_size;
+    return LossRow{trained, trained ? shard_row(t, a.vocab_start, a.cols) : -1};
+}
+// exp(x), x <= 0 but for a row's rounding: one multiplication and the hardware's 2^x.  The product's rounding
+// makes the result |x| 2^-24 of itself wrong, as does that of x itself.
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+
+// (exp(l - lse) - [column = target]) * g for the columns col .. col + N - 1.
+template <int N>
+__device__ __forceinline__ F<N> loss_grad(F<N> l, float lse, int col, int at, float g) {
+    F<N> d;
+#pragma unroll
+    for (int j = 0; j < N; ++j) d[j] = (exp_of(l[j] - lse) - (col + j == at ? 1.0f : 0.0f)) * g;
+    return d;
+}
+// Log of the sum of exponentials from a maximum and a sum relative to it, written with the row's loss.
+__device__ __forceinline__ float finish_row(const LossArgs &a, int64_t row, const LossRow &r, float hit, float top, float sum,
+                                            bool writes) {
+    const float lse = top == -kInf ? -kInf : top + logf(sum);
+    if (writes) {
+        if (a.lse) a.lse[row] = lse;
+        if (a.target) a.target[row] = hit;
+        if (a.loss) a.loss[row] = !r.trained ? 0.0f : lse == -kInf ? kInf : lse - hit;
+    }
+    return lse;
+}
+
+// A team a row, which is read once and stays in registers as it came; with a gradient it is written
+// from there.  Each wavefront takes its maximum and its sum of exponentials relative to it; the team joins
+// them with one exchange.
+template <class T, class I, int THREADS, int E, bool CUT>
+__global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_loss(LossArgs a) {
+    using Q = Team<T, THREADS, E, CUT>;
+    constexpr int N = Q::N, P = Q::P;
+    const Q q(a.cols);
+    __shared__ float2 lds[2][Q::WAVES];
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * Q::TEAMS + q.team; row < a.rows; row += (int64_t)gridDim.x * Q::TEAMS) {
+        const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
+        V<T, N> x[P];
+        q.load(l, x, T(-kInf));
+        const LossRow r = loss_row<I>(a, row);
+        const float hit = r.at >= 0 ? (float)l[r.at] : 0.0f, g = a.grad ? a.grad_loss[row] : 0.0f;
+        float top = -kInf, sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const F<N> f = widen<T, N>(x[k]);
+#pragma unroll
+            for (int j = 0; j < N; ++j) top = fmaxf(top, f[j]);
+        }
+        forget<T, N, P>(x);
+        top = wave_max(top);
+        const float base = top == -kInf ? 0.0f : top;      // nothing here: the sum is 0
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const F<N> f = widen<T, N>(x[k]);
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum += exp_of(f[j] - base);
+        }
+        forget<T, N, P>(x);
+        sum = wave_sum(sum);
+        if constexpr (Q::WAVES > 1) {
+            if (q.lane % kWave == 0) lds[turn][q.wave] = make_float2(top, sum);
+            __syncthreads();      // also: every lane has read the target's logit, and grad may be logits
+#pragma unroll
+            for (int v = 0; v < Q::WAVES; ++v) top = fmaxf(top, lds[turn][v].x);
+            sum = 0.0f;
+#pragma unroll
+            for (int v = 0; v < Q::WAVES; ++v) {
+                const float2 p = lds[turn][v];
+                sum += p.x == -kInf ? p.y : p.y * exp_of(p.x - top);      // p.y is 0, or NaN
+            }
+            turn ^= 1;
+        }
+        // a row of NaN alone has no maximum but a sum
+        const float lse = finish_row(a, row, r, hit, sum != sum ? sum : top, sum, q.lane == 0);
+        if (!a.grad) continue;
+        const bool live = r.trained && lse != -kInf;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            F<N> f = 0.0f;
+            if (live) f = loss_grad<N>(widen<T, N>(x[k]), lse, q.col(k), r.at, g);
+            x[k] = round_to<T, N>(f);
+        }
+        q.drop(static_cast<T *>(a.grad) + row * a.grad_stride, x);
+    }
+}
+
+// Rows too wide for registers, or of less than a piece: one workgroup a row, read once for a running maximum and sum a lane, and
+// with a gradient once more.
+template <class T, class I>
+__global__ __launch_bounds__(kWideBlock) void k_loss_wide(LossArgs a) {
+    constexpr int N = kN<T>, STEP = kWideBlock * N;
+    __shared__ float2 lds[kWideWaves];
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
+        const LossRow r = loss_row<I>(a, row);
+        const float hit = r.at >= 0 ? (float)l[r.at] : 0.0f;
+        float top = -kInf, sum = 0.0f;
+#pragma unroll 4
+        for (int c = threadIdx.x * N; c < a.cols; c += STEP) {
+            const F<N> f = widen<T, N>(load<N>(l, c, a.cols, T(-kInf)));
+            float m = top;
+#pragma unroll
+            for (int j = 0; j < N; ++j) m = fmaxf(m, f[j]);
+            const float base = m == -kInf ? 0.0f : m;
+            sum *= top == -kInf ? 1.0f : exp_of(top - base);      // before a first finite logit the sum is 0, or NaN
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum += exp_of(f[j] - base);
+            top = m;
+        }
+        const float mine = top;
+        top = wave_max(top);
+        sum = wave_sum(mine == -kInf ? sum : sum * exp_of(mine - top));
+        __syncthreads();      // the last row's readers are done
+        if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = make_float2(top, sum);
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < kWideWaves; ++v) top = fmaxf(top, lds[v].x);
+        sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < kWideWaves; ++v) {
+            const float2 p = lds[v];
+            sum += p.x == -kInf ? p.y : p.y * exp_of(p.x - top);
+        }
+        const float lse = finish_row(a, row, r, hit, sum != sum ? sum : top, sum, threadIdx.x == 0);
+        if (!a.grad) continue;
+        T *d = static_cast<T *>(a.grad) + row * a.grad_stride;
+        const bool live = r.trained && lse != -kInf;
+        const float g = a.grad_loss[row];
+        for (int c = threadIdx.x * N; c < a.cols; c += STEP) {
+            F<N> f = 0.0f;
+            if (live) f = loss_grad<N>(widen<T, N>(load<N>(l, c, a.cols)), lse, c, r.at, g);
+            store<N>(d, c, a.cols, round_to<T, N>(f));
+        }
+    }
+}
+
+// The gradient alone, K pieces a lane of one row's stretch of 256 * K pieces.
+constexpr int kGradPieces = 2;
+template <class T, class I>
+__global__ __launch_bounds__(256) void k_loss_grad(LossArgs a) {
+    constexpr int N = kN<T>, K = kGradPieces, SPAN = K * 256 * N;
+    const int spans = (a.cols + SPAN - 1) / SPAN;
+    const int64_t n = a.rows * spans;
+    for (int64_t id = blockIdx.x; id < n; id += gridDim.x) {
+        const int64_t row = id / spans;
+        const int from = (int)(id - row * spans) * SPAN + threadIdx.x * N;
+        const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
+        T *d = static_cast<T *>(a.grad) + row * a.grad_stride;
+        V<T, N> raw[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            raw[k] = T(0);
+            if (from + k * 256 * N < a.cols) raw[k] = load<N>(l, from + k * 256 * N, a.cols);
+        }
+        const LossRow r = loss_row<I>(a, row);
+        const float lse = a.lse_in[row], g = a.grad_loss[row];
+        const bool live = r.trained && lse != -kInf;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = from + k * 256 * N;
+            if (c >= a.cols) continue;
+            F<N> f = 0.0f;
+            if (live) f = loss_grad<N>(widen<T, N>(raw[k]), lse, c, r.at, g);
+            drop<N>(d, c, a.cols, round_to<T, N>(f));
+        }
+    }
+}
+
+template <class T, class I, bool CUT>
+hipError_t loss(const LossArgs &a, hipStream_t s) {
+    const auto run = [&](auto kernel, int threads) {
+        const int teams = threads < 256 ? 256 / threads : 1;
+        return launch(kernel, dim3(grid_of((a.rows + teams - 1) / teams)), dim3(threads * teams), s, a);
+    };
+    if (a.cols < kN<T> || a.cols > 1024 * 64)
+        return launch(k_loss_wide<T, I>, dim3(grid_of(a.rows)), dim3(kWideBlock), s, a);
+    if (a.cols <= 64 * 8) return run(k_loss<T, I, 64, 8, CUT>, 64);
+    if (a.cols <= 64 * 32) return run(k_loss<T, I, 64, 32, CUT>, 64);
+    if (a.cols <= 256 * 32) return run(k_loss<T, I, 256, 32, CUT>, 256);
+    if (a.cols <= 512 * 32) return run(k_loss<T, I, 512, 32, CUT>, 512);
+    if (a.cols <= 1024 * 32) return run(k_loss<T, I, 1024, 32, CUT>, 1024);
+    return run(k_loss<T, I, 1024, 64, CUT>, 1024);
+}
+template <class T, class I>
+hipError_t loss_grad_alone(const LossArgs &a, hipStream_t s) {
+    constexpr int SPAN = kGradPieces * 256 * kN<T>;
+    return launch(k_loss_grad<T, I>, dim3(grid_of(a.rows * ((a.cols + SPAN - 1) / SPAN))), dim3(256), s, a);
+}
+
+}  // namespace
+
+template <class T, class I>
+static hipError_t loss_rows(const LossArgs &a, hipStream_t s) {
+    return a.cols % kN<T> ? loss<T, I, true>(a, s) : loss<T, I, false>(a, s);
+}
+template <class I>
+static hipError_t loss_of(const LossArgs &a, int type, bool grad_alone, hipStream_t s) {
+    switch (type) {
+        case ECHO_F32: return grad_alone ? loss_grad_alone<float, I>(a, s) : loss_rows<float, I>(a, s);
+        case ECHO_F16: return grad_alone ? loss_grad_alone<f16, I>(a, s) : loss_rows<f16, I>(a, s);
+        default: return grad_alone ? loss_grad_alone<bf16, I>(a, s) : loss_rows<bf16, I>(a, s);
+    }
+}
+hipError_t launch_loss(const LossArgs &a, int type, int index_type, hipStream_t s) {
+    return index_type == ECHO_I64 ? loss_of<int64_t>(a, type, false, s) : loss_of<int32_t>(a, type, false, s);
+}
+hipError_t launch_loss_grad(const LossArgs &a, int type, int index_type, hipStream_t s) {
+    return index_type == ECHO_I64 ? loss_of<int64_t>(a, type, true, s) : loss_of<int32_t>(a, type, true, s);
+}
+
+}  // namespace echo
