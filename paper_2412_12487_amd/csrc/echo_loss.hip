@@ -19,22 +19,24 @@ __device__ __forceinline__ LossRow loss_row(const LossArgs &a, int64_t row) {
 // makes the result |x| 2^-24 of itself wrong, as does that of x itself.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 
-// (exp(l - lse) - [column = target]) * g for the columns col .. col + N - 1.
+// (exp(l - base) * part - [column = target]) * g for the columns col .. col + N - 1.
 template <int N>
-__device__ __forceinline__ F<N> loss_grad(F<N> l, float lse, int col, int at, float g) {
+__device__ __forceinline__ F<N> loss_grad(F<N> l, float base, float part, int col, int at, float g) {
     F<N> d;
 #pragma unroll
-    for (int j = 0; j < N; ++j) d[j] = (exp_of(l[j] - lse) - (col + j == at ? 1.0f : 0.0f)) * g;
+    for (int j = 0; j < N; ++j) d[j] = (exp_of(l[j] - base) * part - (col + j == at ? 1.0f : 0.0f)) * g;
     return d;
 }
-// Log of the sum of exponentials from a maximum and a sum relative to it, written with the row's loss.
+// Log of the sum of exponentials from a maximum and a sum relative to it, written with the row's loss.  The loss
+// and a gradient in the same pass are taken from the maximum and the sum, not from their rounded total: in a row of
+// large logits (one masked throughout with the type's lowest value, say) the logarithm is below the maximum's last place.
 __device__ __forceinline__ float finish_row(const LossArgs &a, int64_t row, const LossRow &r, float hit, float top, float sum,
                                             bool writes) {
-    const float lse = top == -kInf ? -kInf : top + logf(sum);
+    const float more = logf(sum), lse = top == -kInf ? -kInf : top + more;
     if (writes) {
         if (a.lse) a.lse[row] = lse;
         if (a.target) a.target[row] = hit;
-        if (a.loss) a.loss[row] = !r.trained ? 0.0f : lse == -kInf ? kInf : lse - hit;
+        if (a.loss) a.loss[row] = !r.trained ? 0.0f : lse == -kInf ? kInf : (top - hit) + more;
     }
     return lse;
 }
@@ -87,13 +89,14 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_loss(Loss
             turn ^= 1;
         }
         // a row of NaN alone has no maximum but a sum
-        const float lse = finish_row(a, row, r, hit, sum != sum ? sum : top, sum, q.lane == 0);
+        if (sum != sum) top = sum;
+        const float lse = finish_row(a, row, r, hit, top, sum, q.lane == 0), part = 1.0f / sum;
         if (!a.grad) continue;
         const bool live = r.trained && lse != -kInf;
 #pragma unroll
         for (int k = 0; k < P; ++k) {
             F<N> f = 0.0f;
-            if (live) f = loss_grad<N>(widen<T, N>(x[k]), lse, q.col(k), r.at, g);
+            if (live) f = loss_grad<N>(widen<T, N>(x[k]), top, part, q.col(k), r.at, g);
             x[k] = round_to<T, N>(f);
         }
         q.drop(static_cast<T *>(a.grad) + row * a.grad_stride, x);
@@ -137,14 +140,15 @@ __global__ __launch_bounds__(kWideBlock) void k_loss_wide(LossArgs a) {
             const float2 p = lds[v];
             sum += p.x == -kInf ? p.y : p.y * exp_of(p.x - top);
         }
-        const float lse = finish_row(a, row, r, hit, sum != sum ? sum : top, sum, threadIdx.x == 0);
+        if (sum != sum) top = sum;
+        const float lse = finish_row(a, row, r, hit, top, sum, threadIdx.x == 0), part = 1.0f / sum;
         if (!a.grad) continue;
         T *d = static_cast<T *>(a.grad) + row * a.grad_stride;
         const bool live = r.trained && lse != -kInf;
         const float g = a.grad_loss[row];
         for (int c = threadIdx.x * N; c < a.cols; c += STEP) {
             F<N> f = 0.0f;
-            if (live) f = loss_grad<N>(widen<T, N>(load<N>(l, c, a.cols)), lse, c, r.at, g);
+            if (live) f = loss_grad<N>(widen<T, N>(load<N>(l, c, a.cols)), top, part, c, r.at, g);
             store<N>(d, c, a.cols, round_to<T, N>(f));
         }
     }
@@ -176,7 +180,7 @@ __global__ __launch_bounds__(256) void k_loss_grad(LossArgs a) {
             const int c = from + k * 256 * N;
             if (c >= a.cols) continue;
             F<N> f = 0.0f;
-            if (live) f = loss_grad<N>(widen<T, N>(raw[k]), lse, c, r.at, g);
+            if (live) f = loss_grad<N>(widen<T, N>(raw[k]), lse, 1.0f, c, r.at, g);
             drop<N>(d, c, a.cols, round_to<T, N>(f));
         }
     }

@@ -485,6 +485,23 @@ def test_cross_entropy_bad_rows_stay_by_themselves(cols):
     assert math.isnan(out["loss"][4]) and torch.isnan(out["grad"][4].float()).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [70, 1024, 51200, 70001])
+def test_cross_entropy_of_rows_masked_with_the_lowest_value(cols, dtype):
+    """Every logit the same, however large: loss log(cols) and even probabilities, although the row's lse itself
+    rounds the logarithm away.  A sum of cols equal terms 1 is off by a chain's roundings at most."""
+    g = torch.tensor([1.0, 0.5, -2.0], device="cuda")
+    l = torch.tensor([torch.finfo(dtype).min, -30000.0, 30000.0], device="cuda").to(dtype)[:, None].repeat(1, cols)
+    t = torch.tensor([3, 0, cols - 1], device="cuda")
+    out = E.cross_entropy(l, t, grad_loss=g)
+    err = R.U * (R.chain(cols) + 32)
+    want = torch.full((3,), math.log(cols), dtype=torch.float64, device="cuda")
+    R.close(out["loss"], want, err + 2 * R.U * want, "loss")
+    p = torch.full((3, cols), 1.0 / cols, dtype=torch.float64, device="cuda")
+    hot = torch.nn.functional.one_hot(t, cols).double()
+    R.close(out["grad"], (p - hot) * g.double()[:, None], (err * p + 4 * R.U * (p + hot)) * g.double().abs()[:, None], "grad")
+
+
 def test_cross_entropy_shapes_and_targets_outside():
     l, t, gl = _loss_case(24, 300, F16, 1)
     t[5], t[6], t[7] = 300, 2 ** 62, -2 ** 63
