@@ -81,7 +81,8 @@ int echo_embedding(const void *ids, int32_t index_type, const void *weight, int6
  *   dweight[v] = scale * sum of dy[t] over the t with ids[t] = vocab_start + v
  * for every row of the shard (zeros where no token has the id), or with accumulate != 0 added to
  * dweight, whose other rows are then left alone.  dy is of `type`, dweight [vocab][cols] of grad_type
- * (`type` or ECHO_F32); vocab <= 2^26 (else ECHO_ERR_RANGE).  Tokens are sorted by id first; a row's tokens are summed in ascending order.
+ * (`type` or ECHO_F32); vocab <= 2^26 and rows <= 2^29 (else ECHO_ERR_RANGE).  Tokens are sorted by id first;
+ * a row's tokens are summed in chunks of ascending order, and the chunks joined in an order that the sizes fix.
  * workspace: at least echo_embedding_grad_workspace(rows, cols, vocab) bytes, aligned to 16.
  */
 int64_t echo_embedding_grad_workspace(int64_t rows, int64_t cols, int64_t vocab);
@@ -96,7 +97,7 @@ int echo_embedding_grad(const void *ids, int32_t index_type, const void *dy, int
  * not trained on.  Per row (any of lse, target, loss may be NULL; 32 bits):
  *   lse     log of the sum of exp(logits): -inf where every logit is -inf
  *   target  the target's logit; 0 where it is not held here or the row is not trained on
- *   loss    lse - target; 0 for a row not trained on, +inf where the target's logit is -inf,
+ *   loss    lse - target, before lse is rounded; 0 for a row not trained on, +inf where the target's logit is -inf,
  *           NaN where the row has a NaN or +inf (whole vocabulary only)
  *   grad    (exp(logit - lse) - [v = target]) * grad_loss[row], [rows][cols] of `type` (whole vocabulary
  *           only): the gradient, in the same pass, for a grad_loss [rows] known beforehand.  Rows not

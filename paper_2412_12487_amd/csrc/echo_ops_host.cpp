@@ -19,6 +19,9 @@ constexpr int64_t kMaxRows = INT32_MAX;
 constexpr int64_t kMaxCols = int64_t(1) << 24;
 constexpr int64_t kMaxElements = int64_t(1) << 38; // grids stay below 2^32 work-items
 constexpr int64_t kMaxSorted = int64_t(1) << 26;   // rows of a table whose gradient's tokens are sorted
+// Tokens of a table's gradient: a wavefront sums at least 32 of them over at least 256 columns, so at most 1.5 * 2^25
+// wavefronts (of rows * cols <= 2^38) and those that write zeros stay below 2^32 work-items.
+constexpr int64_t kMaxTokens = int64_t(1) << 29;
 constexpr int64_t kMaxStride = int64_t(1) << 28;   // 2^31 rows of 4-byte elements stay below 2^62 bytes
 
 int64_t elem(int32_t type) { return type == ECHO_F32 ? 4 : 2; }
@@ -237,6 +240,7 @@ int echo_embedding_grad(const void *ids, int32_t index_type, const void *dy, int
     ECHO_TRY(check_matrix("dy", dy, rows, dy_stride, e));
     ECHO_TRY(check_matrix("dweight", dweight, vocab, cols, ge));
     if (vocab > kMaxSorted) return set_error(ECHO_ERR_RANGE, "vocab = %lld passes 2^26", (long long)vocab);
+    if (rows > kMaxTokens) return set_error(ECHO_ERR_RANGE, "rows = %lld pass 2^29", (long long)rows);
     const int64_t need = echo_embedding_grad_workspace(rows, cols, vocab);
     ECHO_TRY(check_workspace(workspace, workspace_bytes, need));
     ECHO_TRY(check_spans({{"dweight", dweight, vocab * cols * ge, 0}, {"workspace", workspace, need, 0}},

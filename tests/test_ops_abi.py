@@ -151,3 +151,8 @@ def test_workspace_sizes(L):
     assert 0 < norm((1 << 31) - 1, 1 << 24) < 1 << 50
     assert 0 < embed((1 << 31) - 1, 1 << 24, 1 << 26) < 1 << 56 and embed(8, 8, (1 << 26) + 1) == 0
     assert ctypes.sizeof(ctypes.c_int64) == 8
+
+
+def test_more_tokens_than_a_sort_takes_are_out_of_range(E, L):
+    assert _embed_grad(L, rows=(1 << 29) + 1, cols=1) == E.ECHO_ERR_RANGE
+    assert "2^29" in L.echo_last_error().decode()
