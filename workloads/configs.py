@@ -68,8 +68,8 @@ def graph_params(config: int, index: int = 0) -> dict:
     raise ValueError(f"unknown config {config}")
 
 
-def graph(config: int, index: int = 0) -> dict:
-    return gpt1f1b.gpt_graph(**graph_params(config, index))
+def graph(config: int, index: int = 0, operator_ns: dict | None = None) -> dict:
+    return gpt1f1b.gpt_graph(**graph_params(config, index), operator_ns=operator_ns)
 
 
 def scenario_batch(config: int, index: int = 0, n: int | None = None) -> dict:

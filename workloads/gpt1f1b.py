@@ -54,6 +54,11 @@ LOG_SIGMA = 0.5
 _G_TP, _G_DP, _G_P2P = 0, 1, 2
 _DUR_COMPUTE, _DUR_MEMCPY, _DUR_NONE = 0, 1, 2
 
+# Compute ops whose durations `operator_ns` of gpt_graph may give: the operators of a stage outside its
+# matrix products that workloads.measured times.
+OPERATORS = ("embed", "norm", "loss", "loss_grad", "norm_grad", "embed_grad")
+_NO_OPERATOR = len(OPERATORS)
+
 # One transformer layer, forward: (class, all-reduce after this op?)
 _FWD_LAYER = [
     (CLS_LAYERNORM, 0), (CLS_GEMM, 0), (CLS_SUM, 0), (CLS_TRANSFORM, 0),
@@ -85,7 +90,7 @@ class _Stage:
     """Program (issue order) of one pipeline stage, shared by its TP x DP ranks."""
 
     def __init__(self):
-        self.kind, self.stream, self.cls, self.durk = [], [], [], []
+        self.kind, self.stream, self.cls, self.durk, self.operator = [], [], [], [], []
         self.preds, self.gkind, self.gj = [], [], []
         self.last_compute = -1
         self.wait_for = []            # ops the next compute op must depend on
@@ -96,15 +101,18 @@ class _Stage:
         self.stream.append(stream)
         self.cls.append(cls)
         self.durk.append(durk)
+        self.operator.append(_NO_OPERATOR)
         self.preds.append(preds)
         self.gkind.append(gkind)
         self.gj.append(gj)
         return len(self.kind) - 1
 
-    def compute(self, cls, extra=()):
+    def compute(self, cls, extra=(), operator=None):
         preds = self.wait_for + list(extra)
         self.wait_for = []
         i = self._add(KIND_COMPUTE, S_COMPUTE, cls, _DUR_COMPUTE, preds)
+        if operator:
+            self.operator[i] = OPERATORS.index(operator)
         self.last_compute = i
         return i
 
@@ -198,7 +206,7 @@ def _build_stage(p, P, tp, dp, m, n_layers, h, seq, distopt):
         labels = -1
         if first:
             st.memcpy(blocking=True)                      # token ids to the device
-            st.compute(CLS_OTHER)                         # embedding lookup
+            st.compute(CLS_OTHER, operator="embed")       # embedding lookup
             if use_tp:
                 st.tp(COLL_AR, act)                       # vocab-parallel embedding reduce
             st.compute(CLS_OTHER)                         # embedding dropout
@@ -206,15 +214,15 @@ def _build_stage(p, P, tp, dp, m, n_layers, h, seq, distopt):
             labels = st.memcpy(blocking=False)            # labels to the device
         for _ in range(ls):
             for cls, ar in _FWD_LAYER:
-                st.compute(cls)
+                st.compute(cls, operator="norm" if cls == CLS_LAYERNORM else None)
                 if ar and use_tp:
                     st.tp(COLL_AR, act)
         if last:
-            st.compute(CLS_LAYERNORM)                     # final layernorm
+            st.compute(CLS_LAYERNORM, operator="norm")    # final layernorm
             st.compute(CLS_GEMM)                          # vocab-parallel logits
             if use_tp:
                 st.tp(COLL_AR, small)                     # logit max
-            st.compute(CLS_OTHER)                         # exp / partial sums
+            st.compute(CLS_OTHER, operator="loss")        # exp / partial sums
             if use_tp:
                 st.tp(COLL_AR, small)                     # sum of exp
             st.compute(CLS_SUM, extra=[labels])           # loss
@@ -223,23 +231,23 @@ def _build_stage(p, P, tp, dp, m, n_layers, h, seq, distopt):
         last_mb = mb == m - 1
         if last:
             st.compute(CLS_GRAD)
-            st.compute(CLS_GRAD)
+            st.compute(CLS_GRAD, operator="loss_grad")
             st.compute(CLS_GEMM)                          # logits dgrad
             if use_tp:
                 st.tp(COLL_AR, act)
             st.compute(CLS_GEMM)                          # logits wgrad
-            st.compute(CLS_LAYERNORM)                     # final layernorm backward
+            st.compute(CLS_LAYERNORM, operator="norm_grad")  # final layernorm backward
             if last_mb:
                 grads_ready("head")
         for layer in reversed(range(ls)):
             for cls, ar in _BWD_LAYER:
-                st.compute(cls)
+                st.compute(cls, operator="norm_grad" if cls == CLS_LAYERNORM else None)
                 if ar and use_tp:
                     st.tp(COLL_AR, act)
             if last_mb:
                 grads_ready(layer)
         if first:
-            st.compute(CLS_GRAD)                          # embedding gradient
+            st.compute(CLS_GRAD, operator="embed_grad")   # embedding gradient
             if last_mb:
                 grads_ready("embed")
         if last_mb and bucket["cum"] > bucket["issued"] * BUCKET_BYTES:
@@ -284,12 +292,15 @@ def _build_stage(p, P, tp, dp, m, n_layers, h, seq, distopt):
 
 
 def gpt_graph(*, n_layers, hidden, seq, tp, pp, dp, microbatches, seed,
-              distopt=False, gpus_per_node=8, replica_invariant=False):
+              distopt=False, gpus_per_node=8, replica_invariant=False, operator_ns=None):
     """Build the execution graphs of all TP*PP*DP ranks of one training step.
 
     replica_invariant: every data-parallel replica gets the same durations (one
     draw per pipeline stage, tensor-parallel rank and op), as when a single
-    replica is traced and copied."""
+    replica is traced and copied.
+
+    operator_ns: durations in ns of some of OPERATORS, in place of the drawn ones; all
+    other ops keep the durations that they have without it."""
     if n_layers % pp:
         raise ValueError("n_layers must be divisible by pp")
     P, T, D, m = pp, tp, dp, microbatches
@@ -323,7 +334,7 @@ def gpt_graph(*, n_layers, hidden, seq, tp, pp, dp, microbatches, seed,
     coll_bytes[p2p_base:] = seq * hidden * BYTES_PER_ELEM
 
     # Instantiate every stage template for its T*D ranks (rank-major op ids).
-    parts = {k: [] for k in ("rank", "stream", "kind", "cls", "durk", "coll", "pcount", "pidx")}
+    parts = {k: [] for k in ("rank", "stream", "kind", "cls", "durk", "operator", "coll", "pcount", "pidx")}
     base = 0
     q = np.arange(T * D, dtype=np.int64)
     tpi, dpi = q % T, q // T
@@ -332,7 +343,8 @@ def gpt_graph(*, n_layers, hidden, seq, tp, pp, dp, microbatches, seed,
         ranks = q + T * D * p
         bases = base + q * n
         parts["rank"].append(np.repeat(ranks.astype(np.int32), n))
-        for key, src in (("stream", s.stream), ("kind", s.kind), ("cls", s.cls), ("durk", s.durk)):
+        for key, src in (("stream", s.stream), ("kind", s.kind), ("cls", s.cls), ("durk", s.durk),
+                         ("operator", s.operator)):
             parts[key].append(np.tile(np.asarray(src, np.uint8), T * D))
         gk = np.asarray(s.gkind, np.int64)
         gj = np.asarray(s.gj, np.int64)
@@ -359,6 +371,13 @@ def gpt_graph(*, n_layers, hidden, seq, tp, pp, dp, microbatches, seed,
     med = np.where(durk == _DUR_MEMCPY, MEMCPY_MEDIAN_NS, COMPUTE_MEDIAN_NS)
     dur = np.maximum(np.rint(med * np.exp(LOG_SIGMA * z)), 1.0).astype(np.int64)
     dur[durk == _DUR_NONE] = 0
+    if operator_ns:
+        unknown = set(operator_ns) - set(OPERATORS)
+        if unknown:
+            raise ValueError(f"unknown operators {sorted(unknown)}")
+        operator = np.concatenate(parts["operator"])
+        for name, ns in operator_ns.items():
+            dur[operator == OPERATORS.index(name)] = max(int(ns), 1)
     pcount = np.concatenate(parts["pcount"])
     pred_off = np.zeros(n_ops + 1, np.int64)
     np.cumsum(pcount, out=pred_off[1:])
