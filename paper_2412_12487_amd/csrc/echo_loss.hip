@@ -19,12 +19,17 @@ __device__ __forceinline__ LossRow loss_row(const LossArgs &a, int64_t row) {
 // makes the result |x| 2^-24 of itself wrong, as does that of x itself.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 
-// (exp(l - base) * part - [column = target]) * g for the columns col .. col + N - 1.
+// exp(l - base) * scale - [column = target] * g for the columns col .. col + N - 1.  The target is looked for once a piece:
+// with a comparison an element 2048 x 51200 took 107.2 us instead of 103.6.
 template <int N>
-__device__ __forceinline__ F<N> loss_grad(F<N> l, float base, float part, int col, int at, float g) {
+__device__ __forceinline__ F<N> loss_grad(F<N> l, float base, float scale, int col, int at, float g) {
     F<N> d;
 #pragma unroll
-    for (int j = 0; j < N; ++j) d[j] = (exp_of(l[j] - base) * part - (col + j == at ? 1.0f : 0.0f)) * g;
+    for (int j = 0; j < N; ++j) d[j] = exp_of(l[j] - base) * scale;
+    if ((unsigned)(at - col) < (unsigned)N) {      // at is -1 or a column
+#pragma unroll
+        for (int j = 0; j < N; ++j) d[j] -= col + j == at ? g : 0.0f;
+    }
     return d;
 }
 // Log of the sum of exponentials from a maximum and a sum relative to it, written with the row's loss.  The loss
@@ -90,13 +95,13 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_loss(Loss
         }
         // a row of NaN alone has no maximum but a sum
         if (sum != sum) top = sum;
-        const float lse = finish_row(a, row, r, hit, top, sum, q.lane == 0), part = 1.0f / sum;
+        const float lse = finish_row(a, row, r, hit, top, sum, q.lane == 0), scale = g / sum;
         if (!a.grad) continue;
         const bool live = r.trained && lse != -kInf;
 #pragma unroll
         for (int k = 0; k < P; ++k) {
             F<N> f = 0.0f;
-            if (live) f = loss_grad<N>(widen<T, N>(x[k]), top, part, q.col(k), r.at, g);
+            if (live) f = loss_grad<N>(widen<T, N>(x[k]), top, scale, q.col(k), r.at, g);
             x[k] = round_to<T, N>(f);
         }
         q.drop(static_cast<T *>(a.grad) + row * a.grad_stride, x);
@@ -141,14 +146,14 @@ __global__ __launch_bounds__(kWideBlock) void k_loss_wide(LossArgs a) {
             sum += p.x == -kInf ? p.y : p.y * exp_of(p.x - top);
         }
         if (sum != sum) top = sum;
-        const float lse = finish_row(a, row, r, hit, top, sum, threadIdx.x == 0), part = 1.0f / sum;
+        const float lse = finish_row(a, row, r, hit, top, sum, threadIdx.x == 0);
         if (!a.grad) continue;
         T *d = static_cast<T *>(a.grad) + row * a.grad_stride;
         const bool live = r.trained && lse != -kInf;
-        const float g = a.grad_loss[row];
+        const float g = a.grad_loss[row], scale = g / sum;
         for (int c = threadIdx.x * N; c < a.cols; c += STEP) {
             F<N> f = 0.0f;
-            if (live) f = loss_grad<N>(widen<T, N>(load<N>(l, c, a.cols)), top, part, c, r.at, g);
+            if (live) f = loss_grad<N>(widen<T, N>(load<N>(l, c, a.cols)), top, scale, c, r.at, g);
             store<N>(d, c, a.cols, round_to<T, N>(f));
         }
     }
@@ -180,7 +185,7 @@ __global__ __launch_bounds__(256) void k_loss_grad(LossArgs a) {
             const int c = from + k * 256 * N;
             if (c >= a.cols) continue;
             F<N> f = 0.0f;
-            if (live) f = loss_grad<N>(widen<T, N>(raw[k]), lse, 1.0f, c, r.at, g);
+            if (live) f = loss_grad<N>(widen<T, N>(raw[k]), lse, g, c, r.at, g);
             drop<N>(d, c, a.cols, round_to<T, N>(f));
         }
     }
