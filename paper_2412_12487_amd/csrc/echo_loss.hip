@@ -49,8 +49,14 @@ __device__ __forceinline__ float finish_row(const LossArgs &a, int64_t row, cons
 // A team a row, which is read once and stays in registers as it came; with a gradient it is written
 // from there.  Each wavefront takes its maximum and its sum of exponentials relative to it; the team joins
 // them with one exchange.
+// Wavefronts a SIMD that a variant's registers have to leave room for: two workgroups of 16 wavefronts on a compute unit, one
+// reading while the other computes or writes, where the row takes at most half of the 64 registers that each lane then
+// has.  2048 x 51200 of bf16 took 103.6 us with 95 to 128 registers and one workgroup, and takes 77.9.  The
+// compiler stays within 64 because each piece's sums are closed before the next piece is converted (the empty asm in the loops).
+template <class T, int THREADS, int E>
+constexpr int kLossWaves = THREADS == 1024 && E * sizeof(T) <= 128 ? 8 : 1;
 template <class T, class I, int THREADS, int E, bool CUT>
-__global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_loss(LossArgs a) {
+__global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK), (kLossWaves<T, THREADS, E>)) void k_loss(LossArgs a) {
     using Q = Team<T, THREADS, E, CUT>;
     constexpr int N = Q::N, P = Q::P;
     const Q q(a.cols);
@@ -68,6 +74,7 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_loss(Loss
             const F<N> f = widen<T, N>(x[k]);
 #pragma unroll
             for (int j = 0; j < N; ++j) top = fmaxf(top, f[j]);
+            if constexpr (kLossWaves<T, THREADS, E> > 1) asm volatile("" : "+v"(top));
         }
         forget<T, N, P>(x);
         top = wave_max(top);
@@ -77,20 +84,16 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_loss(Loss
             const F<N> f = widen<T, N>(x[k]);
 #pragma unroll
             for (int j = 0; j < N; ++j) sum += exp_of(f[j] - base);
+            if constexpr (kLossWaves<T, THREADS, E> > 1) asm volatile("" : "+v"(sum));
         }
         forget<T, N, P>(x);
         sum = wave_sum(sum);
         if constexpr (Q::WAVES > 1) {
             if (q.lane % kWave == 0) lds[turn][q.wave] = make_float2(top, sum);
             __syncthreads();      // also: every lane has read the target's logit, and grad may be logits
-#pragma unroll
-            for (int v = 0; v < Q::WAVES; ++v) top = fmaxf(top, lds[turn][v].x);
-            sum = 0.0f;
-#pragma unroll
-            for (int v = 0; v < Q::WAVES; ++v) {
-                const float2 p = lds[turn][v];
-                sum += p.x == -kInf ? p.y : p.y * exp_of(p.x - top);      // p.y is 0, or NaN
-            }
+            const float2 p = lds[turn][q.lane % Q::WAVES];      // a wavefront's in a lane
+            top = ring_max<Q::WAVES>(p.x);
+            sum = ring_sum<Q::WAVES>(p.x == -kInf ? p.y : p.y * exp_of(p.x - top));      // p.y is 0 there, or NaN
             turn ^= 1;
         }
         // a row of NaN alone has no maximum but a sum
@@ -103,6 +106,7 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_loss(Loss
             F<N> f = 0.0f;
             if (live) f = loss_grad<N>(widen<T, N>(x[k]), top, scale, q.col(k), r.at, g);
             x[k] = round_to<T, N>(f);
+            if constexpr (kLossWaves<T, THREADS, E> > 1) forget<T, N, 1>(reinterpret_cast<V<T, N>(&)[1]>(x[k]));
         }
         q.drop(static_cast<T *>(a.grad) + row * a.grad_stride, x);
     }
@@ -204,6 +208,11 @@ hipError_t loss(const LossArgs &a, hipStream_t s) {
     if (a.cols <= 256 * 32) return run(k_loss<T, I, 256, 32, CUT>, 256);
     if (a.cols <= 512 * 32) return run(k_loss<T, I, 512, 32, CUT>, 512);
     if (a.cols <= 1024 * 32) return run(k_loss<T, I, 1024, 32, CUT>, 1024);
+    // A lane computes on every piece that the variant has, also past the row's end: 2048 rows of 33000 columns of bf16 take
+    // 64.0 us with 64 elements a lane and 46.0 with 40, 48000 columns 65.3 us with 64 and 61.2 with 48; 56 elements
+    // gained nothing over 64 (51200 columns: 65.1 us with either).
+    if (a.cols <= 1024 * 40) return run(k_loss<T, I, 1024, 40, CUT>, 1024);
+    if (a.cols <= 1024 * 48) return run(k_loss<T, I, 1024, 48, CUT>, 1024);
     return run(k_loss<T, I, 1024, 64, CUT>, 1024);
 }
 template <class T, class I>

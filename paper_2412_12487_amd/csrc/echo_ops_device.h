@@ -85,6 +85,17 @@ __device__ __forceinline__ float rotated(float v) {
 __device__ __forceinline__ float lane_of(float v, int lane) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
+// Sum and maximum over every N lanes side by side that hold N values in turn (N a power of two, at most 16).
+template <int N>
+__device__ __forceinline__ float ring_sum(float v) {
+    if constexpr (N > 1) return ring_sum<N / 2>(v + rotated<N / 2>(v));
+    return v;
+}
+template <int N>
+__device__ __forceinline__ float ring_max(float v) {
+    if constexpr (N > 1) return ring_max<N / 2>(fmaxf(v, rotated<N / 2>(v)));
+    return v;
+}
 __device__ __forceinline__ float wave_sum(float v) {
     v += rotated<8>(v);
     v += rotated<4>(v);
