@@ -210,12 +210,11 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_norm_grad
         if constexpr (Q::WAVES > 1) {
             if (q.lane % kWave == 0) lds[turn][q.wave] = make_float2(s1, s2);
             __syncthreads();
-            s1 = s2 = 0.0f;
-#pragma unroll
-            for (int v = 0; v < Q::WAVES; ++v) {
-                s1 += lds[turn][v].x;
-                s2 += lds[turn][v].y;
-            }
+            constexpr int R = Q::WAVES <= 8 ? Q::WAVES : 16;
+            const int v = q.lane % R;      // a wavefront's sums in a lane
+            const float2 p = v < Q::WAVES ? lds[turn][v] : make_float2(0.0f, 0.0f);
+            s1 = ring_sum<R>(p.x);
+            s2 = ring_sum<R>(p.y);
             turn ^= 1;
         }
         s1 /= (float)a.cols;
@@ -352,26 +351,27 @@ constexpr int64_t kGradCols = 512 * 32, kCutGradCols = 512 * 24;
 
 template <class T, class W, bool CUT>
 hipError_t norm_grad_rows(const NormGradArgs &a, hipStream_t s) {
+    const int whole = a.cols - a.cols % kN<T>;      // what is left of a cut row has a place of its own
     const auto run = [&](auto kernel, int threads) {
         return launch(kernel, dim3((unsigned)a.parts), dim3(threads < 256 ? 256 : threads), s, a);
     };
-    if (a.cols < kN<T> || a.cols > (CUT ? kCutGradCols : kGradCols)) {
+    if (!whole || whole > (CUT ? kCutGradCols : kGradCols)) {
         const unsigned tiles = (unsigned)((a.cols + kWave * kN<T> - 1) / (kWave * kN<T>));
         const hipError_t e = launch(k_norm_dw_wide<T>, dim3(tiles, (unsigned)a.parts), dim3(64), s, a);
         // dx comes second: it may lie where dy is
         return e ? e : launch(k_norm_dx_wide<T, W>, dim3(grid_of(a.rows)), dim3(kWideBlock), s, a);
     }
-    if (a.cols <= 64 * 8) return run(k_norm_grad<T, W, 64, 8, CUT>, 64);
-    if (a.cols <= 64 * 16) return run(k_norm_grad<T, W, 64, 16, CUT>, 64);
-    if (a.cols <= 256 * 8) return run(k_norm_grad<T, W, 256, 8, CUT>, 256);
-    if (a.cols <= 512 * 8) return run(k_norm_grad<T, W, 512, 8, CUT>, 512);
-    if (a.cols <= 768 * 8) return run(k_norm_grad<T, W, 768, 8, CUT>, 768);
+    if (whole <= 64 * 8) return run(k_norm_grad<T, W, 64, 8, CUT>, 64);
+    if (whole <= 64 * 16) return run(k_norm_grad<T, W, 64, 16, CUT>, 64);
+    if (whole <= 256 * 8) return run(k_norm_grad<T, W, 256, 8, CUT>, 256);
+    if (whole <= 512 * 8) return run(k_norm_grad<T, W, 512, 8, CUT>, 512);
+    if (whole <= 768 * 8) return run(k_norm_grad<T, W, 768, 8, CUT>, 768);
     if constexpr (CUT) {      // the rest of a cut row takes 50 registers, which larger workgroups do not have
-        if (a.cols <= 512 * 16) return run(k_norm_grad<T, W, 512, 16, CUT>, 512);
+        if (whole <= 512 * 16) return run(k_norm_grad<T, W, 512, 16, CUT>, 512);
         return run(k_norm_grad<T, W, 512, 24, CUT>, 512);
     } else {
-        if (a.cols <= 1024 * 8) return run(k_norm_grad<T, W, 1024, 8, CUT>, 1024);
-        if (a.cols <= 768 * 16) return run(k_norm_grad<T, W, 768, 16, CUT>, 768);
+        if (whole <= 1024 * 8) return run(k_norm_grad<T, W, 1024, 8, CUT>, 1024);
+        if (whole <= 768 * 16) return run(k_norm_grad<T, W, 768, 16, CUT>, 768);
         return run(k_norm_grad<T, W, 512, 32, CUT>, 512);
     }
 }
