@@ -164,7 +164,7 @@ hipError_t norm(const NormArgs &a, hipStream_t s) {
 template <class T, class W, int THREADS, int E, bool CUT>
 __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_norm_grad(NormGradArgs a) {
     using Q = Team<T, THREADS, E, CUT>;
-    constexpr int N = Q::N, P = Q::P;
+    constexpr int N = Q::N, K = Q::K, P = Q::P;
     constexpr int kRows = E <= 8 ? 2 : 1;      // in registers
     struct Row {
         V<T, N> x[P], dy[P], past[P];
@@ -193,9 +193,14 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_norm_grad
         if (a.grad_residual) q.settle(r.past, T(0));
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-            // past the row's end dy and weight are 0, and so are g and its products, unless the row has
-            // no finite statistics: then all of it has none
-            const F<N> d = widen<T, N>(r.dy[k]), n = (widen<T, N>(r.x[k]) - r.mean) * r.rstd, g = d * widen<W, N>(wv[k]);
+            // past the row's end dy and weight are 0, and so is g.  n is made 0 there too: the product of a finite mean
+            // and a finite rstd can pass 32 bits, and infinity times 0 would be the whole row's
+            F<N> n = (widen<T, N>(r.x[k]) - (q.has(k) ? r.mean : 0.0f)) * r.rstd;
+            if (k == K) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) n[j] = j < q.left ? n[j] : 0.0f;
+            }
+            const F<N> d = widen<T, N>(r.dy[k]), g = d * widen<W, N>(wv[k]);
             dw[k] += d * n;
             db[k] += d;
 #pragma unroll
