@@ -85,13 +85,17 @@ int check_index(int32_t index_type) {
         return set_error(ECHO_ERR_ARG, "unknown index type %d", index_type);
     return ECHO_OK;
 }
-int check_shard(int64_t start, int64_t n, int64_t whole) {
+int check_shard(int64_t start, int64_t n) {
     if (start < 0 || n < 0 || n > kMaxRows || start > INT64_MAX - n)
         return set_error(ECHO_ERR_ARG, "vocabulary shard [%lld, +%lld) out of range", (long long)start, (long long)n);
-    if (whole >= 0 && start + n > whole)
+    return ECHO_OK;
+}
+int check_shard_of(int64_t start, int64_t n, int64_t whole) {
+    const int rc = check_shard(start, n);
+    if (rc == ECHO_OK && start + n > whole)
         return set_error(ECHO_ERR_ARG, "vocabulary shard [%lld, +%lld) passes the vocabulary of %lld",
                          (long long)start, (long long)n, (long long)whole);
-    return ECHO_OK;
+    return rc;
 }
 int check_workspace(const void *p, int64_t bytes, int64_t need) {
     if (need && (!p || bytes < need))
@@ -207,7 +211,7 @@ int echo_embedding(const void *ids, int32_t index_type, const void *weight, int6
     ECHO_TRY(check_types(type, type, "type"));
     ECHO_TRY(check_index(index_type));
     ECHO_TRY(check_sizes(rows, cols));
-    ECHO_TRY(check_shard(vocab_start, vocab, -1));
+    ECHO_TRY(check_shard(vocab_start, vocab));
     const int64_t e = elem(type), ie = index_type == ECHO_I64 ? 8 : 4;
     ECHO_TRY(check_vector("ids", ids, ie, rows > 0));
     ECHO_TRY(check_matrix("weight", weight, rows ? vocab : 0, weight_stride, e));
@@ -234,7 +238,7 @@ int echo_embedding_grad(const void *ids, int32_t index_type, const void *dy, int
     ECHO_TRY(check_types(type, grad_type, "grad_type"));
     ECHO_TRY(check_index(index_type));
     ECHO_TRY(check_sizes(rows, cols));
-    ECHO_TRY(check_shard(vocab_start, vocab, -1));
+    ECHO_TRY(check_shard(vocab_start, vocab));
     const int64_t e = elem(type), ge = elem(grad_type), ie = index_type == ECHO_I64 ? 8 : 4;
     ECHO_TRY(check_vector("ids", ids, ie, rows > 0));
     ECHO_TRY(check_matrix("dy", dy, rows, dy_stride, e));
@@ -261,7 +265,7 @@ int echo_cross_entropy(const void *logits, int64_t logits_stride, int32_t type, 
     ECHO_TRY(check_types(type, type, "type"));
     ECHO_TRY(check_index(index_type));
     ECHO_TRY(check_sizes(rows, cols));
-    ECHO_TRY(check_shard(vocab_start, cols, vocab_size));
+    ECHO_TRY(check_shard_of(vocab_start, cols, vocab_size));
     const bool whole = vocab_start == 0 && vocab_size == cols;
     if (!whole && (loss || grad))
         return set_error(ECHO_ERR_ARG, "loss and grad need the whole vocabulary; a shard gives lse and target");
@@ -297,7 +301,7 @@ int echo_cross_entropy_grad(const void *logits, int64_t logits_stride, int32_t t
     ECHO_TRY(check_types(type, type, "type"));
     ECHO_TRY(check_index(index_type));
     ECHO_TRY(check_sizes(rows, cols));
-    ECHO_TRY(check_shard(vocab_start, cols, vocab_size));
+    ECHO_TRY(check_shard_of(vocab_start, cols, vocab_size));
     const int64_t e = elem(type), ie = index_type == ECHO_I64 ? 8 : 4;
     ECHO_TRY(check_matrix("logits", logits, rows, logits_stride, e));
     ECHO_TRY(check_vector("targets", targets, ie, rows > 0));
