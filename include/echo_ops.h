@@ -81,8 +81,9 @@ int echo_embedding(const void *ids, int32_t index_type, const void *weight, int6
  *   dweight[v] = scale * sum of dy[t] over the t with ids[t] = vocab_start + v
  * for every row of the shard (zeros where no token has the id), or with accumulate != 0 added to
  * dweight, whose other rows are then left alone.  dy is of `type`, dweight [vocab][cols] of grad_type
- * (`type` or ECHO_F32); vocab <= 2^26 and rows <= 2^29 (else ECHO_ERR_RANGE).  Tokens are sorted by id first;
- * a row's tokens are summed in chunks of ascending order, and the chunks joined in an order that the sizes fix.
+ * (`type` or ECHO_F32); vocab <= 2^26, rows <= 2^29 and rows * vocab <= 2^42 (else ECHO_ERR_RANGE).  Tokens are
+ * sorted by id first, by vocab / 64 workgroups that each look through all of them; a row's tokens are summed in
+ * chunks of ascending order, and the chunks joined in an order that the sizes fix.
  * workspace: at least echo_embedding_grad_workspace(rows, cols, vocab) bytes, aligned to 16.
  */
 int64_t echo_embedding_grad_workspace(int64_t rows, int64_t cols, int64_t vocab);

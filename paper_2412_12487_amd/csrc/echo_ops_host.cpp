@@ -22,6 +22,9 @@ constexpr int64_t kMaxSorted = int64_t(1) << 26;   // rows of a table whose grad
 // Tokens of a table's gradient: a wavefront sums at least 32 of them over at least 256 columns, so at most 1.5 * 2^25
 // wavefronts (of rows * cols <= 2^38) and those that write zeros stay below 2^32 work-items.
 constexpr int64_t kMaxTokens = int64_t(1) << 29;
+// Every sorting workgroup, one for 64 rows of the table, reads every id twice: 2^20 tokens and 2^18 rows take 5.4 ms, and a
+// launch at this bound some tenths of a second.  Sizes allowed one by one would take minutes.
+constexpr int64_t kMaxSortWork = int64_t(1) << 42;
 constexpr int64_t kMaxStride = int64_t(1) << 28;   // 2^31 rows of 4-byte elements stay below 2^62 bytes
 
 int64_t elem(int32_t type) { return type == ECHO_F32 ? 4 : 2; }
@@ -245,6 +248,8 @@ int echo_embedding_grad(const void *ids, int32_t index_type, const void *dy, int
     ECHO_TRY(check_matrix("dweight", dweight, vocab, cols, ge));
     if (vocab > kMaxSorted) return set_error(ECHO_ERR_RANGE, "vocab = %lld passes 2^26", (long long)vocab);
     if (rows > kMaxTokens) return set_error(ECHO_ERR_RANGE, "rows = %lld pass 2^29", (long long)rows);
+    if (rows * vocab > kMaxSortWork)
+        return set_error(ECHO_ERR_RANGE, "%lld tokens times %lld rows pass 2^42", (long long)rows, (long long)vocab);
     const int64_t need = echo_embedding_grad_workspace(rows, cols, vocab);
     ECHO_TRY(check_workspace(workspace, workspace_bytes, need));
     ECHO_TRY(check_spans({{"dweight", dweight, vocab * cols * ge, 0}, {"workspace", workspace, need, 0}},

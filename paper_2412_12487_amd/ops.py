@@ -267,7 +267,7 @@ def embedding_grad(ids, dy, vocab, scale=1.0, *, vocab_start=0, dtype=None, out=
     """Gradient of embedding's table: [vocab, cols], of dy's type or of `dtype` (float32).
 
     dy has the shape ids.shape + (cols,).  With accumulate=True the rows that ids name are added to `out` and its
-    other rows are left alone; otherwise every row is written."""
+    other rows are left alone; otherwise every row is written.  Up to 2^29 tokens, 2^26 rows and 2^42 of their product."""
     dev = _gpu(ids, "ids")
     t = _vector(ids, "ids", dev, ids.numel(), _INDEX)
     if not isinstance(dy, torch.Tensor) or dy.dim() != ids.dim() + 1 or dy.shape[:-1] != ids.shape:

@@ -3,7 +3,7 @@ from __future__ import annotations
 
 import pytest
 
-from tests.test_ops_abi import E, L, _loss, _loss_grad  # noqa: F401 (fixtures)
+from tests.test_ops_abi import E, L, _embed_grad, _loss, _loss_grad  # noqa: F401 (fixtures)
 
 
 @pytest.mark.parametrize("whole", [-1, -2, -(1 << 62), 0, 63])
@@ -13,3 +13,14 @@ def test_a_vocabulary_smaller_than_its_shard_is_refused(E, L, call, whole):
     kw = dict(loss=None, gl=None, g=None) if call is _loss else {}
     assert call(L, whole=whole, **kw) == E.ECHO_ERR_ARG
     assert "passes the vocabulary" in L.echo_last_error().decode()
+
+
+def test_a_sort_of_unbounded_work_is_out_of_range(E, L):
+    """The ids are looked through by every sorting workgroup, vocab / 64 of them: 2^29 tokens and 2^26 rows, each allowed
+    by itself, would take minutes in one launch.  (At the bound the calls here go on to the workspace's check.)"""
+    for rows, vocab in ((1 << 20, 1 << 22), (1 << 29, 1 << 13), (1 << 16, 1 << 26)):
+        assert _embed_grad(L, rows=rows, cols=1, vocab=vocab, ws=None) == E.ECHO_ERR_ARG
+        assert "workspace" in L.echo_last_error().decode()
+    for rows, vocab in (((1 << 20) + 1, 1 << 22), (1 << 20, (1 << 22) + 1), (1 << 29, 1 << 26)):
+        assert _embed_grad(L, rows=rows, cols=1, vocab=vocab, ws=None) == E.ECHO_ERR_RANGE
+        assert "2^42" in L.echo_last_error().decode()
