@@ -32,24 +32,23 @@ _fns = None
 
 
 def _ops():
-    """The library with the operators' signatures set."""
+    """The library with the operators' signatures set: each once and to what it stays, since two threads may get here
+    together, and one go on to calls while the other sets them again."""
     global _fns
     if _fns is None:
         L = lib()
         P, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
-        L.echo_layer_norm.argtypes = [P, i64, P, i64, P, P, i32, i32, i64, i64, f32, P, P, P, P, i32, P]
-        L.echo_layer_norm_grad.argtypes = [P, i64, P, i64, P, P, P, P, i64, i32, i32, i64, i64, P, P, P, i32, i32,
-                                           P, i64, i32, P]
-        L.echo_embedding.argtypes = [P, i32, P, i64, i32, i64, i64, i64, i64, f32, P, i32, P]
-        L.echo_embedding_grad.argtypes = [P, i32, P, i64, i32, i64, i64, i64, i64, f32, P, i32, i32, P, i64, i32, P]
-        L.echo_cross_entropy.argtypes = [P, i64, i32, P, i32, i64, i64, i64, i64, P, P, P, P, P, i64, i32, P]
-        L.echo_cross_entropy_grad.argtypes = [P, i64, i32, P, i32, i64, i64, i64, i64, P, P, P, i64, i32, P]
-        for name in EXPORTS:
-            getattr(L, name).restype = i32
-        L.echo_layer_norm_grad_workspace.argtypes = [i64, i64]
-        L.echo_layer_norm_grad_workspace.restype = i64
-        L.echo_embedding_grad_workspace.argtypes = [i64, i64, i64]
-        L.echo_embedding_grad_workspace.restype = i64
+        for name, restype, argtypes in (
+                ("layer_norm", i32, [P, i64, P, i64, P, P, i32, i32, i64, i64, f32, P, P, P, P, i32, P]),
+                ("layer_norm_grad", i32, [P, i64, P, i64, P, P, P, P, i64, i32, i32, i64, i64, P, P, P, i32, i32, P, i64, i32, P]),
+                ("layer_norm_grad_workspace", i64, [i64, i64]),
+                ("embedding", i32, [P, i32, P, i64, i32, i64, i64, i64, i64, f32, P, i32, P]),
+                ("embedding_grad", i32, [P, i32, P, i64, i32, i64, i64, i64, i64, f32, P, i32, i32, P, i64, i32, P]),
+                ("embedding_grad_workspace", i64, [i64, i64, i64]),
+                ("cross_entropy", i32, [P, i64, i32, P, i32, i64, i64, i64, i64, P, P, P, P, P, i64, i32, P]),
+                ("cross_entropy_grad", i32, [P, i64, i32, P, i32, i64, i64, i64, i64, P, P, P, i64, i32, P])):
+            f = getattr(L, "echo_" + name)
+            f.restype, f.argtypes = restype, argtypes
         _fns = L
     return _fns
 

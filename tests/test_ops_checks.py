@@ -24,3 +24,36 @@ def test_a_sort_of_unbounded_work_is_out_of_range(E, L):
     for rows, vocab in (((1 << 20) + 1, 1 << 22), (1 << 20, (1 << 22) + 1), (1 << 29, 1 << 26)):
         assert _embed_grad(L, rows=rows, cols=1, vocab=vocab, ws=None) == E.ECHO_ERR_RANGE
         assert "2^42" in L.echo_last_error().decode()
+
+
+class _Function:
+    """A library function that keeps every result type it was ever given."""
+
+    def __init__(self):
+        self.__dict__["types"] = []
+
+    def __setattr__(self, name, value):
+        if name == "restype":
+            self.types.append(value)
+        self.__dict__[name] = value
+
+
+class _Library:
+    def __getattr__(self, name):
+        self.__dict__[name] = _Function()
+        return self.__dict__[name]
+
+
+def test_signatures_hold_while_another_thread_sets_them(E, monkeypatch):
+    """Two threads may both come first.  The second sets what the first may already be calling, so no function has
+    another signature in between: a workspace size cut to 32 bits would be too small a workspace."""
+    import ctypes
+
+    fake = _Library()
+    monkeypatch.setattr(E.ops, "lib", lambda: fake)
+    monkeypatch.setattr(E.ops, "_fns", None)
+    assert E.ops._ops() is fake
+    for name in E.ops.EXPORTS:
+        size = name.endswith("_workspace")
+        assert getattr(fake, name).types == [ctypes.c_int64 if size else ctypes.c_int32], name
+        assert getattr(fake, name).argtypes
