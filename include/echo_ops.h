@@ -16,7 +16,8 @@
  *     (0 to 2^28; 0 repeats one row).  Elements need the alignment of their type only.  Outputs without a
  *     stride argument are dense.  0 <= rows < 2^31, 1 <= cols <= 2^24, and rows * cols <= 2^38 (else
  *     ECHO_ERR_RANGE);
- *   - outputs may not overlap inputs or each other unless a call says so (ECHO_ERR_ARG);
+ *   - outputs may not overlap inputs or each other unless a call says so (ECHO_ERR_ARG).  Rows of one stride may lie
+ *     between each other's, as the column halves of one buffer do;
  *   - workspaces are scratch: their contents need no initialisation and mean nothing after the call,
  *     so calls on one stream may share one.  Nothing is allocated, cleared by memset or waited for, so
  *     every call can be recorded by HIP stream capture;

@@ -30,21 +30,31 @@ constexpr int64_t kMaxStride = int64_t(1) << 28;   // 2^31 rows of 4-byte elemen
 int64_t elem(int32_t type) { return type == ECHO_F32 ? 4 : 2; }
 bool is_type(int32_t t) { return t == ECHO_F32 || t == ECHO_F16 || t == ECHO_BF16; }
 
-// The bytes that an argument spans.  `same`: an output that may be exactly an input of the same
-// layout; such pairs carry the same nonzero number.
+// The bytes of an argument: rows of `width` bytes, `pitch` apart.  `same`: an output that may be exactly an input of
+// the same layout; such pairs carry the same nonzero number.
 struct Span {
     const char *name;
     const void *p;
-    int64_t bytes;
+    int64_t rows, width, pitch;
     int same;
+    int64_t bytes() const { return rows > 0 && width > 0 ? (rows - 1) * pitch + width : 0; }
 };
-int64_t span_of(int64_t rows, int64_t cols, int64_t stride, int64_t e) {
-    return rows ? ((rows - 1) * stride + cols) * e : 0;
+Span matrix(const char *name, const void *p, int64_t rows, int64_t cols, int64_t stride, int64_t e, int same = 0) {
+    return {name, p, rows, cols * e, stride * e, same};
 }
+Span vector(const char *name, const void *p, int64_t n, int64_t e) { return {name, p, 1, n * e, 0, 0}; }
+// Whether two arguments share a byte.  Rows of one pitch may lie in each other's gaps; of two pitches that are not the same
+// the whole spans have to be apart.
 bool meet(const Span &a, const Span &b) {
-    if (!a.p || !b.p || a.bytes <= 0 || b.bytes <= 0) return false;
+    const int64_t m = a.bytes(), n = b.bytes();
+    if (!a.p || !b.p || m <= 0 || n <= 0) return false;
     const uintptr_t p = (uintptr_t)a.p, q = (uintptr_t)b.p;
-    return p < q + (uintptr_t)b.bytes && q < p + (uintptr_t)a.bytes;
+    if (p >= q + (uintptr_t)n || q >= p + (uintptr_t)m) return false;
+    const int64_t pitch = a.rows > 1 ? a.pitch : b.pitch;
+    if (pitch <= 0 || (b.rows > 1 && b.pitch != pitch)) return true;
+    // how far into a's rows b's begin
+    const int64_t by = p <= q ? (int64_t)(q - p) % pitch : (pitch - (int64_t)(p - q) % pitch) % pitch;
+    return by < a.width || by + b.width > pitch;
 }
 // Every output against every input and every other output.
 int check_spans(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
@@ -52,7 +62,7 @@ int check_spans(std::initializer_list<Span> outs, std::initializer_list<Span> in
         for (const Span *q = outs.begin(); q != o; ++q)
             if (meet(*o, *q)) return set_error(ECHO_ERR_ARG, "%s and %s overlap", o->name, q->name);
         for (const Span &i : ins)
-            if (meet(*o, i) && !(o->same && (o->same & i.same) && o->p == i.p && o->bytes == i.bytes))
+            if (meet(*o, i) && !(o->same && (o->same & i.same) && o->p == i.p && o->bytes() == i.bytes()))
                 return set_error(ECHO_ERR_ARG, "%s overlaps %s", o->name, i.name);
     }
     return ECHO_OK;
@@ -151,12 +161,11 @@ int echo_layer_norm(const void *x, int64_t x_stride, const void *residual, int64
     ECHO_TRY(check_matrix("sum", sum, live, cols, e));
     ECHO_TRY(check_vector("mean", mean, 4, rows > 0));
     ECHO_TRY(check_vector("rstd", rstd, 4, rows > 0));
-    ECHO_TRY(check_spans({{"y", y, rows * cols * e, 0}, {"sum", sum, live * cols * e, 1}, {"mean", mean, rows * 4, 0},
-                          {"rstd", rstd, rows * 4, 0}},
-                         {{"x", x, span_of(rows, cols, x_stride, e), rows < 2 || x_stride == cols},
-                          {"residual", residual, span_of(live, cols, residual_stride, e),
-                           rows < 2 || residual_stride == cols},
-                          {"weight", weight, cols * we, 0}, {"bias", bias, cols * we, 0}}));
+    ECHO_TRY(check_spans({matrix("y", y, rows, cols, cols, e), matrix("sum", sum, live, cols, cols, e, 1), vector("mean", mean, rows, 4),
+                          vector("rstd", rstd, rows, 4)},
+                         {matrix("x", x, rows, cols, x_stride, e, rows < 2 || x_stride == cols),
+                          matrix("residual", residual, live, cols, residual_stride, e, rows < 2 || residual_stride == cols),
+                          vector("weight", weight, cols, we), vector("bias", bias, cols, we)}));
     if (!rows) return ECHO_OK;
     const NormArgs a{x, residual, weight, bias, x_stride, residual_stride, rows, (int)cols, eps, y, sum, mean, rstd};
     return on_device(hip_device, "layer norm", [&] {
@@ -192,13 +201,12 @@ int echo_layer_norm_grad(const void *dy, int64_t dy_stride, const void *x, int64
     ECHO_TRY(check_vector("dbias", dbias, ge, false));
     const int64_t need = echo_layer_norm_grad_workspace(rows, cols);
     ECHO_TRY(check_workspace(workspace, workspace_bytes, need));
-    ECHO_TRY(check_spans({{"dx", dx, rows * cols * e, 1}, {"dweight", dweight, cols * ge, 0},
-                          {"dbias", dbias, cols * ge, 0}, {"workspace", workspace, need, 0}},
-                         {{"dy", dy, span_of(rows, cols, dy_stride, e), rows < 2 || dy_stride == cols},
-                          {"x", x, span_of(rows, cols, x_stride, e), 0},
-                          {"grad_residual", grad_residual, span_of(live, cols, grad_residual_stride, e),
-                           rows < 2 || grad_residual_stride == cols},
-                          {"weight", weight, cols * we, 0}, {"mean", mean, rows * 4, 0}, {"rstd", rstd, rows * 4, 0}}));
+    ECHO_TRY(check_spans({matrix("dx", dx, rows, cols, cols, e, 1), vector("dweight", dweight, cols, ge),
+                          vector("dbias", dbias, cols, ge), vector("workspace", workspace, need, 1)},
+                         {matrix("dy", dy, rows, cols, dy_stride, e, rows < 2 || dy_stride == cols),
+                          matrix("x", x, rows, cols, x_stride, e),
+                          matrix("grad_residual", grad_residual, live, cols, grad_residual_stride, e, rows < 2 || grad_residual_stride == cols),
+                          vector("weight", weight, cols, we), vector("mean", mean, rows, 4), vector("rstd", rstd, rows, 4)}));
     const NormGradArgs a{dy, x, weight, grad_residual, mean, rstd, dy_stride, x_stride, grad_residual_stride, rows,
                          (int)cols, dx, dweight, dbias, static_cast<float *>(workspace), norm_grad_parts(rows, cols),
                          accumulate != 0};
@@ -219,8 +227,8 @@ int echo_embedding(const void *ids, int32_t index_type, const void *weight, int6
     ECHO_TRY(check_vector("ids", ids, ie, rows > 0));
     ECHO_TRY(check_matrix("weight", weight, rows ? vocab : 0, weight_stride, e));
     ECHO_TRY(check_matrix("out", out, rows, cols, e));
-    ECHO_TRY(check_spans({{"out", out, rows * cols * e, 0}},
-                         {{"ids", ids, rows * ie, 0}, {"weight", weight, span_of(vocab, cols, weight_stride, e), 0}}));
+    ECHO_TRY(check_spans({matrix("out", out, rows, cols, cols, e)},
+                         {vector("ids", ids, rows, ie), matrix("weight", weight, vocab, cols, weight_stride, e)}));
     if (!rows) return ECHO_OK;
     const EmbedArgs a{ids, weight, weight_stride, rows, vocab_start, (int)cols, (int)vocab, scale, out};
     return on_device(hip_device, "embedding", [&] {
@@ -252,8 +260,8 @@ int echo_embedding_grad(const void *ids, int32_t index_type, const void *dy, int
         return set_error(ECHO_ERR_RANGE, "%lld tokens times %lld rows pass 2^42", (long long)rows, (long long)vocab);
     const int64_t need = echo_embedding_grad_workspace(rows, cols, vocab);
     ECHO_TRY(check_workspace(workspace, workspace_bytes, need));
-    ECHO_TRY(check_spans({{"dweight", dweight, vocab * cols * ge, 0}, {"workspace", workspace, need, 0}},
-                         {{"ids", ids, rows * ie, 0}, {"dy", dy, span_of(rows, cols, dy_stride, e), 0}}));
+    ECHO_TRY(check_spans({vector("dweight", dweight, vocab * cols, ge), vector("workspace", workspace, need, 1)},
+                         {vector("ids", ids, rows, ie), matrix("dy", dy, rows, cols, dy_stride, e)}));
     if (!vocab || (!rows && accumulate)) return ECHO_OK;
     const EmbedGradArgs a{ids, dy, dy_stride, rows, vocab_start, (int)cols, (int)vocab, scale, dweight,
                           accumulate != 0, workspace};
@@ -286,10 +294,10 @@ int echo_cross_entropy(const void *logits, int64_t logits_stride, int32_t type, 
     ECHO_TRY(check_matrix("grad", grad, live, grad ? grad_stride : 0, e));
     if (live > 1 && grad_stride < cols) return set_error(ECHO_ERR_ARG, "rows of grad overlap");
     const bool dense = rows < 2 || logits_stride == grad_stride;
-    ECHO_TRY(check_spans({{"grad", grad, span_of(live, cols, grad_stride, e), 1}, {"lse", lse, rows * 4, 0},
-                          {"target", target, rows * 4, 0}, {"loss", loss, rows * 4, 0}},
-                         {{"logits", logits, span_of(rows, cols, logits_stride, e), dense},
-                          {"targets", targets, rows * ie, 0}, {"grad_loss", grad_loss, rows * 4, 0}}));
+    ECHO_TRY(check_spans({matrix("grad", grad, live, cols, grad_stride, e, 1), vector("lse", lse, rows, 4),
+                          vector("target", target, rows, 4), vector("loss", loss, rows, 4)},
+                         {matrix("logits", logits, rows, cols, logits_stride, e, dense),
+                          vector("targets", targets, rows, ie), vector("grad_loss", grad_loss, rows, 4)}));
     if (!rows) return ECHO_OK;
     const LossArgs a{logits, targets, logits_stride, rows, vocab_start, vocab_size, (int)cols, lse, target, loss,
                      nullptr, grad_loss, grad, grad_stride};
@@ -315,10 +323,10 @@ int echo_cross_entropy_grad(const void *logits, int64_t logits_stride, int32_t t
     ECHO_TRY(check_matrix("grad", grad, rows, grad_stride, e));
     if (rows > 1 && grad_stride < cols) return set_error(ECHO_ERR_ARG, "rows of grad overlap");
     const bool dense = rows < 2 || logits_stride == grad_stride;
-    ECHO_TRY(check_spans({{"grad", grad, span_of(rows, cols, grad_stride, e), 1}},
-                         {{"logits", logits, span_of(rows, cols, logits_stride, e), dense},
-                          {"targets", targets, rows * ie, 0}, {"lse", lse, rows * 4, 0},
-                          {"grad_loss", grad_loss, rows * 4, 0}}));
+    ECHO_TRY(check_spans({matrix("grad", grad, rows, cols, grad_stride, e, 1)},
+                         {matrix("logits", logits, rows, cols, logits_stride, e, dense),
+                          vector("targets", targets, rows, ie), vector("lse", lse, rows, 4),
+                          vector("grad_loss", grad_loss, rows, 4)}));
     if (!rows) return ECHO_OK;
     const LossArgs a{logits, targets, logits_stride, rows, vocab_start, vocab_size, (int)cols, nullptr, nullptr,
                      nullptr, lse, grad_loss, grad, grad_stride};

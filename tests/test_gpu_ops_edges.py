@@ -1,4 +1,4 @@
-"""Edges of the training-step operators: statistics at the edge of 32 bits."""
+"""Edges of the training-step operators: statistics at the edge of 32 bits, arguments between each other's rows."""
 from __future__ import annotations
 
 import math
@@ -38,3 +38,24 @@ def test_layer_norm_grad_where_mean_times_rstd_passes_32_bits(cols, dtype):
     out = E.layer_norm_grad(dy, x, w, s["mean"], s["rstd"], grad_residual=dr, dtype=F32)
     for k, (v, e) in R.layer_norm_grad(dy, x, w, s["mean"], s["rstd"], dr).items():
         R.close(out[k], v, e, k)
+
+
+@pytest.mark.parametrize("cols", [3, 64, 517, 2056, 20001, 70001])
+def test_cross_entropy_gradient_between_the_rows_of_the_logits(cols):
+    """Column halves of one buffer: nothing shares a byte, and nothing outside the gradient's half is written."""
+    g = _gen(cols)
+    pad = 5
+    buf = _normal(g, 9, 2 * cols + pad, std=2.0, dtype=BF16)
+    t = torch.randint(0, cols, (9,), generator=g, device="cuda")
+    gl = _normal(g, 9)
+    for lo, hi in ((0, cols + pad), (cols + pad, 0)):
+        before = buf.clone()
+        l, d = buf[:, lo:lo + cols], buf[:, hi:hi + cols]
+        want = E.cross_entropy(l.clone(), t, grad_loss=gl)
+        got = E.cross_entropy(l, t, grad_loss=gl, out={"grad": d})
+        assert all(torch.equal(got[k], want[k]) for k in want)
+        d.copy_(before[:, hi:hi + cols])
+        got = E.cross_entropy_grad(l, t, want["lse"], gl, out=d)
+        assert torch.equal(got, E.cross_entropy_grad(l.clone(), t, want["lse"], gl))
+        d.copy_(before[:, hi:hi + cols])
+        assert torch.equal(buf, before)

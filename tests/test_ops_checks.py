@@ -57,3 +57,37 @@ def test_signatures_hold_while_another_thread_sets_them(E, monkeypatch):
         size = name.endswith("_workspace")
         assert getattr(fake, name).types == [ctypes.c_int64 if size else ctypes.c_int32], name
         assert getattr(fake, name).argtypes
+
+
+NOWHERE = 1 << 20      # no such GPU: what passes the checks ends there, with nothing launched
+MB = 1 << 20
+
+
+@pytest.mark.parametrize("what,logits,grad,rows,cols,ls,gs,apart", [
+    ("halves of one buffer", 0, 128, 8, 64, 128, 128, True),
+    ("halves the other way round", 128, 0, 8, 64, 128, 128, True),
+    ("an element into the other half", 0, 126, 8, 64, 128, 128, False),
+    ("an element into the next row", 0, 130, 8, 64, 128, 128, False),
+    ("the other half, three rows on", 0, 128 + 3 * 256, 8, 64, 128, 128, True),
+    ("the same columns, three rows on", 0, 3 * 256, 8, 64, 128, 128, False),
+    ("past the last row", 0, 8 * 256, 8, 64, 128, 128, True),
+    ("one row in the gap of none", 0, 128, 1, 64, 128, 128, True),
+    ("rows that drift through each other's gaps", 0, 128, 8, 64, 128, 192, False),
+    ("rows of one repeated", 0, 64, 8, 64, 0, 128, False),
+    ("logits whose rows overlap, gradient between their starts", 0, 64, 8, 64, 32, 128, False),
+])
+def test_only_what_shares_bytes_overlaps(E, L, what, logits, grad, rows, cols, ls, gs, apart):
+    """bfloat16 matrices in one buffer, offsets in bytes."""
+    rc = L.echo_cross_entropy_grad(MB + logits, ls, 2, 3 * MB, 1, rows, cols, 0, cols, 4 * MB, 5 * MB, MB + grad, gs, NOWHERE, None)
+    assert rc == (E.ECHO_ERR_HIP if apart else E.ECHO_ERR_ARG), (what, L.echo_last_error())
+    assert apart or "grad overlaps logits" in L.echo_last_error().decode()
+
+
+def test_a_vector_between_the_rows_of_a_matrix(E, L):
+    def call(lse, rows=8):
+        return L.echo_cross_entropy(MB, 128, 2, 3 * MB, 1, rows, 64, 0, 64, lse, None, 5 * MB, None, None, 0, NOWHERE, None)
+
+    assert call(MB + 128) == E.ECHO_ERR_HIP                   # 32 bytes in the first row's gap
+    assert call(MB + 128, rows=1) == E.ECHO_ERR_HIP
+    assert call(MB + 256 - 16) == E.ECHO_ERR_ARG              # into the second row
+    assert call(MB + 64) == E.ECHO_ERR_ARG
