@@ -40,7 +40,8 @@ def _ops():
         P, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
         for name, restype, argtypes in (
                 ("layer_norm", i32, [P, i64, P, i64, P, P, i32, i32, i64, i64, f32, P, P, P, P, i32, P]),
-                ("layer_norm_grad", i32, [P, i64, P, i64, P, P, P, P, i64, i32, i32, i64, i64, P, P, P, i32, i32, P, i64, i32, P]),
+                ("layer_norm_grad", i32, [P, i64, P, i64, P, P, P, P, i64, i32, i32, i64, i64, P, P, P, i32, i32, P, i64, i32,
+                                          P]),
                 ("layer_norm_grad_workspace", i64, [i64, i64]),
                 ("embedding", i32, [P, i32, P, i64, i32, i64, i64, i64, i64, f32, P, i32, P]),
                 ("embedding_grad", i32, [P, i32, P, i64, i32, i64, i64, i64, i64, f32, P, i32, i32, P, i64, i32, P]),
@@ -55,6 +56,14 @@ def _ops():
 
 def _bad(msg):
     return EchoError(ECHO_ERR_ARG, msg)
+
+
+def _int64(n, name):
+    """n as the library takes it; ctypes would cut a larger one."""
+    n = int(n)
+    if not -(1 << 63) <= n < 1 << 63:
+        raise _bad(f"{name} = {n} does not fit 64 bits")
+    return n
 
 
 def _gpu(t, name):
@@ -249,7 +258,7 @@ def embedding(ids, weight, scale=1.0, *, vocab_start=0, out=None):
 
     weight holds the rows vocab_start .. vocab_start + len(weight) - 1 of the vocabulary; an id
     outside them (another rank's, or a negative one for padding) gives a row of zeros."""
-    dev = _gpu(ids, "ids")
+    start, dev = _int64(vocab_start, "vocab_start"), _gpu(ids, "ids")
     t = _vector(ids, "ids", dev, ids.numel(), _INDEX)
     if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
         raise _bad("weight must be a matrix")
@@ -257,7 +266,7 @@ def embedding(ids, weight, scale=1.0, *, vocab_start=0, out=None):
     shape = ids.shape + (cols,)
     res = weight.new_empty(shape) if out is None else _dense(out, "out", dev, shape, weight.dtype)
     _check(_ops().echo_embedding(t, _INDEX[ids.dtype], weight.data_ptr(), ws, _TYPES[weight.dtype], ids.numel(), cols,
-                                 int(vocab_start), vocab, float(scale), res.data_ptr(), dev.index, _stream(dev.index)))
+                                 start, vocab, float(scale), res.data_ptr(), dev.index, _stream(dev.index)))
     return res
 
 
@@ -267,7 +276,7 @@ def embedding_grad(ids, dy, vocab, scale=1.0, *, vocab_start=0, dtype=None, out=
 
     dy has the shape ids.shape + (cols,).  With accumulate=True the rows that ids name are added to `out` and its
     other rows are left alone; otherwise every row is written.  Up to 2^29 tokens, 2^26 rows and 2^42 of their product."""
-    dev = _gpu(ids, "ids")
+    start, dev = _int64(vocab_start, "vocab_start"), _gpu(ids, "ids")
     t = _vector(ids, "ids", dev, ids.numel(), _INDEX)
     if not isinstance(dy, torch.Tensor) or dy.dim() != ids.dim() + 1 or dy.shape[:-1] != ids.shape:
         raise _bad("dy must have the shape of ids and one dimension more")
@@ -278,24 +287,27 @@ def embedding_grad(ids, dy, vocab, scale=1.0, *, vocab_start=0, dtype=None, out=
         dtype = out.dtype if isinstance(out, torch.Tensor) else dy.dtype
     if dtype not in (dy.dtype, torch.float32):
         raise _bad(f"dtype must be {dy.dtype} or torch.float32 (got {dtype})")
-    vocab = int(vocab)
+    vocab = _int64(vocab, "vocab")
     if vocab < 0:
         raise _bad("vocab must be >= 0")
     res = dy.new_empty((vocab, cols), dtype=dtype) if out is None else _dense(out, "out", dev, (vocab, cols), dtype)
     L = _ops()
     space = _space(workspace, L.echo_embedding_grad_workspace(rows, cols, vocab), dy)
     _check(L.echo_embedding_grad(
-        t, _INDEX[ids.dtype], dy.data_ptr(), ds, _TYPES[dy.dtype], rows, cols, int(vocab_start), vocab, float(scale),
+        t, _INDEX[ids.dtype], dy.data_ptr(), ds, _TYPES[dy.dtype], rows, cols, start, vocab, float(scale),
         res.data_ptr(), _TYPES[dtype], int(bool(accumulate)), *_space_args(space), dev.index, _stream(dev.index)))
     return res
 
 
-def _loss_args(logits, targets):
+def _loss_args(logits, targets, vocab_start, vocab_size):
     dev = _gpu(logits, "logits")
     rows, cols, ls = _matrix(logits, "logits", dev, _TYPES)
     if not isinstance(targets, torch.Tensor) or targets.shape != logits.shape[:-1]:
         raise _bad("targets must have the leading shape of logits")
-    return dev, rows, cols, ls, _vector(targets, "targets", dev, rows, _INDEX)
+    if vocab_size is None and vocab_start:
+        raise _bad("vocab_start needs vocab_size")
+    return (dev, rows, cols, ls, _vector(targets, "targets", dev, rows, _INDEX), _int64(vocab_start, "vocab_start"),
+            cols if vocab_size is None else _int64(vocab_size, "vocab_size"))
 
 
 def _grad_out(t, logits, dev, rows, cols):
@@ -319,12 +331,10 @@ def cross_entropy(logits, targets, *, vocab_start=0, vocab_size=None, grad_loss=
     them: a dict with 'lse' over these rows and 'target', the target's logit or 0 where it is another
     rank's.  The whole lse is the logarithm of the ranks' sum of exp(lse), the target's logit their sum, and
     loss = lse - target; cross_entropy_grad then gives each rank its gradient."""
-    dev, rows, cols, ls, t = _loss_args(logits, targets)
+    dev, rows, cols, ls, t, start, whole = _loss_args(logits, targets, vocab_start, vocab_size)
     shape = logits.shape[:-1]
     if vocab_size is None:
-        if vocab_start:
-            raise _bad("vocab_start needs vocab_size")
-        vocab_size, names = cols, ("loss", "lse")
+        names = ("loss", "lse")
     else:
         if grad_loss is not None:
             raise _bad("a shard's gradient needs the whole vocabulary's lse: use cross_entropy_grad")
@@ -342,8 +352,8 @@ def cross_entropy(logits, targets, *, vocab_start=0, vocab_size=None, grad_loss=
         res["grad"], gs = _grad_out(res.get("grad"), logits, dev, rows, cols)
         g = res["grad"].data_ptr()
     _check(_ops().echo_cross_entropy(
-        logits.data_ptr(), ls, _TYPES[logits.dtype], t, _INDEX[targets.dtype], rows, cols, int(vocab_start),
-        int(vocab_size), res["lse"].data_ptr(), res["target"].data_ptr() if "target" in res else None,
+        logits.data_ptr(), ls, _TYPES[logits.dtype], t, _INDEX[targets.dtype], rows, cols, start, whole,
+        res["lse"].data_ptr(), res["target"].data_ptr() if "target" in res else None,
         res["loss"].data_ptr() if "loss" in res else None, gl, g, gs, dev.index, _stream(dev.index)))
     return res
 
@@ -351,15 +361,11 @@ def cross_entropy(logits, targets, *, vocab_start=0, vocab_size=None, grad_loss=
 def cross_entropy_grad(logits, targets, lse, grad_loss, *, vocab_start=0, vocab_size=None, out=None):
     """(exp(logits - lse) - onehot(targets)) * grad_loss, like logits: the gradient of cross entropy for the
     columns held here, with lse and grad_loss float32 of targets' shape.  `out` may be logits itself."""
-    dev, rows, cols, ls, t = _loss_args(logits, targets)
-    if vocab_size is None:
-        if vocab_start:
-            raise _bad("vocab_start needs vocab_size")
-        vocab_size = cols
+    dev, rows, cols, ls, t, start, whole = _loss_args(logits, targets, vocab_start, vocab_size)
     e = _vector(lse, "lse", dev, rows, (torch.float32,))
     gl = _vector(grad_loss, "grad_loss", dev, rows, (torch.float32,))
     res, gs = _grad_out(out, logits, dev, rows, cols)
     _check(_ops().echo_cross_entropy_grad(
-        logits.data_ptr(), ls, _TYPES[logits.dtype], t, _INDEX[targets.dtype], rows, cols, int(vocab_start),
-        int(vocab_size), e, gl, res.data_ptr(), gs, dev.index, _stream(dev.index)))
+        logits.data_ptr(), ls, _TYPES[logits.dtype], t, _INDEX[targets.dtype], rows, cols, start, whole,
+        e, gl, res.data_ptr(), gs, dev.index, _stream(dev.index)))
     return res

@@ -59,3 +59,17 @@ def test_cross_entropy_gradient_between_the_rows_of_the_logits(cols):
         assert torch.equal(got, E.cross_entropy_grad(l.clone(), t, want["lse"], gl))
         d.copy_(before[:, hi:hi + cols])
         assert torch.equal(buf, before)
+
+
+@pytest.mark.parametrize("start", [1 << 63, 1 << 64, 1 - (1 << 64)])
+def test_shards_that_start_beyond_64_bits_are_refused(start):
+    table, logits = torch.ones(10, 4, device="cuda"), torch.zeros(2, 8, device="cuda")
+    ids = torch.tensor([0, 3], device="cuda")
+    for call in (lambda: E.embedding(ids, table, vocab_start=start),
+                 lambda: E.embedding_grad(ids, table[:2], 10, vocab_start=start),
+                 lambda: E.cross_entropy(logits, ids, vocab_start=start, vocab_size=100),
+                 lambda: E.cross_entropy(logits, ids, vocab_start=0, vocab_size=start),
+                 lambda: E.cross_entropy_grad(logits, ids, logits[:, 0].contiguous(), logits[:, 1].contiguous(), vocab_start=start,
+                                              vocab_size=100)):
+        with pytest.raises(E.EchoError, match="64 bits"):
+            call()

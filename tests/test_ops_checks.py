@@ -91,3 +91,13 @@ def test_a_vector_between_the_rows_of_a_matrix(E, L):
     assert call(MB + 128, rows=1) == E.ECHO_ERR_HIP
     assert call(MB + 256 - 16) == E.ECHO_ERR_ARG              # into the second row
     assert call(MB + 64) == E.ECHO_ERR_ARG
+
+
+def test_shard_starts_beyond_64_bits_are_refused(E, monkeypatch):
+    """ctypes would cut them to 64 bits: 2^64 would be the id 0."""
+    for n in (1 << 63, 1 << 64, -(1 << 63) - 1, 1 - (1 << 64)):
+        with pytest.raises(E.EchoError, match="64 bits") as e:
+            E.ops._int64(n, "vocab_start")
+        assert e.value.code == E.ECHO_ERR_ARG
+    for n in (0, 5, (1 << 63) - 1, -(1 << 63)):
+        assert E.ops._int64(n, "vocab_start") == n
