@@ -13,6 +13,9 @@ one stride; nothing is copied into order behind the caller's back: another layou
 Sums and statistics are in 32 bits and each result is rounded once.  Work is enqueued on the
 current stream of the tensors' GPU; outputs and workspaces not passed in come from torch's allocator on
 that stream.  Every call can be captured in a HIP graph.  Results do not vary from run to run.
+
+Nothing is recorded for automatic differentiation: gradients are calls of their own, and tensors that require grad
+are taken under torch.no_grad() or detached (where a graph is recorded they raise EchoError).
 """
 from __future__ import annotations
 
@@ -75,6 +78,9 @@ def _gpu(t, name):
     return t.device
 
 
+_GRAPH = "%s requires grad, and the operators record no graph: call them under torch.no_grad() or with detached tensors"
+
+
 def _matrix(t, name, dev, types):
     """(rows, cols, row stride) of a tensor read as rows of its last dimension."""
     if not isinstance(t, torch.Tensor):
@@ -83,6 +89,8 @@ def _matrix(t, name, dev, types):
         raise _bad(f"{name} is on {t.device}, the call on {dev}")
     if t.dtype not in types:
         raise _bad(f"{name} must be {' or '.join(str(x) for x in types)} (got {t.dtype})")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise _bad(_GRAPH % name)
     if t.dim() < 1:
         raise _bad(f"{name} must have at least one dimension")
     cols = t.shape[-1]
@@ -118,6 +126,8 @@ def _vector(t, name, dev, n, types):
         raise _bad(f"{name} is on {t.device}, the call on {dev}")
     if t.dtype not in types:
         raise _bad(f"{name} must be {' or '.join(str(x) for x in types)} (got {t.dtype})")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise _bad(_GRAPH % name)
     if t.numel() != n:
         raise _bad(f"{name} has {t.numel()} elements, needs {n}")
     if not t.is_contiguous():
@@ -144,6 +154,8 @@ def _dense(t, name, dev, shape, dtype):
         raise _bad(f"{name} is on {t.device}, the call on {dev}")
     if t.dtype != dtype:
         raise _bad(f"{name} must be {dtype} (got {t.dtype})")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise _bad(_GRAPH % name)
     if t.shape != torch.Size(shape):
         raise _bad(f"{name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
     if not t.is_contiguous():

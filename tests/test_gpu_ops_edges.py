@@ -73,3 +73,39 @@ def test_shards_that_start_beyond_64_bits_are_refused(start):
                                               vocab_size=100)):
         with pytest.raises(E.EchoError, match="64 bits"):
             call()
+
+
+def _calls():
+    """{name: (call of the tensors, those tensors)} over every input and every tensor that may be written."""
+    g = _gen(7)
+    x, r, dy = (_normal(g, 6, 40) for _ in range(3))
+    w, b = _normal(g, 40), _normal(g, 40)
+    s = E.layer_norm(x, w, b)
+    ids, table = torch.arange(6, device="cuda"), _normal(g, 9, 40)
+    logits, gl, lse = _normal(g, 6, 40), _normal(g, 6), _normal(g, 6)
+    e = torch.empty_like
+    return {
+        "layer_norm": (lambda x, w, b, r, y, t: E.layer_norm(x, w, b, residual=r, out={"y": y, "sum": t}), (x, w, b, r, e(x), e(x)), 4),
+        "layer_norm_grad": (lambda dy, x, w, m, k, r, dx, dw, db: E.layer_norm_grad(
+            dy, x, w, m, k, grad_residual=r, out={"dx": dx, "dweight": dw, "dbias": db}),
+            (dy, x, w, s["mean"], s["rstd"], r, e(x), e(w), e(b)), 6),
+        "embedding": (lambda w, o: E.embedding(ids, w, out=o), (table, e(x)), 1),
+        "embedding_grad": (lambda dy, o: E.embedding_grad(ids, dy, 9, out=o), (dy, e(table)), 1),
+        "cross_entropy": (lambda l, gl, d, lse: E.cross_entropy(l, ids, grad_loss=gl, out={"grad": d, "lse": lse}),
+                          (logits, gl, e(logits), e(gl)), 2),
+        "cross_entropy_grad": (lambda l, lse, gl, d: E.cross_entropy_grad(l, ids, lse, gl, out=d), (logits, lse, gl, e(logits)), 3),
+    }
+
+
+@pytest.mark.parametrize("name", ["layer_norm", "layer_norm_grad", "embedding", "embedding_grad", "cross_entropy", "cross_entropy_grad"])
+def test_tensors_that_require_grad_are_refused_where_a_graph_is_recorded(name):
+    """The calls record nothing for automatic differentiation: a gradient would be lost without a word."""
+    call, tensors, _ = _calls()[name]
+    call(*tensors)
+    for i in range(len(tensors)):
+        leaf = [t.clone().requires_grad_(k == i) for k, t in enumerate(tensors)]
+        with pytest.raises(E.EchoError, match="requires grad"):
+            call(*leaf)
+        with torch.no_grad():
+            call(*leaf)
+        call(*[t.detach() for t in leaf])
