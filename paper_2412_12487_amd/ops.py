@@ -15,7 +15,8 @@ current stream of the tensors' GPU; outputs and workspaces not passed in come fr
 that stream.  Every call can be captured in a HIP graph.  Results do not vary from run to run.
 
 Nothing is recorded for automatic differentiation: gradients are calls of their own, and tensors that require grad
-are taken under torch.no_grad() or detached (where a graph is recorded they raise EchoError).
+are taken under torch.no_grad() or detached (where a graph is recorded they raise EchoError).  Tensors that a call
+writes over count as modified in place.
 """
 from __future__ import annotations
 
@@ -192,6 +193,10 @@ def _only(out, names):
     return out
 
 
+# Counts tensors as modified in place, so that a backward pass that saved one of them notices.
+_written = torch.autograd.graph.increment_version
+
+
 def layer_norm(x, weight, bias=None, eps=1e-5, *, residual=None, out=None):
     """Layer norm over the last dimension, of x or of x + residual.
 
@@ -220,6 +225,8 @@ def layer_norm(x, weight, bias=None, eps=1e-5, *, residual=None, out=None):
         x.data_ptr(), xs, r, rs, w, b, _TYPES[x.dtype], _TYPES[weight.dtype], rows, cols, float(eps),
         res["y"].data_ptr(), None if r is None else res["sum"].data_ptr(), res["mean"].data_ptr(),
         res["rstd"].data_ptr(), dev.index, _stream(dev.index)))
+    if out:
+        _written([res[k] for k in out])
     return res
 
 
@@ -262,6 +269,8 @@ def layer_norm_grad(dy, x, weight, mean, rstd, *, grad_residual=None, bias=True,
         dy.data_ptr(), ds, x.data_ptr(), xs, w, m, k, r, rs, _TYPES[dy.dtype], _TYPES[weight.dtype], rows, cols,
         res["dx"].data_ptr(), res["dweight"].data_ptr(), res["dbias"].data_ptr() if bias else None, _TYPES[dtype],
         int(bool(accumulate)), *_space_args(space), dev.index, _stream(dev.index)))
+    if out:
+        _written([res[k] for k in out])
     return res
 
 
@@ -279,6 +288,8 @@ def embedding(ids, weight, scale=1.0, *, vocab_start=0, out=None):
     res = weight.new_empty(shape) if out is None else _dense(out, "out", dev, shape, weight.dtype)
     _check(_ops().echo_embedding(t, _INDEX[ids.dtype], weight.data_ptr(), ws, _TYPES[weight.dtype], ids.numel(), cols,
                                  start, vocab, float(scale), res.data_ptr(), dev.index, _stream(dev.index)))
+    if out is not None:
+        _written(out)
     return res
 
 
@@ -308,6 +319,8 @@ def embedding_grad(ids, dy, vocab, scale=1.0, *, vocab_start=0, dtype=None, out=
     _check(L.echo_embedding_grad(
         t, _INDEX[ids.dtype], dy.data_ptr(), ds, _TYPES[dy.dtype], rows, cols, start, vocab, float(scale),
         res.data_ptr(), _TYPES[dtype], int(bool(accumulate)), *_space_args(space), dev.index, _stream(dev.index)))
+    if out is not None:
+        _written(out)
     return res
 
 
@@ -367,6 +380,8 @@ def cross_entropy(logits, targets, *, vocab_start=0, vocab_size=None, grad_loss=
         logits.data_ptr(), ls, _TYPES[logits.dtype], t, _INDEX[targets.dtype], rows, cols, start, whole,
         res["lse"].data_ptr(), res["target"].data_ptr() if "target" in res else None,
         res["loss"].data_ptr() if "loss" in res else None, gl, g, gs, dev.index, _stream(dev.index)))
+    if out:
+        _written([res[k] for k in out])
     return res
 
 
@@ -380,4 +395,6 @@ def cross_entropy_grad(logits, targets, lse, grad_loss, *, vocab_start=0, vocab_
     _check(_ops().echo_cross_entropy_grad(
         logits.data_ptr(), ls, _TYPES[logits.dtype], t, _INDEX[targets.dtype], rows, cols, start, whole,
         e, gl, res.data_ptr(), gs, dev.index, _stream(dev.index)))
+    if out is not None:
+        _written(out)
     return res

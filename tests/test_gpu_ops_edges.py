@@ -109,3 +109,34 @@ def test_tensors_that_require_grad_are_refused_where_a_graph_is_recorded(name):
         with torch.no_grad():
             call(*leaf)
         call(*[t.detach() for t in leaf])
+
+
+@pytest.mark.parametrize("name", ["layer_norm", "layer_norm_grad", "embedding", "embedding_grad", "cross_entropy", "cross_entropy_grad"])
+def test_a_saved_tensor_that_a_call_wrote_is_noticed(name):
+    """As after any in-place operation: backward through a tensor that was written since raises."""
+    call, tensors, first = _calls()[name]
+    for i in range(first, len(tensors)):
+        leaf = torch.zeros_like(tensors[i]).requires_grad_()
+        saved = leaf.exp()                 # its backward reads what it returned
+        call(*[saved.detach() if k == i else t for k, t in enumerate(tensors)])
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            saved.sum().backward()
+    kept = torch.zeros_like(tensors[0]).requires_grad_()
+    read = kept.exp()
+    call(read.detach(), *tensors[1:])      # an input is only read
+    read.sum().backward()
+
+
+def test_outputs_over_inputs_count_as_written():
+    g = _gen(8)
+    x, r, w = _normal(g, 6, 40), _normal(g, 6, 40), _normal(g, 40)
+    ids, gl = torch.arange(6, device="cuda"), _normal(g, 6)
+    s = E.layer_norm(x, w)
+    for call in (lambda t: E.layer_norm(t, w, residual=r, out={"sum": t}), lambda t: E.layer_norm(x, w, residual=t, out={"sum": t}),
+                 lambda t: E.layer_norm_grad(t, x, w, s["mean"], s["rstd"], out={"dx": t}),
+                 lambda t: E.cross_entropy(t, ids, grad_loss=gl, out={"grad": t}),
+                 lambda t: E.cross_entropy_grad(t, ids, gl, gl, out=t)):
+        saved = _normal(g, 6, 40).requires_grad_().exp()
+        call(saved.detach())
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            saved.sum().backward()
