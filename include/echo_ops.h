@@ -97,7 +97,7 @@ int echo_embedding_grad(const void *ids, int32_t index_type, const void *dy, int
  * Cross entropy of rows of logits over the ids [vocab_start, vocab_start + cols) of a vocabulary of
  * vocab_size ids (the others belong to other ranks).  A row whose target lies outside [0, vocab_size) is
  * not trained on.  Per row (any of lse, target, loss may be NULL; 32 bits):
- *   lse     log of the sum of exp(logits): -inf where every logit is -inf
+ *   lse     log of the sum of exp(logits): -inf where every logit is -inf, NaN where the row has a NaN or +inf
  *   target  the target's logit; 0 where it is not held here or the row is not trained on
  *   loss    lse - target, before lse is rounded; 0 for a row not trained on, +inf where the target's logit is -inf,
  *           NaN where the row has a NaN or +inf (whole vocabulary only)
@@ -115,6 +115,8 @@ int echo_cross_entropy(const void *logits, int64_t logits_stride, int32_t type, 
 /*
  * grad = (exp(logits - lse) - [v = target]) * grad_loss for the columns held here, lse [rows] that of
  * the whole vocabulary.  Rows not trained on and rows with lse = -inf get zeros.  grad may be logits itself.
+ * lse is taken as it is given: in a row masked throughout with a value so low that the logarithm is below lse's last place,
+ * the probabilities are those of that rounded lse (echo_cross_entropy's own gradient has the maximum and the sum).
  */
 int echo_cross_entropy_grad(const void *logits, int64_t logits_stride, int32_t type, const void *targets,
                             int32_t index_type, int64_t rows, int64_t cols, int64_t vocab_start, int64_t vocab_size,

@@ -88,7 +88,8 @@ int embed_chunk(int64_t rows, int64_t cols) {
 // place the tokens in order.  A lane's place among those of its 64 tokens with the same row follows from six
 // ballots, one for each bit of the row's number in the workgroup.  No scan over workgroups and no atomics whose
 // order matters: one launch sorts.  A lane reads LOADS ids at a time, and a share of as many only once.
-// Latency bounds it: 512 tokens over 512 workgroups take 4.2 us, 16384 over 128 workgroups 14.9 us.
+// Latency bounds it: 512 tokens over 512 workgroups take 4.1 us, 16384 over 128 workgroups 14.9 us.  Many tokens and a large
+// table together are bound by the workgroups all reading every id: 2^20 tokens over 4096 workgroups some 5 ms.
 constexpr int kSortWaves = 16;
 template <class I, int LOADS>
 __global__ __launch_bounds__(kSortWaves * kWave) void k_embed_sort(EmbedGradArgs a, EmbedSpace ws, int bits) {

@@ -20,7 +20,7 @@ __device__ __forceinline__ LossRow loss_row(const LossArgs &a, int64_t row) {
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 
 // exp(l - base) * scale - [column = target] * g for the columns col .. col + N - 1.  The target is looked for once a piece:
-// with a comparison an element 2048 x 51200 took 107.2 us instead of 103.6.
+// with a comparison an element a pass of 2048 x 51200 took 107.2 us instead of 103.6 (79.4 now, for the reason at k_loss).
 template <int N>
 __device__ __forceinline__ F<N> loss_grad(F<N> l, float base, float scale, int col, int at, float g) {
     F<N> d;
@@ -48,10 +48,12 @@ __device__ __forceinline__ float finish_row(const LossArgs &a, int64_t row, cons
 
 // A team a row, which is read once and stays in registers as it came; with a gradient it is written
 // from there.  Each wavefront takes its maximum and its sum of exponentials relative to it; the team joins
-// them with one exchange.  Memory bounds it: 2048 x 51200 of bf16 with its gradient in 65.5 us, 6.4 TB/s.
+// them with one exchange.  Memory bounds it: 2048 x 51200 of bf16 with its gradient takes 65.5 us, 6.4 TB/s, on logits that
+// the 256 MB cache still has, and 79.4 a pass on new ones, 5.3 TB/s.  Without a gradient the workgroups of a launch read
+// together and reduce together: 512 x 25600 in 9.6 us, 2.7 TB/s.
 // Wavefronts a SIMD that a variant's registers have to leave room for: two workgroups of 16 wavefronts on a compute unit, one
 // reading while the other computes or writes, where the row takes at most half of the 64 registers that each lane then
-// has.  2048 x 51200 of bf16 took 103.6 us with 95 to 128 registers and one workgroup, and takes 77.9.  The
+// has.  A pass of 2048 x 51200 of bf16 took 103.6 us with 95 to 128 registers and one workgroup, and 77.9 with two.  The
 // compiler stays within 64 because each piece's sums are closed before the next piece is converted (the empty asm in the loops).
 template <class T, int THREADS, int E>
 constexpr int kLossWaves = THREADS == 1024 && E * sizeof(T) <= 128 ? 8 : 1;
@@ -113,7 +115,7 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK), (kLossWaves<T, T
 }
 
 // Rows too wide for registers, or of less than a piece: one workgroup a row, read once for a running maximum and sum a lane, and
-// with a gradient once more.
+// with a gradient once more.  2048 x 65544 of bf16: 55.4 us without a gradient, 4.8 TB/s, and 133.6 with one.
 template <class T, class I>
 __global__ __launch_bounds__(kWideBlock) void k_loss_wide(LossArgs a) {
     constexpr int N = kN<T>, STEP = kWideBlock * N;
@@ -163,7 +165,7 @@ __global__ __launch_bounds__(kWideBlock) void k_loss_wide(LossArgs a) {
     }
 }
 
-// The gradient alone, K pieces a lane of one row's stretch of 256 * K pieces: 512 x 25600 of bf16 in 10.3 us, 5.1 TB/s.
+// The gradient alone, K pieces a lane of one row's stretch of 256 * K pieces: 512 x 25600 of bf16 in 10.7 us, 4.9 TB/s.
 constexpr int kGradPieces = 2;
 template <class T, class I>
 __global__ __launch_bounds__(256) void k_loss_grad(LossArgs a) {

@@ -6,7 +6,8 @@ namespace {
 
 // A team a row, which is read once.  The mean and the sum of squares about it are taken per wavefront, both
 // from the registers, and joined over the team's wavefronts (n, mean, squares) in their order, so the team
-// waits for itself once a row.  Memory bounds it: 2048 x 8192 of bf16 with a residual in 22.0 us, 6.1 TB/s; one row takes 2.3 us.
+// waits for itself once a row.  Memory bounds it: 2048 x 8192 of bf16 with a residual in 22.0 us a pass, 6.1 TB/s; one row
+// takes 2.3 us.
 template <class T, class W, int THREADS, int E, bool CUT>
 __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_norm(NormArgs a) {
     using Q = Team<T, THREADS, E, CUT>;
@@ -87,7 +88,7 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_norm(Norm
 }
 
 // Rows too wide for registers (or of less than a piece): one workgroup a row, which is read three times (sum, squares about the
-// mean, result), from the cache after the first.
+// mean, result), from the cache after the first.  2048 x 20480 of bf16 in 34.3 us, 4.9 TB/s.
 template <class T, class W>
 __global__ __launch_bounds__(kWideBlock) void k_norm_wide(NormArgs a) {
     constexpr int N = kN<T>, STEP = kWideBlock * N;
@@ -160,7 +161,8 @@ hipError_t norm(const NormArgs &a, hipStream_t s) {
 // of dweight and dbias in registers, which leaves the chip few wavefronts; so the next row is on its way
 // while one is worked on, where its lanes hold only 8 elements of a row (with 16 the registers of the second
 // row cost more wavefronts than it hides).  A workgroup leaves one row of each weight sum in `part`.
-// 2048 x 12288 of bf16 with a residual's gradient: 39.2 us, 5.1 TB/s, and 5.3 us for the join.
+// 2048 x 12288 of bf16 with a residual's gradient: 39.1 us, 5.1 TB/s, and 5.3 us for the join.  Narrower rows are
+// further from memory's rate (2048 x 4096: 16.0 us, 3.1 TB/s, and 3.9): few wavefronts a SIMD, each waiting for its row.
 template <class T, class W, int THREADS, int E, bool CUT>
 __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_norm_grad(NormGradArgs a) {
     using Q = Team<T, THREADS, E, CUT>;
@@ -275,7 +277,8 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK)) void k_norm_grad
     q.store(p + a.cols, db);
 }
 
-// Rows too wide for that, or of less than a piece: dx, one workgroup a row, read twice.
+// Rows too wide for that, or of less than a piece: dx, one workgroup a row, read twice.  2048 x 16392 of bf16: 44.9 us,
+// after 23.4 for the weights' gradients below, which read x and dy again, and 4.7 for their join.
 template <class T, class W>
 __global__ __launch_bounds__(kWideBlock) void k_norm_dx_wide(NormGradArgs a) {
     constexpr int N = kN<T>, STEP = kWideBlock * N;
@@ -378,8 +381,8 @@ hipError_t norm_grad_rows(const NormGradArgs &a, hipStream_t s) {
     } else {
         if (whole <= 1024 * 8) return run(k_norm_grad<T, W, 1024, 8, CUT>, 1024);
         if (whole <= 768 * 16) return run(k_norm_grad<T, W, 768, 16, CUT>, 768);
-        // 2048 x 16384: 45.5 us of bf16 with 16 wavefronts and 49.1 with 8; of f32, whose rows do not fit the registers that
-        // 16 wavefronts leave a lane, 110.3 and 95.5
+        // 2048 x 16384: 45.5 us of bf16 with 16 wavefronts and 49.1 with 8; of f32 110.3 and 95.5.  An f32 row fits the
+        // registers of neither: with 8 wavefronts a lane has 256 and spills 115 (80 bytes of scratch), with 16 it has 128
         if constexpr (sizeof(T) == 2)
             return run(k_norm_grad<T, W, 1024, 16, CUT>, 1024);
         else

