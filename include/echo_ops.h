@@ -2,9 +2,9 @@
  * echo_ops.h -- C ABI of the training-step operators of libecho.so.
  *
  * The composer (echo.h) plans training jobs from the durations of their operators.  These are the
- * operators that a pipeline stage of such a job runs outside its matrix products -- embedding lookup,
- * layer norm, cross entropy, and their gradients -- so that their durations, and what they compute,
- * can be had on the GPU at hand.
+ * operators that a pipeline stage of such a job runs outside its layers' matrix products -- embedding lookup,
+ * layer norm, cross entropy, distillation, the output head with either loss, and their gradients -- so that
+ * their durations, and what they compute, can be had on the GPU at hand.
  *
  * Conventions, besides those of echo.h (return codes, echo_last_error, asynchronous work on the
  * caller's stream, nothing throws):
@@ -122,6 +122,86 @@ int echo_cross_entropy_grad(const void *logits, int64_t logits_stride, int32_t t
                             int32_t index_type, int64_t rows, int64_t cols, int64_t vocab_start, int64_t vocab_size,
                             const float *lse, const float *grad_loss, void *grad, int64_t grad_stride,
                             int hip_device, void *hip_stream);
+
+/*
+ * Distillation of rows of logits over the ids [vocab_start, vocab_start + cols) of a vocabulary of vocab_size ids from a
+ * teacher's top logits: `top` ids a row and their logits, ids [rows][top] and teacher [rows][top] of teacher_type (`type` or
+ * ECHO_F32), 1 <= top <= 1024.  Ids outside [0, vocab_size) are padding, and an id may come more than once (its masses add
+ * up).  With T the temperature (1e-6 to 1e6), q the softmax of teacher / T over the row's ids in the vocabulary and p that of
+ * logits / T over the vocabulary, per row (any of lse, target, entropy, loss may be NULL; 32 bits):
+ *   lse      log of the sum of exp(logits / T): -inf where every logit is -inf, NaN where the row has a NaN or +inf
+ *   target   sum of q * logit / T over the ids held here
+ *   entropy  -sum of q log q over all ids of the row
+ *   loss     T^2 * sum of q (log q - log p); 0 for a row without an id whose logit is above -inf, which is not trained on, +inf
+ *            where q is not 0 and the logit is -inf (whole vocabulary only)
+ *   grad     T (p - q) * grad_loss[row], [rows][cols] of `type` (whole vocabulary only), in the same pass.  Rows not
+ *            trained on and rows without a finite logit get zeros.  May be logits itself.
+ * For a vocabulary over several ranks, every rank is given all of a row's ids; the whole lse is log(sum over ranks of
+ * exp(lse)), loss = T^2 * (lse - sum over ranks of target - entropy), and echo_distillation_grad gives each rank its gradient.
+ */
+int echo_distillation(const void *logits, int64_t logits_stride, int32_t type, const void *ids, int32_t index_type,
+                      const void *teacher, int32_t teacher_type, int64_t rows, int64_t cols, int64_t top,
+                      int64_t vocab_start, int64_t vocab_size, float temperature, float *lse, float *target,
+                      float *entropy, float *loss, const float *grad_loss, void *grad, int64_t grad_stride,
+                      int hip_device, void *hip_stream);
+
+/*
+ * grad = T (exp(logits / T - lse) - q) * grad_loss for the columns held here, lse [rows] that of the whole vocabulary, taken as
+ * it is given.  Rows not trained on and rows with lse = -inf get zeros.  grad may be logits itself.
+ */
+int echo_distillation_grad(const void *logits, int64_t logits_stride, int32_t type, const void *ids, int32_t index_type,
+                           const void *teacher, int32_t teacher_type, int64_t rows, int64_t cols, int64_t top,
+                           int64_t vocab_start, int64_t vocab_size, float temperature, const float *lse,
+                           const float *grad_loss, void *grad, int64_t grad_stride, int hip_device, void *hip_stream);
+
+/*
+ * The same losses straight from hidden states [rows][cols] and an output table, `vocab` rows of cols elements for the ids
+ * [vocab_start, vocab_start + vocab): logits = hidden weight^T, which are not kept.  hidden and weight are of `type`; the
+ * products are of 16-bit elements (three of them for one of 32 bits) with sums in 32 bits, and logits, statistics and losses
+ * are in 32 bits.  Gradients (both or neither), of the loss sum over rows of grad_loss * loss, with d the logits'
+ * gradient of above:
+ *   dhidden = d weight, [rows][cols] of `type`;   dweight = d^T hidden, [vocab][cols] of grad_type (`type` or ECHO_F32),
+ *   written, or with accumulate != 0 added to.
+ * Of 16-bit types d is rounded to `type` (relative to the largest |grad_loss|) before these products, as the logits'
+ * gradient of echo_cross_entropy is; of 32 bits it is not.  Rows not trained on have d = 0.  A row whose hidden state has a NaN or
+ * an infinity gives NaN to every row of dweight, trained on or not.
+ * echo_linear_cross_entropy gives loss and gradients with the whole vocabulary, or a shard's lse and target;
+ * echo_linear_cross_entropy_grad is given the whole vocabulary's lse.  The distillations are their counterparts.
+ * rows, vocab <= 2^24, cols <= 2^20, and the product of any two <= 2^38 (else ECHO_ERR_RANGE).
+ * workspace: at least echo_linear_workspace(...) bytes for the same matrices, aligned to 16; top is 0 for the cross entropies,
+ * loss and grads say which of the two the call computes.  It holds at most about 1 GiB of the logits' gradient at a time, besides
+ * 32-bit sums of dhidden, and copies of matrices that the products do not take as they are: those of 32 bits, and those whose cols
+ * are no multiple of 64, whose rows do not begin at multiples of 16 bytes or whose stride passes 2^22.
+ */
+int64_t echo_linear_workspace(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                              int32_t type, int64_t rows, int64_t cols, int64_t vocab, int64_t top, int32_t loss,
+                              int32_t grads);
+int echo_linear_cross_entropy(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                              int32_t type, const void *targets, int32_t index_type, int64_t rows, int64_t cols,
+                              int64_t vocab, int64_t vocab_start, int64_t vocab_size, float *lse, float *target,
+                              float *loss, const float *grad_loss, void *dhidden, void *dweight, int32_t grad_type,
+                              int32_t accumulate, void *workspace, int64_t workspace_bytes, int hip_device,
+                              void *hip_stream);
+int echo_linear_cross_entropy_grad(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                                   int32_t type, const void *targets, int32_t index_type, int64_t rows, int64_t cols,
+                                   int64_t vocab, int64_t vocab_start, int64_t vocab_size, const float *lse,
+                                   const float *grad_loss, void *dhidden, void *dweight, int32_t grad_type,
+                                   int32_t accumulate, void *workspace, int64_t workspace_bytes, int hip_device,
+                                   void *hip_stream);
+int echo_linear_distillation(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                             int32_t type, const void *ids, int32_t index_type, const void *teacher,
+                             int32_t teacher_type, int64_t rows, int64_t cols, int64_t vocab, int64_t top,
+                             int64_t vocab_start, int64_t vocab_size, float temperature, float *lse, float *target,
+                             float *entropy, float *loss, const float *grad_loss, void *dhidden, void *dweight,
+                             int32_t grad_type, int32_t accumulate, void *workspace, int64_t workspace_bytes,
+                             int hip_device, void *hip_stream);
+int echo_linear_distillation_grad(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                                  int32_t type, const void *ids, int32_t index_type, const void *teacher,
+                                  int32_t teacher_type, int64_t rows, int64_t cols, int64_t vocab, int64_t top,
+                                  int64_t vocab_start, int64_t vocab_size, float temperature, const float *lse,
+                                  const float *grad_loss, void *dhidden, void *dweight, int32_t grad_type,
+                                  int32_t accumulate, void *workspace, int64_t workspace_bytes, int hip_device,
+                                  void *hip_stream);
 
 #ifdef __cplusplus
 }

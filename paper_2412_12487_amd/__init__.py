@@ -7,13 +7,16 @@
 
 and the operators of the simulated training steps (`ops`, include/echo_ops.h), which need torch:
 
-    layer_norm, layer_norm_grad, embedding, embedding_grad, cross_entropy, cross_entropy_grad
+    layer_norm, layer_norm_grad, embedding, embedding_grad, cross_entropy, cross_entropy_grad, distillation,
+    distillation_grad, linear_cross_entropy, linear_cross_entropy_grad, linear_distillation, linear_distillation_grad
 """
 from .echo import (ECHO_ERR_ARG, ECHO_ERR_CYCLE, ECHO_ERR_DEVICE, ECHO_ERR_HIP, ECHO_ERR_MATCH,
                    ECHO_ERR_NOMEM, ECHO_ERR_RANGE, ECHO_OK, EXPORTS, LIB_PATH, SCENARIO_DTYPE, EchoError,
                    Graph, lib, pack_scenarios, scenarios_to_device)
 
-_OPS = ("layer_norm", "layer_norm_grad", "embedding", "embedding_grad", "cross_entropy", "cross_entropy_grad")
+_OPS = ("layer_norm", "layer_norm_grad", "embedding", "embedding_grad", "cross_entropy", "cross_entropy_grad",
+        "distillation", "distillation_grad", "linear_cross_entropy", "linear_cross_entropy_grad", "linear_distillation",
+        "linear_distillation_grad")
 
 __all__ = ["Graph", "EchoError", "lib", "pack_scenarios", "scenarios_to_device", "SCENARIO_DTYPE",
            "LIB_PATH", "EXPORTS", "ECHO_OK", "ECHO_ERR_ARG", "ECHO_ERR_RANGE", "ECHO_ERR_MATCH",

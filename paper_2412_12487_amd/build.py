@@ -20,7 +20,8 @@ DEVICE_FLAGS = ["--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-I", INCLUDE, "-I", CSRC]
 
 
-SOURCES = ("echo_kernels.hip", "echo_norm.hip", "echo_embed.hip", "echo_loss.hip", "echo_host.cpp", "echo_ops_host.cpp")
+SOURCES = ("echo_kernels.hip", "echo_norm.hip", "echo_embed.hip", "echo_loss.hip", "echo_distill.hip", "echo_linear.hip",
+           "echo_linear_grad.hip", "echo_host.cpp", "echo_ops_host.cpp")
 
 
 def _run(cmds, verbose):

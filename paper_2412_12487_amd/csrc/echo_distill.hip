@@ -1,0 +1,320 @@
+// echo_distill.hip -- distillation from a teacher's top logits over a vocabulary or a shard of one, on gfx950.
+//
+// Per row, at temperature T: q = softmax of the teacher's logits / T over its ids in the vocabulary, p = softmax of the
+// logits / T over the vocabulary, loss = T^2 sum q (log q - log p), and the logits' gradient T (p - q) grad_loss.
+#include "echo_ops_device.h"
+
+namespace echo {
+namespace {
+
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+
+// An entry of the teacher: its column here (or -1), the mass of its id, which the first entry of an id holds, and the
+// logit of it / T.  One wavefront prepares a row's entries, and each lane reads again only what it wrote itself.
+struct Entry {
+    int at;
+    float mass, x;
+};
+struct Teacher {
+    bool trained;      // an id of the vocabulary has a mass
+    float prior;       // sum of q log q
+};
+template <class T, class I, class Z>
+__device__ __forceinline__ Teacher teacher_of(const DistillArgs &a, int64_t row, float inv_t, int first, int cols, Entry *entries) {
+    const int lane = threadIdx.x % kWave;
+    const I *ids = static_cast<const I *>(a.ids) + row * a.top;
+    const Z *z = static_cast<const Z *>(a.teacher) + row * a.top;
+    const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
+    const auto logit = [&](int k) {
+        const int64_t id = (int64_t)ids[k];
+        return id >= 0 && id < a.vocab_size ? (float)z[k] * inv_t : -kInf;
+    };
+    float top = -kInf, sum = 0.0f, prior = 0.0f;
+    for (int k = lane; k < a.top; k += kWave) top = fmaxf(top, logit(k));
+    top = wave_max(top);
+    const float base = top == -kInf ? 0.0f : top;
+    for (int k = lane; k < a.top; k += kWave) sum += expf(logit(k) - base);
+    sum = wave_sum(sum);
+    const bool live = sum != 0.0f;      // NaN too
+    const float log_sum = logf(sum);
+    for (int k = lane; k < a.top; k += kWave) {
+        const int64_t id = (int64_t)ids[k];
+        const float d = logit(k) - base, q = live ? expf(d) / sum : 0.0f;
+        if (q != 0.0f) prior += q * (d - log_sum);
+        int at = q != 0.0f ? shard_row(id, a.vocab_start, a.cols) : -1;
+        if (at >= 0 && (unsigned)(at - first) >= (unsigned)cols) at = -1;
+        float mass = 0.0f;
+        if (at >= 0) {
+            for (int o = 0; o < a.top; ++o) {
+                if ((int64_t)ids[o] != id) continue;
+                const float more = expf(logit(o) - base) / sum;
+                if (o < k && more != 0.0f) at = -1;
+                mass += more;
+            }
+        }
+        entries[k] = Entry{at, at >= 0 ? mass : 0.0f, at >= 0 ? (float)l[at] * inv_t : 0.0f};
+    }
+    return Teacher{live, wave_sum(prior)};
+}
+// The entries' share of the loss's cross term, of logits taken from `from` on.
+__device__ __forceinline__ float cross_of(const Entry *entries, int top, float from) {
+    float cross = 0.0f;
+    for (int k = threadIdx.x % kWave; k < top; k += kWave) {
+        const Entry e = entries[k];
+        if (e.at >= 0) cross += e.mass * (e.x - from);
+    }
+    return wave_sum(cross);
+}
+// The gradient where the teacher has a mass, over what its row has there.
+template <class T>
+__device__ __forceinline__ void put_entries(T *grad, const Entry *entries, int top, float base, float scale, float g) {
+    for (int k = threadIdx.x % kWave; k < top; k += kWave) {
+        const Entry e = entries[k];
+        if (e.at >= 0) grad[e.at] = (T)(exp_of(e.x - base) * scale - e.mass * g);
+    }
+}
+__device__ __forceinline__ float finish_row(const DistillArgs &a, int64_t row, const Teacher &t, const Entry *entries, float top, float sum) {
+    const float more = logf(sum), lse = top == -kInf ? -kInf : top + more;
+    const float cross = cross_of(entries, a.top, a.loss && lse != -kInf ? top : 0.0f);
+    if (threadIdx.x % kWave == 0) {
+        if (a.lse) a.lse[row] = lse;
+        if (a.target) a.target[row] = cross;
+        if (a.entropy) a.entropy[row] = -t.prior;
+        if (a.loss)
+            a.loss[row] = !t.trained ? 0.0f : lse == -kInf ? kInf : a.temperature * a.temperature * (t.prior - cross + more);
+    }
+    return lse;
+}
+// Stores that are already on their way are behind this: what the whole team wrote is where later stores find it.
+template <int WAVES>
+__device__ __forceinline__ void settled() {
+    __threadfence_block();
+    if constexpr (WAVES > 1) __syncthreads();
+    else __builtin_amdgcn_s_waitcnt(0);
+}
+
+// A team a row, as in cross entropy: the row is read once and its gradient written from registers.  The gradient is then
+// written over at the teacher's ids.
+template <class T, int THREADS, int E>
+constexpr int kDistillWaves = THREADS == 1024 && E * sizeof(T) <= 128 ? 8 : 1;
+template <class T, class I, class Z, int THREADS, int E, bool CUT>
+__global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK), (kDistillWaves<T, THREADS, E>)) void k_distill(DistillArgs a) {
+    using Q = Team<T, THREADS, E, CUT>;
+    constexpr int N = Q::N, P = Q::P;
+    const Q q(a.cols);
+    extern __shared__ __attribute__((aligned(16))) char space[];
+    Entry *entries = reinterpret_cast<Entry *>(space) + q.team * a.top;
+    __shared__ float4 lds[2][Q::WAVES];
+    const float inv_t = 1.0f / a.temperature;
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * Q::TEAMS + q.team; row < a.rows; row += (int64_t)gridDim.x * Q::TEAMS) {
+        const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
+        V<T, N> x[P];
+        q.load(l, x, T(-kInf));
+        Teacher t{};
+        if (q.wave == 0) t = teacher_of<T, I, Z>(a, row, inv_t, 0, a.cols, entries);
+        float top = -kInf, sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const F<N> f = widen<T, N>(x[k]);
+#pragma unroll
+            for (int j = 0; j < N; ++j) top = fmaxf(top, f[j] * inv_t);
+            if constexpr (kDistillWaves<T, THREADS, E> > 1) asm volatile("" : "+v"(top));
+        }
+        forget<T, N, P>(x);
+        top = wave_max(top);
+        const float base = top == -kInf ? 0.0f : top;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const F<N> f = widen<T, N>(x[k]);
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum += exp_of(f[j] * inv_t - base);
+            if constexpr (kDistillWaves<T, THREADS, E> > 1) asm volatile("" : "+v"(sum));
+        }
+        forget<T, N, P>(x);
+        sum = wave_sum(sum);
+        bool trained = t.trained;
+        if constexpr (Q::WAVES > 1) {
+            if (q.lane % kWave == 0) lds[turn][q.wave] = make_float4(top, sum, t.trained ? 1.0f : 0.0f, 0.0f);
+            __syncthreads();      // also: the teacher's logits have been read, and grad may be logits
+            const float4 p = lds[turn][q.lane % Q::WAVES];
+            top = ring_max<Q::WAVES>(p.x);
+            sum = ring_sum<Q::WAVES>(p.x == -kInf ? p.y : p.y * exp_of(p.x - top));
+            trained = ring_sum<Q::WAVES>(p.z) > 0.0f;      // the first wavefront's
+            turn ^= 1;
+        }
+        if (sum != sum) top = sum;      // a row of NaN alone has no maximum but a sum
+        float lse = top == -kInf ? -kInf : 0.0f;
+        if (q.wave == 0) finish_row(a, row, t, entries, top, sum);
+        if (!a.grad) continue;
+        const bool live = trained && lse != -kInf;
+        const float g = a.grad_loss[row] * a.temperature, scale = g / sum;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            F<N> f = 0.0f;
+            if (live) {
+                f = widen<T, N>(x[k]);
+#pragma unroll
+                for (int j = 0; j < N; ++j) f[j] = exp_of(f[j] * inv_t - top) * scale;
+            }
+            x[k] = round_to<T, N>(f);
+            if constexpr (kDistillWaves<T, THREADS, E> > 1) forget<T, N, 1>(reinterpret_cast<V<T, N>(&)[1]>(x[k]));
+        }
+        T *d = static_cast<T *>(a.grad) + row * a.grad_stride;
+        q.drop(d, x);
+        settled<Q::WAVES>();
+        if (q.wave == 0 && live) put_entries(d, entries, a.top, top, scale, g);
+    }
+}
+
+// Rows too wide for registers, or of less than a piece: read once for the statistics and once more for the gradient.
+template <class T, class I, class Z>
+__global__ __launch_bounds__(kWideBlock) void k_distill_wide(DistillArgs a) {
+    constexpr int N = kN<T>, STEP = kWideBlock * N;
+    extern __shared__ __attribute__((aligned(16))) char space[];
+    Entry *entries = reinterpret_cast<Entry *>(space);
+    __shared__ float4 lds[kWideWaves];
+    const float inv_t = 1.0f / a.temperature;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
+        Teacher t{};
+        if (threadIdx.x < kWave) t = teacher_of<T, I, Z>(a, row, inv_t, 0, a.cols, entries);
+        float top = -kInf, sum = 0.0f;
+#pragma unroll 4
+        for (int c = threadIdx.x * N; c < a.cols; c += STEP) {
+            const F<N> f = widen<T, N>(load<N>(l, c, a.cols, T(-kInf)));
+            float m = top;
+#pragma unroll
+            for (int j = 0; j < N; ++j) m = fmaxf(m, f[j] * inv_t);
+            const float base = m == -kInf ? 0.0f : m;
+            sum *= top == -kInf ? 1.0f : exp_of(top - base);
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum += exp_of(f[j] * inv_t - base);
+            top = m;
+        }
+        const float mine = top;
+        top = wave_max(top);
+        sum = wave_sum(mine == -kInf ? sum : sum * exp_of(mine - top));
+        __syncthreads();      // the last row's readers are done
+        if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = make_float4(top, sum, t.trained ? 1.0f : 0.0f, 0.0f);
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < kWideWaves; ++v) top = fmaxf(top, lds[v].x);
+        sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < kWideWaves; ++v) {
+            const float4 p = lds[v];
+            sum += p.x == -kInf ? p.y : p.y * exp_of(p.x - top);
+        }
+        const bool live = lds[0].z > 0.0f && (top != -kInf || sum != sum);
+        if (sum != sum) top = sum;
+        if (threadIdx.x < kWave) finish_row(a, row, t, entries, top, sum);
+        if (!a.grad) continue;
+        T *d = static_cast<T *>(a.grad) + row * a.grad_stride;
+        const float g = a.grad_loss[row] * a.temperature, scale = g / sum;
+        for (int c = threadIdx.x * N; c < a.cols; c += STEP) {
+            F<N> f = 0.0f;
+            if (live) {
+                f = widen<T, N>(load<N>(l, c, a.cols));
+#pragma unroll
+                for (int j = 0; j < N; ++j) f[j] = exp_of(f[j] * inv_t - top) * scale;
+            }
+            store<N>(d, c, a.cols, round_to<T, N>(f));
+        }
+        settled<kWideWaves>();
+        if (threadIdx.x < kWave && live) put_entries(d, entries, a.top, top, scale, g);
+    }
+}
+
+// The gradient alone, from the whole vocabulary's lse: a workgroup takes a stretch of one row, and the teacher's entries in it.
+constexpr int kGradPieces = 4;
+template <class T, class I, class Z>
+__global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
+    constexpr int N = kN<T>, K = kGradPieces, SPAN = K * 256 * N;
+    extern __shared__ __attribute__((aligned(16))) char space[];
+    Entry *entries = reinterpret_cast<Entry *>(space);
+    __shared__ int lds;
+    const float inv_t = 1.0f / a.temperature;
+    const int spans = (a.cols + SPAN - 1) / SPAN;
+    const int64_t n = a.rows * spans;
+    for (int64_t id = blockIdx.x; id < n; id += gridDim.x) {
+        const int64_t row = id / spans;
+        const int first = (int)(id - row * spans) * SPAN, from = first + threadIdx.x * N;
+        const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
+        T *d = static_cast<T *>(a.grad) + row * a.grad_stride;
+        V<T, N> raw[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            raw[k] = T(0);
+            if (from + k * 256 * N < a.cols) raw[k] = load<N>(l, from + k * 256 * N, a.cols);
+        }
+        if (threadIdx.x < kWave) {
+            const Teacher t = teacher_of<T, I, Z>(a, row, inv_t, first, SPAN, entries);
+            if (threadIdx.x == 0) lds = t.trained;
+        }
+        __syncthreads();      // also: the teacher's logits have been read
+        const float lse = a.lse_in[row], g = a.grad_loss[row] * a.temperature;
+        const bool live = lds && lse != -kInf;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = from + k * 256 * N;
+            if (c >= a.cols) continue;
+            F<N> f = 0.0f;
+            if (live) {
+                f = widen<T, N>(raw[k]);
+#pragma unroll
+                for (int j = 0; j < N; ++j) f[j] = exp_of(f[j] * inv_t - lse) * g;
+            }
+            drop<N>(d, c, a.cols, round_to<T, N>(f));
+        }
+        settled<4>();
+        if (threadIdx.x < kWave && live) put_entries(d, entries, a.top, lse, g, g);
+    }
+}
+
+template <class A>
+hipError_t launch_with(void (*kernel)(A), unsigned grid, int block, size_t lds, hipStream_t s, A a) {
+    void *args[] = {&a};
+    return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3(grid), dim3(block), args, lds, s);
+}
+template <class T, class I, class Z, bool CUT>
+hipError_t distill(const DistillArgs &a, hipStream_t s) {
+    const size_t each = sizeof(Entry) * a.top;
+    const auto run = [&](auto kernel, int threads) {
+        const int teams = threads < 256 ? 256 / threads : 1;
+        return launch_with(kernel, grid_of((a.rows + teams - 1) / teams), threads * teams, each * teams, s, a);
+    };
+    if (a.cols < kN<T> || a.cols > 1024 * 64)
+        return launch_with(k_distill_wide<T, I, Z>, grid_of(a.rows), kWideBlock, each, s, a);
+    if (a.cols <= 64 * 32) return run(k_distill<T, I, Z, 64, 32, CUT>, 64);
+    if (a.cols <= 256 * 32) return run(k_distill<T, I, Z, 256, 32, CUT>, 256);
+    if (a.cols <= 1024 * 32) return run(k_distill<T, I, Z, 1024, 32, CUT>, 1024);
+    return run(k_distill<T, I, Z, 1024, 64, CUT>, 1024);
+}
+template <class T, class I, class Z>
+hipError_t distill(const DistillArgs &a, hipStream_t s) {
+    if (a.lse_in) {
+        constexpr int SPAN = kGradPieces * 256 * kN<T>;
+        return launch_with(k_distill_grad<T, I, Z>, grid_of(a.rows * ((a.cols + SPAN - 1) / SPAN)), 256, sizeof(Entry) * a.top, s, a);
+    }
+    return a.cols % kN<T> ? distill<T, I, Z, true>(a, s) : distill<T, I, Z, false>(a, s);
+}
+template <class T>
+hipError_t distill(const DistillArgs &a, int index_type, int teacher_type, hipStream_t s) {
+    // the teacher's logits are the student's type or 32 bits
+    if (teacher_type == ECHO_F32)
+        return index_type == ECHO_I64 ? distill<T, int64_t, float>(a, s) : distill<T, int32_t, float>(a, s);
+    return index_type == ECHO_I64 ? distill<T, int64_t, T>(a, s) : distill<T, int32_t, T>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_distill(const DistillArgs &a, int type, int index_type, int teacher_type, hipStream_t s) {
+    switch (type) {
+        case ECHO_F32: return distill<float>(a, index_type, teacher_type, s);
+        case ECHO_F16: return distill<f16>(a, index_type, teacher_type, s);
+        default: return distill<bf16>(a, index_type, teacher_type, s);
+    }
+}
+
+}  // namespace echo

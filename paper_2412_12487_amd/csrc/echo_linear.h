@@ -1,0 +1,89 @@
+// echo_linear.h -- arguments of the output head's kernels and the tiles that they come in.
+#pragma once
+
+#include "echo_product.h"
+
+namespace echo {
+
+struct HeadArgs {
+    Product m;                    // a: the table's rows, b: the hidden states
+    int rows, vocab;              // rows, and ids held here
+    int first;                    // column that the product's first one is
+    float inv_t;
+    const void *targets;          // one target a row, where top is 0
+    int wide_index, top;
+    int64_t vocab_start, vocab_size;
+    const int *local;             // [rows][top]: an entry's column here, or -1
+    const float *q;               // [rows][top]
+    const float2 *prior;          // [rows]: sum of q log q, and 1 where the row is trained on
+    float2 *stats;                // [tiles][rows]: maximum, and sum relative to it
+    float *hits;                  // logits of the target or of the entries
+    const float *lse, *grad_loss, *scale;
+    char *prob;                   // [planes][prob_rows][prob_cols]
+    int64_t prob_stride, prob_plane;
+    int prob_rows, prob_cols;
+};
+struct JoinArgs {
+    const float2 *stats, *prior;
+    const float *hits, *q;
+    const int *local;
+    const void *targets;
+    int wide_index, top, rows, vocab, tiles;
+    int64_t vocab_start, vocab_size;
+    float square;                 // T^2
+    float *lse, *target, *entropy, *loss;
+};
+struct TeacherArgs {
+    const void *ids, *teacher;
+    int64_t rows, vocab_start, vocab_size;
+    int top, vocab;
+    float inv_t;
+    int *local;
+    float *q;
+    float2 *prior;
+};
+struct LayoutArgs {
+    const void *from;
+    int64_t stride, rows;         // stride in elements
+    int cols, width;
+    char *to;
+    int64_t plane;
+};
+// D of a product, or a part's share of it, times what the head's gradient is relative to.
+struct OutArgs {
+    Product m;
+    const float *scale;
+    float factor;
+    float *parts;                 // [splits][nj][ni] of 32 bits, or null: D is whole
+    bool add_parts;               // parts are added to
+    void *out;                    // [nj][ni]
+    bool accumulate;
+};
+struct GatherArgs {
+    const float *parts;
+    int64_t n;                    // elements of a part
+    int splits;
+    const float *scale;
+    float factor;
+    void *out;
+};
+
+namespace {
+// Shapes of the tiles.  Wide: 256 x 256 by 8 wavefronts.  Middle: 128 x 128 by 4.  Thin: 256 x 64 by 4, for few rows.
+using Wide = Shape<256, 256, 2, 4>;
+using Middle = Shape<128, 128, 2, 2>;
+using Thin = Shape<256, 64, 4, 1>;
+// Shares of the gradient lie in [-1, 1]; those of half precision are taken 2^14 times as large, since
+// most of a softmax is below its smallest number.
+template <class T>
+constexpr float kUnit = 1.0f;
+template <>
+constexpr float kUnit<f16> = 16384.0f;
+}  // namespace
+
+// deep: b's sum runs along its rows (the hidden states' gradient), or across them (the table's)
+hipError_t launch_out(const OutArgs &a, int type, int out_type, bool deep, int shape, hipStream_t s);
+hipError_t launch_zero(void *out, int64_t bytes, hipStream_t s);
+hipError_t launch_gather(const GatherArgs &a, int type, int out_type, hipStream_t s);
+
+}  // namespace echo

@@ -1,0 +1,532 @@
+// echo_linear.hip -- losses taken straight from hidden states and the output table, on gfx950: the logits' tiles with
+// their statistics or their gradient, and what prepares and joins them.
+#include "echo_linear.h"
+
+namespace echo {
+namespace {
+
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+
+// A row's place in the loss: whether it is trained on, and with one target a row its column here or -1.
+struct Row {
+    bool trained;
+    int at;
+};
+__device__ __forceinline__ Row row_of(const HeadArgs &a, int n) {
+    if (a.top) return Row{a.prior[n].y > 0.0f, -1};
+    const int64_t t = a.wide_index ? id_at<int64_t>(a.targets, n) : id_at<int32_t>(a.targets, n);
+    const bool trained = t >= 0 && t < a.vocab_size;
+    return Row{trained, trained ? shard_row(t, a.vocab_start, a.vocab) : -1};
+}
+
+// The teacher's entries of a tile: a cell of 16 bits for each of its logits, 0 or the entry's number and one more.  Cells of
+// 4 columns side by side are exchanged within a row, so that a wavefront's 16 rows meet different banks.
+template <class S>
+struct Cells {
+    static constexpr int PITCH = S::TI * 2, ROWS = S::BYTES / PITCH < S::TJ ? S::BYTES / PITCH : S::TJ, MASK = S::TI / 16 - 1;
+    static_assert(2 * ROWS >= S::TJ, "two buffers hold the cells");
+    char *t0, *t1;
+    __device__ __forceinline__ char *cell(int j, int i) const {
+        char *t = j < ROWS ? t0 : t1;
+        return t + (j < ROWS ? j : j - ROWS) * PITCH + (((i / 4) ^ ((j & MASK) << 2)) * 8);
+    }
+    // every entry of the rows j0 .. j0 + TJ - 1 whose column is in i0 .. i0 + TI - 1
+    __device__ __forceinline__ void fill(const HeadArgs &a, int i0, int j0) const {
+        __syncthreads();      // the last step has been read
+        typedef __attribute__((ext_vector_type(4))) int I4;
+        for (int c = threadIdx.x * 16; c < ROWS * PITCH; c += S::THREADS * 16) {
+            *reinterpret_cast<I4 *>(t0 + c) = 0;
+            if (ROWS < S::TJ) *reinterpret_cast<I4 *>(t1 + c) = 0;
+        }
+        __syncthreads();
+        const int rows = a.rows - j0 < S::TJ ? a.rows - j0 : S::TJ, n = rows * a.top;
+        const int *local = a.local + (int64_t)j0 * a.top;
+        for (int e = threadIdx.x; e < n; e += S::THREADS) {
+            const unsigned i = (unsigned)(local[e] - i0);       // -1 where there is none
+            if (i < (unsigned)S::TI && local[e] >= 0) {
+                const int j = e / a.top;
+                *reinterpret_cast<unsigned short *>(cell(j, i) + (i % 4) * 2) = (unsigned short)(e - j * a.top + 1);
+            }
+        }
+        __syncthreads();
+    }
+};
+
+// Tiles of logits, i over the vocabulary and j over the rows.
+//   GRAD false: each row's maximum and sum of exponentials over the tile's columns, and the logits of its target or entries.
+//   GRAD true: the gradient's share of each logit, (exp(x / T - lse) - q) * grad_loss / scale, rounded to T.
+template <class T, class S, bool GRAD, int PLANES>
+__global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArgs a) {
+    __shared__ __attribute__((aligned(16))) char t0[S::BYTES];
+    __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
+    const Place at = place_of(a.m);
+    F4 acc[S::BI][S::BJ];
+    multiply<T, true, true, S>(a.m, at, t0, t1, acc);
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wi = wave / S::WJ, wj = wave % S::WJ;
+    const int i0 = at.ti * S::TI, j0 = at.tj * S::TJ, il = wi * S::BI * 16 + (lane / 16) * 4, jl = wj * S::BJ * 16 + lane % 16;
+    const Cells<S> cells{t0, t1};
+    if (a.top) cells.fill(a, a.first + i0, j0);
+    using Quad = __attribute__((ext_vector_type(4))) unsigned short;
+    if constexpr (!GRAD) {
+        float2 mine[S::BJ];
+#pragma unroll
+        for (int b = 0; b < S::BJ; ++b) {
+            const int n = j0 + jl + b * 16;
+            const bool live = n < a.rows;
+            const int hit = live && !a.top ? row_of(a, n).at : -1;
+            float top = -kInf;
+#pragma unroll
+            for (int k = 0; k < S::BI; ++k) {
+                const int i = il + k * 16, v = i0 + i;
+                Quad entry = 0;
+                if (a.top) entry = *reinterpret_cast<const Quad *>(cells.cell(jl + b * 16, i));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = v + e < a.m.ni ? acc[k][b][e] * a.inv_t : -kInf;
+                    acc[k][b][e] = x;
+                    if (a.top) {
+                        if (live && entry[e]) a.hits[(int64_t)n * a.top + entry[e] - 1] = x;
+                    } else if (v + e == hit) {
+                        a.hits[n] = x;
+                    }
+                    top = fmaxf(top, x);
+                }
+            }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float base = top == -kInf ? 0.0f : top;
+            float sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < S::BI; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += exp_of(acc[k][b][e] - base);
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            mine[b] = make_float2(top, sum);
+        }
+        __syncthreads();
+        float2 *part = reinterpret_cast<float2 *>(t0);      // [WI][TJ]
+#pragma unroll
+        for (int b = 0; b < S::BJ; ++b)
+            if (lane < 16) part[wi * S::TJ + jl + b * 16] = mine[b];
+        __syncthreads();
+        for (int j = threadIdx.x; j < S::TJ; j += S::THREADS) {
+            if (j0 + j >= a.rows) continue;
+            float top = -kInf, sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < S::WI; ++w) top = fmaxf(top, part[w * S::TJ + j].x);
+#pragma unroll
+            for (int w = 0; w < S::WI; ++w) {
+                const float2 p = part[w * S::TJ + j];
+                sum += p.x == -kInf ? p.y : p.y * exp_of(p.x - top);      // p.y is 0 there, or NaN
+            }
+            a.stats[(int64_t)at.ti * a.rows + j0 + j] = make_float2(top, sum);
+        }
+    } else {
+        const float scale = *a.scale;
+#pragma unroll
+        for (int b = 0; b < S::BJ; ++b) {
+            const int n = j0 + jl + b * 16;
+            bool live = n < a.rows;
+            int hit = -1;
+            float lse = 0.0f, g = 0.0f;
+            if (live) {
+                const Row r = row_of(a, n);
+                hit = r.at - a.first;
+                if (r.at < 0) hit = -1;
+                lse = a.lse[n];
+                live = r.trained && lse != -kInf;
+                g = a.grad_loss[n] / scale * kUnit<T>;
+            }
+            if (n >= a.prob_rows) continue;
+#pragma unroll
+            for (int k = 0; k < S::BI; ++k) {
+                const int i = il + k * 16, v = i0 + i;
+                if (v >= a.prob_cols) continue;
+                Quad entry = 0;
+                if (a.top) entry = *reinterpret_cast<const Quad *>(cells.cell(jl + b * 16, i));
+                F4 d;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float p = exp_of(acc[k][b][e] * a.inv_t - lse);
+                    if (a.top) {
+                        if (live && entry[e]) p -= a.q[(int64_t)n * a.top + entry[e] - 1];
+                    } else if (v + e == hit) {
+                        p -= 1.0f;
+                    }
+                    d[e] = live && v + e < a.m.ni ? p * g : 0.0f;
+                }
+                char *out = a.prob + n * a.prob_stride + v * 2;
+                typedef __attribute__((ext_vector_type(4))) T T4;
+#pragma unroll
+                for (int plane = 0; plane < PLANES; ++plane) {
+                    const T4 h = __builtin_convertvector(d, T4);
+                    *reinterpret_cast<T4 *>(out + plane * a.prob_plane) = h;
+                    if (plane + 1 < PLANES) d -= __builtin_convertvector(h, F4);
+                }
+            }
+        }
+    }
+}
+
+// Joins the tiles' statistics of 16 rows: lanes of 16 over the rows, 64 over the tiles.
+__global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
+    __shared__ float2 part[64][17];
+    const int r = threadIdx.x % 16, w = threadIdx.x / 16;
+    const int n = blockIdx.x * 16 + r;
+    float top = -kInf, sum = 0.0f;
+    if (n < a.rows) {
+        for (int t = w; t < a.tiles; t += 64) {
+            const float2 p = a.stats[(int64_t)t * a.rows + n];
+            const float m = fmaxf(top, p.x);
+            sum = (top == -kInf ? sum : sum * exp_of(top - m)) + (p.x == -kInf ? p.y : p.y * exp_of(p.x - m));
+            top = m;
+        }
+    }
+    part[w][r] = make_float2(top, sum);
+    for (int by = 32; by; by /= 2) {
+        __syncthreads();
+        if (w < by) {
+            const float2 p = part[w][r], o = part[w + by][r];
+            const float m = fmaxf(p.x, o.x);
+            part[w][r] = make_float2(m, (p.x == -kInf ? p.y : p.y * exp_of(p.x - m)) + (o.x == -kInf ? o.y : o.y * exp_of(o.x - m)));
+        }
+    }
+    __syncthreads();
+    if (w || n >= a.rows) return;
+    top = part[0][r].x;
+    sum = part[0][r].y;
+    if (sum != sum) top = sum;      // a row of NaN alone has no maximum but a sum
+    const float more = logf(sum), lse = top == -kInf ? -kInf : top + more;
+    if (a.lse) a.lse[n] = lse;
+    if (!a.top) {
+        const int64_t t = a.wide_index ? id_at<int64_t>(a.targets, n) : id_at<int32_t>(a.targets, n);
+        const bool trained = t >= 0 && t < a.vocab_size;
+        const float hit = trained && shard_row(t, a.vocab_start, a.vocab) >= 0 ? a.hits[n] : 0.0f;
+        if (a.target) a.target[n] = hit;
+        if (a.loss) a.loss[n] = !trained ? 0.0f : lse == -kInf ? kInf : (top - hit) + more;
+        return;
+    }
+    const float2 prior = a.prior[n];
+    const bool trained = prior.y > 0.0f;
+    const float from = a.loss && lse != -kInf ? top : 0.0f;      // the loss takes logits from their maximum on
+    float cross = 0.0f;
+    for (int k = 0; k < a.top; ++k) {
+        const int64_t e = (int64_t)n * a.top + k;
+        const float q = a.q[e];
+        if (a.local[e] >= 0 && q != 0.0f) cross += q * (a.hits[e] - from);
+    }
+    if (a.target) a.target[n] = cross;
+    if (a.entropy) a.entropy[n] = -prior.x;
+    if (a.loss) a.loss[n] = !trained ? 0.0f : lse == -kInf ? kInf : a.square * (prior.x - cross + more);
+}
+
+// The teacher's distribution of a row, a wavefront a row: masses over its ids in the vocabulary, entries of the same id
+// summed in the first of them, and the sum of q log q of the entries as given.
+template <class I, class Z>
+__global__ __launch_bounds__(256) void k_teacher(TeacherArgs a) {
+    const int lane = threadIdx.x % kWave;
+    for (int64_t n = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave; n < a.rows; n += (int64_t)gridDim.x * 4) {
+        const I *ids = static_cast<const I *>(a.ids) + n * a.top;
+        const Z *z = static_cast<const Z *>(a.teacher) + n * a.top;
+        const auto logit = [&](int k) {
+            const int64_t id = (int64_t)ids[k];
+            return id >= 0 && id < a.vocab_size ? (float)z[k] * a.inv_t : -kInf;
+        };
+        float top = -kInf, sum = 0.0f;
+        for (int k = lane; k < a.top; k += kWave) top = fmaxf(top, logit(k));
+        top = wave_max(top);
+        const float base = top == -kInf ? 0.0f : top;
+        for (int k = lane; k < a.top; k += kWave) sum += expf(logit(k) - base);
+        sum = wave_sum(sum);
+        const bool live = sum != 0.0f;      // a row of NaN has a sum
+        const float log_sum = logf(sum);
+        float prior = 0.0f;
+        for (int k = lane; k < a.top; k += kWave) {
+            const int64_t id = (int64_t)ids[k];
+            const float l = logit(k) - base, q = live ? expf(l) / sum : 0.0f;
+            if (q != 0.0f) prior += q * (l - log_sum);
+            float mass = 0.0f;
+            int at = q != 0.0f ? shard_row(id, a.vocab_start, a.vocab) : -1;
+            if (at >= 0) {
+                bool first = true;
+                for (int o = 0; o < a.top; ++o) {
+                    if ((int64_t)ids[o] != id) continue;
+                    const float more = expf(logit(o) - base) / sum;
+                    if (o < k && more != 0.0f) first = false;
+                    mass += more;
+                }
+                if (!first) at = -1;
+            }
+            a.local[n * a.top + k] = at;
+            a.q[n * a.top + k] = at >= 0 ? mass : 0.0f;
+        }
+        prior = wave_sum(prior);
+        if (lane == 0) a.prior[n] = make_float2(prior, live ? 1.0f : sum != sum ? 1.0f : 0.0f);
+    }
+}
+
+// The largest |grad_loss| of the rows, or 1 where that is 0 or not finite: what the gradient's shares are relative to, so that
+// rows of one weight have it exactly.
+__global__ __launch_bounds__(1024) void k_scale(const float *grad_loss, int rows, float *scale) {
+    __shared__ float lds[16];
+    float top = 0.0f;
+    for (int n = threadIdx.x; n < rows; n += 1024) top = fmaxf(top, fabsf(grad_loss[n]));
+    top = wave_max(top);
+    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = top;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < 16; ++w) top = fmaxf(top, lds[w]);
+    *scale = top > 0.0f && top < kInf ? top : 1.0f;
+}
+
+// Rows laid out for the products: PLANES planes of 16 bits, rows filled up with zeros to whole steps.
+template <class U, class T, int PLANES>
+__global__ __launch_bounds__(256) void k_layout(LayoutArgs a) {
+    const int pieces = a.width / 8;
+    const int64_t all = a.rows * pieces;
+    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < all; id += (int64_t)gridDim.x * 256) {
+        const int64_t row = id / pieces;
+        const int c = (int)(id - row * pieces) * 8;
+        const U *from = static_cast<const U *>(a.from) + row * a.stride;
+        F<8> f = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c + j < a.cols) f[j] = (float)from[c + j];
+#pragma unroll
+        for (int plane = 0; plane < PLANES; ++plane) {
+            const V<T, 8> h = round_to<T, 8>(f);
+            *reinterpret_cast<H8<T> *>(a.to + plane * a.plane + (row * a.width + c) * 2) = __builtin_bit_cast(H8<T>, h);
+            if (plane + 1 < PLANES) f -= widen<T, 8>(h);
+        }
+    }
+}
+
+template <class T, bool GRAD, int PLANES>
+hipError_t logits(const HeadArgs &a, int shape, hipStream_t s) {
+    const dim3 grid(a.m.tiles_i * a.m.tiles_j);
+    switch (shape) {
+        case 0: return launch(k_logits<T, Wide, GRAD, PLANES>, grid, dim3(Wide::THREADS), s, a);
+        case 1: return launch(k_logits<T, Middle, GRAD, PLANES>, grid, dim3(Middle::THREADS), s, a);
+        default: return launch(k_logits<T, Thin, GRAD, PLANES>, grid, dim3(Thin::THREADS), s, a);
+    }
+}
+template <class I>
+hipError_t teacher(const TeacherArgs &a, int type, hipStream_t s) {
+    const dim3 grid(grid_of((a.rows + 3) / 4));
+    switch (type) {
+        case ECHO_F32: return launch(k_teacher<I, float>, grid, dim3(256), s, a);
+        case ECHO_F16: return launch(k_teacher<I, f16>, grid, dim3(256), s, a);
+        default: return launch(k_teacher<I, bf16>, grid, dim3(256), s, a);
+    }
+}
+
+hipError_t launch_logits(const HeadArgs &a, int type, bool grad, int shape, hipStream_t s) {
+    if (type == ECHO_F16) return grad ? logits<f16, true, 1>(a, shape, s) : logits<f16, false, 1>(a, shape, s);
+    if (!grad) return logits<bf16, false, 1>(a, shape, s);
+    return type == ECHO_F32 ? logits<bf16, true, 3>(a, shape, s) : logits<bf16, true, 1>(a, shape, s);
+}
+hipError_t launch_join(const JoinArgs &a, hipStream_t s) { return launch(k_join, dim3((a.rows + 15) / 16), dim3(1024), s, a); }
+hipError_t launch_teacher(const TeacherArgs &a, int type, int index_type, hipStream_t s) {
+    return index_type == ECHO_I64 ? teacher<int64_t>(a, type, s) : teacher<int32_t>(a, type, s);
+}
+hipError_t launch_scale(const float *grad_loss, int rows, float *scale, hipStream_t s) {
+    return launch(k_scale, dim3(1), dim3(1024), s, grad_loss, rows, scale);
+}
+hipError_t launch_layout(const LayoutArgs &a, int type, hipStream_t s) {
+    const dim3 grid(grid_of((a.rows * (a.width / 8) + 255) / 256));
+    switch (type) {
+        case ECHO_F32: return launch(k_layout<float, bf16, 3>, grid, dim3(256), s, a);
+        case ECHO_F16: return launch(k_layout<f16, f16, 1>, grid, dim3(256), s, a);
+        default: return launch(k_layout<bf16, bf16, 1>, grid, dim3(256), s, a);
+    }
+}
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+int tiles(int64_t n, int t) { return (int)((n + t - 1) / t); }
+
+// How full `wg` workgroups leave a launch's last round, of 256 or 512 at a time.
+double full(int64_t wg, int at_once) { return (double)wg / (double)up(wg, at_once); }
+// Shape of a product's tiles: wide ones do the most work for what they read, and middle ones fill the GPU where there
+// are few.  Thin ones (logits alone) are for up to 64 rows.
+int shape_of(int64_t ni, int64_t nj, bool thin) {
+    if (thin && nj <= 64) return 2;
+    const int64_t wide = (int64_t)tiles(ni, 256) * tiles(nj, 256), middle = (int64_t)tiles(ni, 128) * tiles(nj, 128);
+    return full(wide, 256) >= 0.75 * full(middle, 512) ? 0 : 1;
+}
+void tile(Product &m, int shape) {
+    m.tiles_i = tiles(m.ni, shape == 1 ? 128 : 256);
+    m.tiles_j = tiles(m.nj, shape == 0 ? 256 : shape == 1 ? 128 : 64);
+}
+
+constexpr int64_t kProbBytes = int64_t(1) << 30;      // of the logits' gradient at a time
+constexpr int64_t kProbCols = int64_t(1) << 21;
+
+// Sizes of a call's products, and where its workspace has what.
+struct Plan {
+    int planes, pairs;
+    int width;                     // hidden size in whole steps
+    bool copy_hidden, copy_weight;
+    int logits_shape, stats_tiles; // the loss's
+    int64_t prob_rows, prob_cols, pieces;
+    int hidden_shape, splits;      // the hidden states' gradient
+    bool parts;
+    int64_t hidden, weight, stats, hits, local, q, prior, scale, prob, part, bytes;
+};
+bool direct(const void *p, int64_t stride, int type, int cols) {
+    return type != ECHO_F32 && cols % kDepth == 0 && stride % 8 == 0 && stride <= int64_t(1) << 22 && (uintptr_t)p % 16 == 0;
+}
+Plan plan_of(const LinearArgs &a) {
+    Plan p{};
+    p.planes = a.type == ECHO_F32 ? 3 : 1;
+    p.pairs = a.type == ECHO_F32 ? 6 : 1;
+    p.width = (int)up(a.cols, kDepth);
+    p.copy_hidden = !direct(a.hidden, a.hidden_stride, a.type, a.cols);
+    p.copy_weight = !direct(a.weight, a.weight_stride, a.type, a.cols);
+    const auto take = [&](int64_t n) {
+        const int64_t at = p.bytes;
+        p.bytes += up(n, 256);
+        return at;
+    };
+    if (p.copy_hidden) p.hidden = take(a.rows * p.width * 2 * p.planes);
+    if (p.copy_weight) p.weight = take((int64_t)a.vocab * p.width * 2 * p.planes);
+    if (a.top) {
+        p.local = take(a.rows * a.top * 4);
+        p.q = take(a.rows * a.top * 4);
+        p.prior = take(a.rows * 8);
+    }
+    if (a.forward) {
+        p.logits_shape = shape_of(a.vocab, a.rows, true);
+        p.stats_tiles = tiles(a.vocab, p.logits_shape == 1 ? 128 : 256);
+        p.stats = take(p.stats_tiles * a.rows * 8);
+        p.hits = take(a.rows * (a.top ? a.top : 1) * 4);
+    }
+    if (a.grads) {
+        p.scale = take(4);
+        p.prob_rows = up(a.rows, kDepth);
+        const int64_t whole = up(a.vocab, kDepth);
+        int64_t most = kProbBytes / (p.prob_rows * 2 * p.planes) / 256 * 256;
+        most = most < 256 ? 256 : most > kProbCols ? kProbCols : most;
+        p.pieces = (whole + most - 1) / most;
+        p.prob_cols = p.pieces == 1 ? whole : up((whole + p.pieces - 1) / p.pieces, 256);
+        p.prob = take(p.prob_rows * p.prob_cols * 2 * p.planes);
+        p.hidden_shape = shape_of(a.cols, a.rows, false);
+        const int t = p.hidden_shape ? 128 : 256, at_once = p.hidden_shape ? 512 : 256;
+        const int64_t wg = (int64_t)tiles(a.cols, t) * tiles(a.rows, t), steps = p.prob_cols / kDepth * p.pairs;
+        int64_t splits = wg >= at_once ? 1 : at_once / wg;
+        if (splits > steps / 4) splits = steps / 4;
+        p.splits = splits < 1 ? 1 : (int)splits;
+        p.parts = p.splits > 1 || p.pieces > 1;
+        if (p.parts) p.part = take(p.splits * a.rows * a.cols * 4);
+    }
+    return p;
+}
+
+}  // namespace
+
+int64_t linear_bytes(const LinearArgs &a) { return plan_of(a).bytes; }
+
+#define ECHO_HIP(call)                        \
+    do {                                      \
+        const hipError_t e_ = (call);         \
+        if (e_ != hipSuccess) return e_;      \
+    } while (0)
+
+hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
+    if (!a.rows) return launch_zero(a.dweight, (int64_t)a.vocab * a.cols * (a.grad_type == ECHO_F32 ? 4 : 2), s);
+    const Plan p = plan_of(a);
+    char *w = static_cast<char *>(a.workspace);
+    const int64_t row_bytes = (int64_t)p.width * 2;
+    Operand hidden{static_cast<const char *>(a.hidden), a.hidden_stride * 2, 0, a.rows, p.width},
+        weight{static_cast<const char *>(a.weight), a.weight_stride * 2, 0, a.vocab, p.width};
+    if (p.copy_hidden) {
+        hidden = Operand{w + p.hidden, row_bytes, a.rows * row_bytes, a.rows, p.width};
+        ECHO_HIP(launch_layout(LayoutArgs{a.hidden, a.hidden_stride, a.rows, a.cols, p.width, w + p.hidden, hidden.plane}, a.type, s));
+    }
+    if (p.copy_weight) {
+        weight = Operand{w + p.weight, row_bytes, a.vocab * row_bytes, a.vocab, p.width};
+        ECHO_HIP(launch_layout(LayoutArgs{a.weight, a.weight_stride, a.vocab, a.cols, p.width, w + p.weight, weight.plane}, a.type, s));
+    }
+    HeadArgs h{};
+    h.rows = (int)a.rows;
+    h.vocab = a.vocab;
+    h.inv_t = 1.0f / a.temperature;
+    h.targets = a.targets;
+    h.wide_index = a.index_type == ECHO_I64;
+    h.top = a.top;
+    h.vocab_start = a.vocab_start;
+    h.vocab_size = a.vocab_size;
+    if (a.top) {
+        const TeacherArgs t{a.targets, a.teacher, a.rows, a.vocab_start, a.vocab_size, a.top, a.vocab, h.inv_t,
+                            reinterpret_cast<int *>(w + p.local), reinterpret_cast<float *>(w + p.q),
+                            reinterpret_cast<float2 *>(w + p.prior)};
+        ECHO_HIP(launch_teacher(t, a.teacher_type, a.index_type, s));
+        h.local = t.local;
+        h.q = t.q;
+        h.prior = t.prior;
+    }
+    h.m = Product{weight, hidden, a.vocab, (int)a.rows, 0, 0, p.width / kDepth, p.pairs, 1};
+    if (a.forward) {
+        h.stats = reinterpret_cast<float2 *>(w + p.stats);
+        h.hits = reinterpret_cast<float *>(w + p.hits);
+        tile(h.m, p.logits_shape);
+        ECHO_HIP(launch_logits(h, a.type, false, p.logits_shape, s));
+        ECHO_HIP(launch_join(JoinArgs{h.stats, h.prior, h.hits, h.q, h.local, h.targets, h.wide_index, h.top, h.rows, h.vocab,
+                                      p.stats_tiles, h.vocab_start, h.vocab_size, a.temperature * a.temperature, a.lse, a.target,
+                                      a.entropy, a.loss}, s));
+    }
+    if (!a.grads) return hipSuccess;
+    h.lse = a.forward ? a.lse : a.lse_in;
+    h.grad_loss = a.grad_loss;
+    h.scale = reinterpret_cast<float *>(w + p.scale);
+    h.prob = w + p.prob;
+    h.prob_stride = p.prob_cols * 2;
+    h.prob_plane = p.prob_rows * h.prob_stride;
+    h.prob_rows = (int)p.prob_rows;
+    h.prob_cols = (int)p.prob_cols;
+    ECHO_HIP(launch_scale(a.grad_loss, h.rows, reinterpret_cast<float *>(w + p.scale), s));
+    const Operand prob{h.prob, h.prob_stride, h.prob_plane, p.prob_rows, (int)p.prob_cols};
+    const int64_t grad_elem = a.grad_type == ECHO_F32 ? 4 : 2;
+    const int out_type = a.type;
+    float *parts = p.parts ? reinterpret_cast<float *>(w + p.part) : nullptr;
+    for (int64_t piece = 0; piece < p.pieces; ++piece) {
+        const int64_t first = piece * p.prob_cols, left = a.vocab - first;
+        const int n = (int)(left < p.prob_cols ? left : p.prob_cols);
+        Operand table = weight;
+        table.p += first * weight.stride;
+        table.rows = n;
+        h.first = (int)first;
+        h.m.a = table;
+        h.m.ni = n;
+        // the tiles fill the piece's columns, past the vocabulary's end too
+        const int shape = shape_of(p.prob_cols, a.rows, true);
+        Product cover = h.m;
+        cover.ni = (int)p.prob_cols;
+        tile(cover, shape);
+        h.m.tiles_i = cover.tiles_i;
+        h.m.tiles_j = cover.tiles_j;
+        ECHO_HIP(launch_logits(h, a.type, true, shape, s));
+        OutArgs o{};
+        o.scale = h.scale;
+        o.factor = a.temperature;
+        o.m = Product{table, prob, a.cols, (int)a.rows, 0, 0, (int)(p.prob_cols / kDepth), p.pairs, p.splits};
+        o.parts = parts;
+        o.add_parts = piece > 0;
+        o.out = a.dhidden;
+        tile(o.m, p.hidden_shape);
+        ECHO_HIP(launch_out(o, a.type, out_type, true, p.hidden_shape, s));
+        o.m = Product{hidden, prob, a.cols, n, 0, 0, (int)(p.prob_rows / kDepth), p.pairs, 1};
+        o.parts = nullptr;
+        o.out = static_cast<char *>(a.dweight) + first * a.cols * grad_elem;
+        o.accumulate = a.accumulate;
+        const int table_shape = shape_of(a.cols, n, false);
+        tile(o.m, table_shape);
+        ECHO_HIP(launch_out(o, a.type, a.grad_type, false, table_shape, s));
+    }
+    if (parts)
+        ECHO_HIP(launch_gather(GatherArgs{parts, a.rows * a.cols, p.splits, h.scale, a.temperature, a.dhidden}, a.type, out_type, s));
+    return hipSuccess;
+}
+
+}  // namespace echo

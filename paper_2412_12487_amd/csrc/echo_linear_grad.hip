@@ -1,0 +1,107 @@
+// echo_linear_grad.hip -- gradients of hidden states and of the output table from the logits' gradient, on gfx950.
+#include "echo_linear.h"
+
+namespace echo {
+namespace {
+
+template <class U>
+__device__ __forceinline__ void put4(U *out, int left, F4 d, bool add) {
+    typedef V<U, 4> U4;
+    if (left >= 4) {
+        if (add) d += __builtin_convertvector(*reinterpret_cast<const U4 *>(out), F4);
+        *reinterpret_cast<U4 *>(out) = __builtin_convertvector(d, U4);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < left) out[e] = (U)(d[e] + (add ? (float)out[e] : 0.0f));
+}
+
+// i over the hidden size, across the rows of operand a; j over rows (deep) or over the vocabulary.
+template <class T, class U, class S, bool DEEP>
+__global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_out(OutArgs a) {
+    [[maybe_unused]] __shared__ __attribute__((aligned(16))) char t0[S::BYTES];
+    [[maybe_unused]] __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
+    const Place at = place_of(a.m);
+    F4 acc[S::BI][S::BJ];
+#ifdef __HIP_DEVICE_COMPILE__      // reads shared memory transposed, which the host's pass does not know
+    multiply<T, false, DEEP, S>(a.m, at, t0, t1, acc);
+#endif
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wi = wave / S::WJ, wj = wave % S::WJ;
+    const int i0 = at.ti * S::TI + wi * S::BI * 16 + (lane / 16) * 4, j0 = at.tj * S::TJ + wj * S::BJ * 16 + lane % 16;
+    const float scale = a.parts ? 1.0f : *a.scale * (a.factor / kUnit<T>);
+#pragma unroll
+    for (int b = 0; b < S::BJ; ++b) {
+        const int j = j0 + b * 16;
+        if (j >= a.m.nj) continue;
+#pragma unroll
+        for (int k = 0; k < S::BI; ++k) {
+            const int i = i0 + k * 16;
+            if (i >= a.m.ni) continue;
+            const F4 d = acc[k][b] * scale;
+            if (a.parts)
+                put4(a.parts + ((int64_t)at.split * a.m.nj + j) * a.m.ni + i, a.m.ni - i, d, a.add_parts);
+            else
+                put4(static_cast<U *>(a.out) + (int64_t)j * a.m.ni + i, a.m.ni - i, d, a.accumulate);
+        }
+    }
+}
+
+// Sums the parts, in their order.
+template <class U>
+__global__ __launch_bounds__(256) void k_gather(GatherArgs a, float unit) {
+    const float scale = *a.scale * (a.factor / unit);
+    for (int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; at < a.n; at += (int64_t)gridDim.x * 1024) {
+        const int left = a.n - at < 4 ? (int)(a.n - at) : 4;
+        F4 d = 0.0f;
+        for (int p = 0; p < a.splits; ++p) {
+            const float *from = a.parts + p * a.n + at;
+            if (left == 4) {
+                d += *reinterpret_cast<const V<float, 4> *>(from);
+            } else {
+                for (int e = 0; e < left; ++e) d[e] += from[e];
+            }
+        }
+        put4(static_cast<U *>(a.out) + at, left, d * scale, false);
+    }
+}
+
+// No rows: the table's gradient is zeros.
+__global__ __launch_bounds__(256) void k_zero(unsigned short *out, int64_t n) {
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (int64_t)gridDim.x * 256) out[at] = 0;
+}
+
+template <class T, class U, bool DEEP>
+hipError_t out(const OutArgs &a, int shape, hipStream_t s) {
+    const dim3 grid((unsigned)(a.m.tiles_i * a.m.tiles_j * a.m.splits));
+    switch (shape) {
+        case 0: return launch(k_out<T, U, Wide, DEEP>, grid, dim3(Wide::THREADS), s, a);
+        default: return launch(k_out<T, U, Middle, DEEP>, grid, dim3(Middle::THREADS), s, a);
+    }
+}
+template <class T, class U>
+hipError_t out(const OutArgs &a, bool deep, int shape, hipStream_t s) {
+    return deep ? out<T, U, true>(a, shape, s) : out<T, U, false>(a, shape, s);
+}
+
+}  // namespace
+
+hipError_t launch_out(const OutArgs &a, int type, int out_type, bool deep, int shape, hipStream_t s) {
+    if (type == ECHO_F16) return out_type == ECHO_F32 ? out<f16, float>(a, deep, shape, s) : out<f16, f16>(a, deep, shape, s);
+    return out_type == ECHO_F32 ? out<bf16, float>(a, deep, shape, s) : out<bf16, bf16>(a, deep, shape, s);
+}
+hipError_t launch_zero(void *out, int64_t bytes, hipStream_t s) {
+    return launch(k_zero, dim3(grid_of((bytes / 2 + 255) / 256)), dim3(256), s, static_cast<unsigned short *>(out), bytes / 2);
+}
+hipError_t launch_gather(const GatherArgs &a, int type, int out_type, hipStream_t s) {
+    const dim3 grid(grid_of((a.n + 1023) / 1024));
+    const float unit = type == ECHO_F16 ? kUnit<f16> : 1.0f;
+    switch (out_type) {
+        case ECHO_F32: return launch(k_gather<float>, grid, dim3(256), s, a, unit);
+        case ECHO_F16: return launch(k_gather<f16>, grid, dim3(256), s, a, unit);
+        default: return launch(k_gather<bf16>, grid, dim3(256), s, a, unit);
+    }
+}
+
+}  // namespace echo

@@ -118,6 +118,29 @@ int check_workspace(const void *p, int64_t bytes, int64_t need) {
     return ECHO_OK;
 }
 
+constexpr int64_t kMaxTop = 1024;
+constexpr int64_t kMaxHeadRows = int64_t(1) << 24, kMaxHidden = int64_t(1) << 20;
+
+int check_teacher(const void *ids, int32_t index_type, const void *teacher, int32_t teacher_type, int32_t type, int64_t rows,
+                  int64_t top, float temperature) {
+    if (teacher_type != type && teacher_type != ECHO_F32)
+        return set_error(ECHO_ERR_ARG, "teacher_type must be the activations' type or 32 bits (got %d)", teacher_type);
+    if (top < 1 || top > kMaxTop) return set_error(ECHO_ERR_ARG, "top = %lld outside [1, 1024]", (long long)top);
+    if (!(temperature >= 1e-6f && temperature <= 1e6f))
+        return set_error(ECHO_ERR_ARG, "temperature %g outside [1e-6, 1e6]", (double)temperature);
+    const int rc = check_vector("ids", ids, index_type == ECHO_I64 ? 8 : 4, rows > 0);
+    return rc != ECHO_OK ? rc : check_vector("teacher", teacher, elem(teacher_type), rows > 0);
+}
+int check_head_sizes(int64_t rows, int64_t cols, int64_t vocab) {
+    if (rows < 0 || rows > kMaxHeadRows) return set_error(ECHO_ERR_ARG, "rows = %lld outside [0, 2^24]", (long long)rows);
+    if (cols < 1 || cols > kMaxHidden) return set_error(ECHO_ERR_ARG, "cols = %lld outside [1, 2^20]", (long long)cols);
+    if (vocab < 1 || vocab > kMaxHeadRows) return set_error(ECHO_ERR_ARG, "vocab = %lld outside [1, 2^24]", (long long)vocab);
+    if (rows * cols > kMaxElements || rows * vocab > kMaxElements || vocab * cols > kMaxElements)
+        return set_error(ECHO_ERR_RANGE, "%lld rows of %lld over %lld ids: a product passes 2^38", (long long)rows, (long long)cols,
+                         (long long)vocab);
+    return ECHO_OK;
+}
+
 // Runs f on GPU `device` and leaves the thread's current device as it was.
 template <class F>
 int on_device(int device, const char *what, F f) {
@@ -333,6 +356,206 @@ int echo_cross_entropy_grad(const void *logits, int64_t logits_stride, int32_t t
     return on_device(hip_device, "cross entropy gradient", [&] {
         return launch_loss_grad(a, type, index_type, static_cast<hipStream_t>(hip_stream));
     });
+}
+
+}  // extern "C"
+
+namespace {
+
+// Loss (lse_in null) and gradient of distillation.
+int distill(DistillArgs a, int32_t type, int32_t index_type, int32_t teacher_type, int64_t cols, int64_t top, bool grads,
+            int hip_device, void *hip_stream, const char *what) {
+    ECHO_TRY(check_types(type, type, "type"));
+    ECHO_TRY(check_index(index_type));
+    ECHO_TRY(check_sizes(a.rows, cols));
+    ECHO_TRY(check_teacher(a.ids, index_type, a.teacher, teacher_type, type, a.rows, top, a.temperature));
+    ECHO_TRY(check_shard_of(a.vocab_start, cols, a.vocab_size));
+    const bool whole = a.vocab_start == 0 && a.vocab_size == cols, only_grad = grads;
+    if (!only_grad) {
+        if (!whole && (a.loss || a.grad))
+            return set_error(ECHO_ERR_ARG, "loss and grad need the whole vocabulary; a shard gives lse, target and entropy");
+        if (a.rows && !a.lse && !a.target && !a.entropy && !a.loss && !a.grad)
+            return set_error(ECHO_ERR_ARG, "no output is asked for");
+        if (a.rows && !a.grad != !a.grad_loss) return set_error(ECHO_ERR_ARG, "grad_loss is given exactly when grad is");
+    }
+    const int64_t e = elem(type), ie = index_type == ECHO_I64 ? 8 : 4, live = only_grad || a.grad ? a.rows : 0;
+    ECHO_TRY(check_matrix("logits", a.logits, a.rows, a.logits_stride, e));
+    ECHO_TRY(check_vector("lse", only_grad ? a.lse_in : a.lse, 4, only_grad && a.rows > 0));
+    ECHO_TRY(check_vector("target", a.target, 4, false));
+    ECHO_TRY(check_vector("entropy", a.entropy, 4, false));
+    ECHO_TRY(check_vector("loss", a.loss, 4, false));
+    ECHO_TRY(check_vector("grad_loss", a.grad_loss, 4, live > 0));
+    ECHO_TRY(check_matrix("grad", a.grad, live, live ? a.grad_stride : 0, e));
+    if (live > 1 && a.grad_stride < cols) return set_error(ECHO_ERR_ARG, "rows of grad overlap");
+    const bool dense = a.rows < 2 || a.logits_stride == a.grad_stride;
+    ECHO_TRY(check_spans({matrix("grad", a.grad, live, cols, a.grad_stride, e, 1), vector("lse", a.lse, a.rows, 4),
+                          vector("target", a.target, a.rows, 4), vector("entropy", a.entropy, a.rows, 4),
+                          vector("loss", a.loss, a.rows, 4)},
+                         {matrix("logits", a.logits, a.rows, cols, a.logits_stride, e, dense),
+                          vector("ids", a.ids, a.rows * top, ie), vector("teacher", a.teacher, a.rows * top, elem(teacher_type)),
+                          vector("lse", a.lse_in, a.rows, 4), vector("grad_loss", a.grad_loss, a.rows, 4)}));
+    if (!a.rows) return ECHO_OK;
+    a.cols = (int)cols;
+    a.top = (int)top;
+    return on_device(hip_device, what, [&] {
+        return launch_distill(a, type, index_type, teacher_type, static_cast<hipStream_t>(hip_stream));
+    });
+}
+
+// The head's four calls; top is 0 with one target a row.
+int linear(LinearArgs a, int64_t cols, int64_t vocab, int64_t top, int64_t workspace_bytes, int hip_device, void *hip_stream,
+           const char *what) {
+    const bool teacher = top != 0;
+    ECHO_TRY(check_types(a.type, a.type, "type"));
+    ECHO_TRY(check_index(a.index_type));
+    ECHO_TRY(check_head_sizes(a.rows, cols, vocab));
+    if (teacher)
+        ECHO_TRY(check_teacher(a.targets, a.index_type, a.teacher, a.teacher_type, a.type, a.rows, top, a.temperature));
+    else
+        ECHO_TRY(check_vector("targets", a.targets, a.index_type == ECHO_I64 ? 8 : 4, a.rows > 0));
+    ECHO_TRY(check_shard_of(a.vocab_start, vocab, a.vocab_size));
+    a.cols = (int)cols;
+    a.vocab = (int)vocab;
+    a.top = (int)top;
+    const bool whole = a.vocab_start == 0 && a.vocab_size == vocab;
+    if (a.forward) {
+        if (!whole && (a.loss || a.dhidden || a.dweight))
+            return set_error(ECHO_ERR_ARG, "loss and gradients need the whole vocabulary; a shard gives its statistics");
+        if (a.rows && !a.lse && !a.target && !a.entropy && !a.loss && !a.dweight)
+            return set_error(ECHO_ERR_ARG, "no output is asked for");
+        a.grads = a.dweight != nullptr;
+        if (a.rows && (!a.dhidden != !a.dweight || !a.grad_loss != !a.dweight))
+            return set_error(ECHO_ERR_ARG, "grad_loss, dhidden and dweight are given together");
+        if (a.rows && a.grads && !a.lse) return set_error(ECHO_ERR_ARG, "gradients need lse");
+    }
+    const int64_t e = elem(a.type), ie = a.index_type == ECHO_I64 ? 8 : 4, live = a.grads ? a.rows : 0;
+    if (a.grads && a.grad_type != a.type && a.grad_type != ECHO_F32)
+        return set_error(ECHO_ERR_ARG, "grad_type must be the activations' type or 32 bits (got %d)", a.grad_type);
+    const int64_t ge = elem(a.grad_type);
+    ECHO_TRY(check_matrix("hidden", a.hidden, a.rows, a.hidden_stride, e));
+    ECHO_TRY(check_matrix("weight", a.weight, a.rows ? vocab : 0, a.weight_stride, e));
+    ECHO_TRY(check_vector("lse", a.forward ? a.lse : a.lse_in, 4, !a.forward && a.rows > 0));
+    ECHO_TRY(check_vector("target", a.target, 4, false));
+    ECHO_TRY(check_vector("entropy", a.entropy, 4, false));
+    ECHO_TRY(check_vector("loss", a.loss, 4, false));
+    ECHO_TRY(check_vector("grad_loss", a.grad_loss, 4, live > 0));
+    ECHO_TRY(check_matrix("dhidden", a.dhidden, live, a.cols, e));
+    ECHO_TRY(check_vector("dweight", a.dweight, ge, a.grads));
+    const int64_t need = a.rows ? linear_bytes(a) : 0;
+    ECHO_TRY(check_workspace(a.workspace, workspace_bytes, need));
+    ECHO_TRY(check_spans({matrix("dhidden", a.dhidden, live, cols, cols, e), vector("dweight", a.grads ? a.dweight : nullptr, vocab * cols, ge),
+                          vector("lse", a.lse, a.rows, 4), vector("target", a.target, a.rows, 4),
+                          vector("entropy", a.entropy, a.rows, 4), vector("loss", a.loss, a.rows, 4),
+                          vector("workspace", a.workspace, need, 1)},
+                         {matrix("hidden", a.hidden, a.rows, cols, a.hidden_stride, e),
+                          matrix("weight", a.weight, vocab, cols, a.weight_stride, e),
+                          vector(teacher ? "ids" : "targets", a.targets, a.rows * (teacher ? top : 1), ie),
+                          vector("teacher", a.teacher, a.rows * top, teacher ? elem(a.teacher_type) : 4),
+                          vector("lse", a.lse_in, a.rows, 4), vector("grad_loss", a.grad_loss, a.rows, 4)}));
+    if (!a.rows && (!a.grads || a.accumulate)) return ECHO_OK;
+    return on_device(hip_device, what, [&] { return launch_linear(a, static_cast<hipStream_t>(hip_stream)); });
+}
+
+}  // namespace
+
+extern "C" {
+
+int echo_distillation(const void *logits, int64_t logits_stride, int32_t type, const void *ids, int32_t index_type,
+                      const void *teacher, int32_t teacher_type, int64_t rows, int64_t cols, int64_t top,
+                      int64_t vocab_start, int64_t vocab_size, float temperature, float *lse, float *target,
+                      float *entropy, float *loss, const float *grad_loss, void *grad, int64_t grad_stride,
+                      int hip_device, void *hip_stream) {
+    clear_error();
+    const DistillArgs a{logits, ids, teacher, logits_stride, rows, vocab_start, vocab_size, 0, 0, temperature, lse, target,
+                        entropy, loss, nullptr, grad_loss, grad, grad_stride};
+    return distill(a, type, index_type, teacher_type, cols, top, false, hip_device, hip_stream, "distillation");
+}
+
+int echo_distillation_grad(const void *logits, int64_t logits_stride, int32_t type, const void *ids, int32_t index_type,
+                           const void *teacher, int32_t teacher_type, int64_t rows, int64_t cols, int64_t top,
+                           int64_t vocab_start, int64_t vocab_size, float temperature, const float *lse,
+                           const float *grad_loss, void *grad, int64_t grad_stride, int hip_device, void *hip_stream) {
+    clear_error();
+    const DistillArgs a{logits, ids, teacher, logits_stride, rows, vocab_start, vocab_size, 0, 0, temperature, nullptr, nullptr,
+                        nullptr, nullptr, lse, grad_loss, grad, grad_stride};
+    return distill(a, type, index_type, teacher_type, cols, top, true, hip_device, hip_stream, "distillation gradient");
+}
+
+int64_t echo_linear_workspace(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                              int32_t type, int64_t rows, int64_t cols, int64_t vocab, int64_t top, int32_t loss,
+                              int32_t grads) {
+    if (!is_type(type) || rows < 1 || rows > kMaxHeadRows || cols < 1 || cols > kMaxHidden || vocab < 1 || vocab > kMaxHeadRows ||
+        top < 0 || top > kMaxTop || rows * cols > kMaxElements || rows * vocab > kMaxElements || vocab * cols > kMaxElements)
+        return 0;
+    LinearArgs a{};
+    a.hidden = hidden;
+    a.weight = weight;
+    a.hidden_stride = hidden_stride;
+    a.weight_stride = weight_stride;
+    a.rows = rows;
+    a.type = type;
+    a.cols = (int)cols;
+    a.vocab = (int)vocab;
+    a.top = (int)top;
+    a.forward = loss != 0;
+    a.grads = grads != 0;
+    return linear_bytes(a);
+}
+
+int echo_linear_cross_entropy(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                              int32_t type, const void *targets, int32_t index_type, int64_t rows, int64_t cols,
+                              int64_t vocab, int64_t vocab_start, int64_t vocab_size, float *lse, float *target,
+                              float *loss, const float *grad_loss, void *dhidden, void *dweight, int32_t grad_type,
+                              int32_t accumulate, void *workspace, int64_t workspace_bytes, int hip_device,
+                              void *hip_stream) {
+    clear_error();
+    const LinearArgs a{hidden, weight, hidden_stride, weight_stride, rows, type, 0, 0, targets, nullptr, index_type, ECHO_F32, 0,
+                       1.0f, vocab_start, vocab_size, true, false, lse, target, nullptr, loss, nullptr, grad_loss, dhidden,
+                       dweight, grad_type, accumulate != 0, workspace};
+    return linear(a, cols, vocab, 0, workspace_bytes, hip_device, hip_stream, "linear cross entropy");
+}
+
+int echo_linear_cross_entropy_grad(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                                   int32_t type, const void *targets, int32_t index_type, int64_t rows, int64_t cols,
+                                   int64_t vocab, int64_t vocab_start, int64_t vocab_size, const float *lse,
+                                   const float *grad_loss, void *dhidden, void *dweight, int32_t grad_type,
+                                   int32_t accumulate, void *workspace, int64_t workspace_bytes, int hip_device,
+                                   void *hip_stream) {
+    clear_error();
+    const LinearArgs a{hidden, weight, hidden_stride, weight_stride, rows, type, 0, 0, targets, nullptr, index_type, ECHO_F32, 0,
+                       1.0f, vocab_start, vocab_size, false, true, nullptr, nullptr, nullptr, nullptr, lse, grad_loss, dhidden,
+                       dweight, grad_type, accumulate != 0, workspace};
+    return linear(a, cols, vocab, 0, workspace_bytes, hip_device, hip_stream, "linear cross entropy gradient");
+}
+
+int echo_linear_distillation(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                             int32_t type, const void *ids, int32_t index_type, const void *teacher,
+                             int32_t teacher_type, int64_t rows, int64_t cols, int64_t vocab, int64_t top,
+                             int64_t vocab_start, int64_t vocab_size, float temperature, float *lse, float *target,
+                             float *entropy, float *loss, const float *grad_loss, void *dhidden, void *dweight,
+                             int32_t grad_type, int32_t accumulate, void *workspace, int64_t workspace_bytes,
+                             int hip_device, void *hip_stream) {
+    clear_error();
+    if (top < 1) return set_error(ECHO_ERR_ARG, "top = %lld outside [1, 1024]", (long long)top);
+    const LinearArgs a{hidden, weight, hidden_stride, weight_stride, rows, type, 0, 0, ids, teacher, index_type, teacher_type, 0,
+                       temperature, vocab_start, vocab_size, true, false, lse, target, entropy, loss, nullptr, grad_loss,
+                       dhidden, dweight, grad_type, accumulate != 0, workspace};
+    return linear(a, cols, vocab, top, workspace_bytes, hip_device, hip_stream, "linear distillation");
+}
+
+int echo_linear_distillation_grad(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                                  int32_t type, const void *ids, int32_t index_type, const void *teacher,
+                                  int32_t teacher_type, int64_t rows, int64_t cols, int64_t vocab, int64_t top,
+                                  int64_t vocab_start, int64_t vocab_size, float temperature, const float *lse,
+                                  const float *grad_loss, void *dhidden, void *dweight, int32_t grad_type,
+                                  int32_t accumulate, void *workspace, int64_t workspace_bytes, int hip_device,
+                                  void *hip_stream) {
+    clear_error();
+    if (top < 1) return set_error(ECHO_ERR_ARG, "top = %lld outside [1, 1024]", (long long)top);
+    const LinearArgs a{hidden, weight, hidden_stride, weight_stride, rows, type, 0, 0, ids, teacher, index_type, teacher_type, 0,
+                       temperature, vocab_start, vocab_size, false, true, nullptr, nullptr, nullptr, nullptr, lse, grad_loss,
+                       dhidden, dweight, grad_type, accumulate != 0, workspace};
+    return linear(a, cols, vocab, top, workspace_bytes, hip_device, hip_stream, "linear distillation gradient");
 }
 
 }  // extern "C"

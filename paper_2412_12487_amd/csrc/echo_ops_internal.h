@@ -54,9 +54,39 @@ struct LossArgs {
     int64_t grad_stride;
 };
 
+// Losses straight from hidden states and the output table: one target a row (top 0) or a teacher's top ids.
+struct LinearArgs {
+    const void *hidden, *weight;
+    int64_t hidden_stride, weight_stride, rows;
+    int type, cols, vocab;
+    const void *targets, *teacher;     // ids, and the teacher's logits of them
+    int index_type, teacher_type, top;
+    float temperature;
+    int64_t vocab_start, vocab_size;
+    bool forward, grads;               // the loss's statistics; the gradients
+    float *lse, *target, *entropy, *loss;
+    const float *lse_in, *grad_loss;
+    void *dhidden, *dweight;
+    int grad_type;
+    bool accumulate;
+    void *workspace;
+};
+struct DistillArgs {
+    const void *logits, *ids, *teacher;
+    int64_t logits_stride, rows, vocab_start, vocab_size;
+    int cols, top;
+    float temperature;
+    float *lse, *target, *entropy, *loss;
+    const float *lse_in, *grad_loss;
+    void *grad;
+    int64_t grad_stride;
+};
+
 // Row partitions of the weight-gradient reduction, and bytes of scratch.
 int norm_grad_parts(int64_t rows, int64_t cols);
 int64_t embed_grad_bytes(int64_t rows, int64_t cols, int64_t vocab);
+
+int64_t linear_bytes(const LinearArgs &a);
 
 hipError_t launch_norm(const NormArgs &a, int type, int weight_type, hipStream_t s);
 hipError_t launch_norm_grad(const NormGradArgs &a, int type, int weight_type, int grad_type, hipStream_t s);
@@ -64,5 +94,7 @@ hipError_t launch_embed(const EmbedArgs &a, int type, int index_type, hipStream_
 hipError_t launch_embed_grad(const EmbedGradArgs &a, int type, int index_type, int grad_type, hipStream_t s);
 hipError_t launch_loss(const LossArgs &a, int type, int index_type, hipStream_t s);
 hipError_t launch_loss_grad(const LossArgs &a, int type, int index_type, hipStream_t s);
+hipError_t launch_linear(const LinearArgs &a, hipStream_t s);
+hipError_t launch_distill(const DistillArgs &a, int type, int index_type, int teacher_type, hipStream_t s);
 
 }  // namespace echo

@@ -1,0 +1,185 @@
+// echo_product.h -- tiles of matrix products on the matrix cores of gfx950, for the output head's kernels.
+//
+//   D[j][i] = sum over k of A(i, k) B(j, k)
+//
+// in 32 bits, of operands of 16 bits.  A workgroup has TI x TJ of D in registers and takes k in steps of 64: both operands'
+// pieces of a step go from memory straight into one of two buffers of shared memory, while the matrix
+// instructions work on the other one.  An operand lies with k along its rows (DEEP) or across them; the latter is
+// transposed on its way out of shared memory (ds_read_b64_tr_b16).  Reads past an operand's end give zeros.
+#pragma once
+
+#include "echo_ops_device.h"
+
+namespace echo {
+namespace {
+
+// An operand: `rows` rows of `width` elements of 16 bits, `stride` bytes apart, in planes `plane` bytes apart.
+// Rows begin at multiples of 16 bytes and hold whole pieces of 64 elements; 255 strides stay below 2^31.
+struct Operand {
+    const char *p;
+    int64_t stride, plane, rows;
+    int width;
+};
+struct Product {
+    Operand a, b;
+    int ni, nj;               // size of D
+    int tiles_i, tiles_j;
+    int steps;                // of 64 along k, in a plane
+    int pairs;                // products of planes that are summed: 1, or 6 of 3 planes each
+    int splits;               // parts of the steps, each in a workgroup of its own
+};
+// 3 planes of 8 significant bits each make 24: the products that matter, of planes (a, b).
+__device__ __forceinline__ int plane_a(int pair) { return (0x120100 >> (4 * pair)) & 3; }   // 0 0 1 0 2 1
+__device__ __forceinline__ int plane_b(int pair) { return (0x102010 >> (4 * pair)) & 3; }   // 0 1 0 2 0 1
+
+using F4 = __attribute__((ext_vector_type(4))) float;
+template <class T>
+using H8 = __attribute__((ext_vector_type(8))) T;
+using S4 = __attribute__((ext_vector_type(4))) short;
+using S8 = __attribute__((ext_vector_type(8))) short;
+using LdsPtr = __attribute__((address_space(3))) void *;
+
+constexpr int kDepth = 64;
+
+__device__ __forceinline__ F4 mfma(H8<bf16> a, H8<bf16> b, F4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ F4 mfma(H8<f16> a, H8<f16> b, F4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// Where the 16-byte piece c of row r lies in shared memory: pieces are exchanged within a row so that the lanes which
+// read together meet different banks.
+__device__ __forceinline__ int turned(int k) { return (k & 3) | ((k >> 3) & 1) << 2; }
+
+// One operand's share of a step: R rows of D's side, from memory to shared memory and from there to registers.
+template <class T, int R, bool DEEP, int WAVES>
+struct Feed {
+    static constexpr int BYTES = R * kDepth * 2, LOADS = BYTES / (WAVES * 1024), UNITS = R / 16;
+    static_assert(LOADS * WAVES * 1024 == BYTES, "");
+    const char *origin, *p;
+    int64_t left0, left, advance, plane;
+    unsigned off[LOADS];
+    __device__ __forceinline__ Feed(const Operand &o, int64_t row, int wave, int lane) {
+        origin = o.p + (DEEP ? row * o.stride : row * 2);
+        left0 = (o.rows - 1 - (DEEP ? row : 0)) * o.stride + ((int64_t)o.width - (DEEP ? 0 : row)) * 2;
+        advance = DEEP ? kDepth * 2 : kDepth * o.stride;
+        plane = o.plane;
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) {
+            const int q = (n * WAVES + wave) * kWave + lane, PIECES = DEEP ? 8 : R / 8, r = q / PIECES, c = q % PIECES;
+            const int from = DEEP ? c ^ (r & 7) : c ^ ((turned(r) & (UNITS - 1)) << 1);
+            off[n] = (unsigned)(r * o.stride) + from * 16;
+        }
+    }
+    __device__ __forceinline__ void seek(int in_plane, int step) {
+        const int64_t by = step * advance;
+        p = origin + in_plane * plane + by;
+        left = left0 - by;
+    }
+    // starts the loads of a step and goes on to the next
+    __device__ __forceinline__ void fetch(char *lds, int wave) {
+        const unsigned records = left > 0xffffffffll ? 0xffffffffu : (unsigned)left;
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p), 0, records, 0x00020000);
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (LdsPtr)(lds + (n * WAVES + wave) * 1024), 16, off[n], 0, 0, 0);
+        p += advance;
+        left -= advance;
+    }
+    // Fragment of the 16 rows from `unit` * 16 and k = half * 32 .. + 31: lane l has row l % 16, k 8 * (l / 16) .. + 7.
+    __device__ __forceinline__ static H8<T> frag(const char *lds, int unit, int half, int lane) {
+        if constexpr (DEEP) {
+            const int r = lane % 16, c = (half * 4 + lane / 16) ^ (r & 7);
+            return *reinterpret_cast<const H8<T> *>(lds + (unit * 16 + r) * 128 + c * 16);
+        } else {
+#ifdef __HIP_DEVICE_COMPILE__      // the builtin is the GPU's
+            const int k = half * 32 + (lane / 16) * 8 + (lane % 16) / 4;
+            const char *at = lds + k * (R * 2) + ((unit ^ (turned(k) & (UNITS - 1))) << 5) + (lane % 4) * 8;
+            typedef __attribute__((address_space(3))) S4 *Lds4;
+            const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)at);
+            const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(at + 4 * R * 2));
+            return __builtin_bit_cast(H8<T>, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#else
+            return H8<T>{};
+#endif
+        }
+    }
+};
+
+template <int TI_, int TJ_, int WI_, int WJ_>
+struct Shape {
+    static constexpr int TI = TI_, TJ = TJ_, WI = WI_, WJ = WJ_, WAVES = WI * WJ, THREADS = WAVES * kWave;
+    static constexpr int BI = TI / WI / 16, BJ = TJ / WJ / 16;       // blocks of 16 x 16 that a wavefront has
+    static constexpr int BYTES = (TI + TJ) * kDepth * 2;             // of a step in shared memory
+};
+// A workgroup's place in D.  Workgroups go to the eight dies in turn; those of one die take neighbouring tiles, and
+// eight tiles along j before the next along i, so that their operands meet in that die's cache.
+struct Place {
+    int ti, tj, split;
+};
+__device__ __forceinline__ Place place_of(const Product &m) {
+    const int tiles = m.tiles_i * m.tiles_j, all = tiles * m.splits, id = blockIdx.x;
+    const int die = id % 8, each = all / 8, more = all % 8;
+    int t = die * each + (die < more ? die : more) + id / 8;
+    const int split = t / tiles;
+    t -= split * tiles;
+    const int group = t / (8 * m.tiles_i), first = group * 8, wide = m.tiles_j - first < 8 ? m.tiles_j - first : 8;
+    t -= group * 8 * m.tiles_i;
+    return Place{t / wide, first + t % wide, split};
+}
+
+// D's tile in registers: acc[a][b][e] belongs to i = a * 16 + 4 * (lane / 16) + e and j = b * 16 + lane % 16 of the wavefront's part.
+template <class T, bool ADEEP, bool BDEEP, class S, class Acc>
+__device__ __forceinline__ void multiply(const Product &m, const Place &at, char *t0, char *t1, Acc &acc) {
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wi = wave / S::WJ, wj = wave % S::WJ;
+    using FA = Feed<T, S::TI, ADEEP, S::WAVES>;
+    using FB = Feed<T, S::TJ, BDEEP, S::WAVES>;
+    FA fa(m.a, (int64_t)at.ti * S::TI, wave, lane);
+    FB fb(m.b, (int64_t)at.tj * S::TJ, wave, lane);
+    const int all = m.steps * m.pairs, begin = (int)((int64_t)all * at.split / m.splits),
+              end = (int)((int64_t)all * (at.split + 1) / m.splits);
+    int pair = begin / m.steps, step = begin - pair * m.steps;
+    fa.seek(plane_a(pair), step);
+    fb.seek(plane_b(pair), step);
+    const auto fetch = [&](char *t) {
+        fa.fetch(t, wave);
+        fb.fetch(t + FA::BYTES, wave);
+        if (++step == m.steps) {
+            step = 0;
+            ++pair;
+            fa.seek(plane_a(pair), 0);
+            fb.seek(plane_b(pair), 0);
+        }
+    };
+#pragma unroll
+    for (int a = 0; a < S::BI; ++a)
+#pragma unroll
+        for (int b = 0; b < S::BJ; ++b) acc[a][b] = 0.0f;
+    const auto half = [&](const char *t, int h) {
+        H8<T> x[S::BI], y[S::BJ];
+#pragma unroll
+        for (int a = 0; a < S::BI; ++a) x[a] = FA::frag(t, wi * S::BI + a, h, lane);
+#pragma unroll
+        for (int b = 0; b < S::BJ; ++b) y[b] = FB::frag(t + FA::BYTES, wj * S::BJ + b, h, lane);
+#pragma unroll
+        for (int a = 0; a < S::BI; ++a)
+#pragma unroll
+            for (int b = 0; b < S::BJ; ++b) acc[a][b] = mfma(x[a], y[b], acc[a][b]);
+    };
+    // The barrier says two things: the step that begins is in shared memory for everybody (each wavefront has waited for its own
+    // loads), and everybody has read the buffer that is filled next.
+    const auto turn = [&](char *mine, char *next, bool more) {
+        __syncthreads();
+        if (more) fetch(next);
+        half(mine, 0);
+        half(mine, 1);
+    };
+    if (begin < end) fetch(t0);
+    int s = begin;
+    for (; s + 1 < end; s += 2) {
+        turn(t0, t1, true);
+        turn(t1, t0, s + 2 < end);
+    }
+    if (s < end) turn(t0, t1, false);
+}
+
+}  // namespace
+}  // namespace echo

@@ -1,12 +1,14 @@
-"""Operators of a training step (include/echo_ops.h): embedding, layer norm and cross entropy, each
-with its gradient, as HIP kernels of libecho.so.
+"""Operators of a training step (include/echo_ops.h): embedding, layer norm, cross entropy, distillation and the output
+head with either loss, each with its gradient, as HIP kernels of libecho.so.
 
 The composer plans a job from its operators' durations; these are the operators of a pipeline
-stage outside its matrix products, on the GPU at hand (`workloads.measured` times them for a graph).
+stage outside its layers' matrix products, on the GPU at hand (`workloads.measured` times them for a graph).
 
     y = layer_norm(x, weight, bias)["y"]
     h = embedding(ids, table, scale)
     r = cross_entropy(logits, targets, grad_loss=g)          # loss, lse and the logits' gradient
+    r = linear_cross_entropy(h, table, targets, grad_loss=g) # loss, lse, dhidden and dweight: logits are not kept
+    r = distillation(logits, ids, teacher, temperature=2.0, grad_loss=g)
 
 Activations are float32, float16 or bfloat16 matrices whose rows are contiguous (leading dimensions in
 one stride; nothing is copied into order behind the caller's back: another layout raises EchoError).
@@ -27,7 +29,9 @@ import torch
 from .echo import ECHO_ERR_ARG, EchoError, _check, lib
 
 EXPORTS = ("echo_layer_norm", "echo_layer_norm_grad", "echo_layer_norm_grad_workspace", "echo_embedding",
-           "echo_embedding_grad", "echo_embedding_grad_workspace", "echo_cross_entropy", "echo_cross_entropy_grad")
+           "echo_embedding_grad", "echo_embedding_grad_workspace", "echo_cross_entropy", "echo_cross_entropy_grad",
+           "echo_distillation", "echo_distillation_grad", "echo_linear_workspace", "echo_linear_cross_entropy",
+           "echo_linear_cross_entropy_grad", "echo_linear_distillation", "echo_linear_distillation_grad")
 
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _INDEX = {torch.int32: 0, torch.int64: 1}
@@ -51,7 +55,18 @@ def _ops():
                 ("embedding_grad", i32, [P, i32, P, i64, i32, i64, i64, i64, i64, f32, P, i32, i32, P, i64, i32, P]),
                 ("embedding_grad_workspace", i64, [i64, i64, i64]),
                 ("cross_entropy", i32, [P, i64, i32, P, i32, i64, i64, i64, i64, P, P, P, P, P, i64, i32, P]),
-                ("cross_entropy_grad", i32, [P, i64, i32, P, i32, i64, i64, i64, i64, P, P, P, i64, i32, P])):
+                ("cross_entropy_grad", i32, [P, i64, i32, P, i32, i64, i64, i64, i64, P, P, P, i64, i32, P]),
+                ("distillation", i32, [P, i64, i32, P, i32, P, i32, i64, i64, i64, i64, i64, f32, P, P, P, P, P, P, i64, i32, P]),
+                ("distillation_grad", i32, [P, i64, i32, P, i32, P, i32, i64, i64, i64, i64, i64, f32, P, P, P, i64, i32, P]),
+                ("linear_workspace", i64, [P, i64, P, i64, i32, i64, i64, i64, i64, i32, i32]),
+                ("linear_cross_entropy", i32, [P, i64, P, i64, i32, P, i32, i64, i64, i64, i64, i64, P, P, P, P, P, P, i32, i32, P,
+                                               i64, i32, P]),
+                ("linear_cross_entropy_grad", i32, [P, i64, P, i64, i32, P, i32, i64, i64, i64, i64, i64, P, P, P, P, i32, i32, P,
+                                                    i64, i32, P]),
+                ("linear_distillation", i32, [P, i64, P, i64, i32, P, i32, P, i32, i64, i64, i64, i64, i64, i64, f32, P, P, P, P, P,
+                                              P, P, i32, i32, P, i64, i32, P]),
+                ("linear_distillation_grad", i32, [P, i64, P, i64, i32, P, i32, P, i32, i64, i64, i64, i64, i64, i64, f32, P, P, P, P,
+                                                   i32, i32, P, i64, i32, P])):
             f = getattr(L, "echo_" + name)
             f.restype, f.argtypes = restype, argtypes
         _fns = L
@@ -398,3 +413,203 @@ def cross_entropy_grad(logits, targets, lse, grad_loss, *, vocab_start=0, vocab_
     if out is not None:
         _written(out)
     return res
+
+
+def _teacher_args(ids, teacher, temperature, dev, rows, lead, dtype):
+    """The teacher's part of a distillation's arguments: ids, index type, logits, their type; and how many a row."""
+    if not isinstance(ids, torch.Tensor) or ids.dim() != len(lead) + 1 or ids.shape[:-1] != torch.Size(lead):
+        raise _bad(f"ids must have the leading shape {tuple(lead)} and one dimension more")
+    if not isinstance(teacher, torch.Tensor) or teacher.shape != ids.shape:
+        raise _bad("teacher must have the shape of ids")
+    top = ids.shape[-1]
+    i = _vector(ids, "ids", dev, rows * top, _INDEX)
+    z = _vector(teacher, "teacher", dev, rows * top, (dtype, torch.float32))
+    return (i, _INDEX[ids.dtype], z, _TYPES[teacher.dtype]), top, float(temperature)
+
+
+def _stats(res, names, like, dev, shape):
+    """Fills res with the float32 tensors of `names` that the caller does not supply; their addresses, in the order of the
+    library's lse, target, entropy and loss."""
+    new = None
+    for n in names:
+        if n in res:
+            res[n] = _dense(res[n], n, dev, shape, torch.float32)
+        else:
+            res[n] = new = like.new_empty(shape, dtype=torch.float32) if new is None else torch.empty_like(new)
+    return [res[n].data_ptr() if n in res else None for n in ("lse", "target", "entropy", "loss")]
+
+
+def distillation(logits, ids, teacher, *, temperature=1.0, vocab_start=0, vocab_size=None, grad_loss=None, out=None):
+    """Distillation of rows of logits from a teacher's top logits: ids and teacher have the leading shape of logits and up to
+    1024 entries a row, teacher logits' type or float32.  Ids outside the vocabulary are padding; a row of padding alone is not
+    trained on; an id may come more than once.  With q the softmax of teacher / temperature over a row's ids and p
+    that of logits / temperature over the vocabulary, loss = temperature^2 * sum of q (log q - log p).
+
+    Whole vocabulary (vocab_size not given): a dict with 'loss', 'lse' (log of the sum of exp(logits / temperature)),
+    float32, and, if grad_loss is given, 'grad': that of the logits, in the same pass.  `out` may supply tensors
+    of those names; 'grad' may be logits itself.
+
+    A shard of it, as in cross_entropy: a dict with 'lse' over these rows, 'target' (sum of q * logit / temperature over the
+    ids held here) and 'entropy' (-sum of q log q over all of a row's ids, the same on every rank).  loss =
+    temperature^2 * (whole lse - sum over ranks of target - entropy); distillation_grad gives each rank its gradient."""
+    dev = _gpu(logits, "logits")
+    rows, cols, ls = _matrix(logits, "logits", dev, _TYPES)
+    if vocab_size is None and vocab_start:
+        raise _bad("vocab_start needs vocab_size")
+    shape = logits.shape[:-1]
+    given, top, temp = _teacher_args(ids, teacher, temperature, dev, rows, shape, logits.dtype)
+    start, whole = _int64(vocab_start, "vocab_start"), cols if vocab_size is None else _int64(vocab_size, "vocab_size")
+    names = ("loss", "lse") if vocab_size is None else ("lse", "target", "entropy")
+    if vocab_size is not None and grad_loss is not None:
+        raise _bad("a shard's gradient needs the whole vocabulary's lse: use distillation_grad")
+    res = _only(out, names + (("grad",) if grad_loss is not None else ()))
+    stats = _stats(res, names, logits, dev, shape)
+    g, gs, gl = None, 0, None
+    if grad_loss is not None:
+        gl = _vector(grad_loss, "grad_loss", dev, rows, (torch.float32,))
+        res["grad"], gs = _grad_out(res.get("grad"), logits, dev, rows, cols)
+        g = res["grad"].data_ptr()
+    _check(_ops().echo_distillation(logits.data_ptr(), ls, _TYPES[logits.dtype], *given, rows, cols, top, start, whole, temp, *stats,
+                                    gl, g, gs, dev.index, _stream(dev.index)))
+    if out:
+        _written([res[k] for k in out])
+    return res
+
+
+def distillation_grad(logits, ids, teacher, lse, grad_loss, *, temperature=1.0, vocab_start=0, vocab_size=None, out=None):
+    """temperature * (exp(logits / temperature - lse) - q) * grad_loss, like logits: the gradient of distillation for the
+    columns held here, with lse (the whole vocabulary's) and grad_loss float32.  `out` may be logits itself."""
+    dev = _gpu(logits, "logits")
+    rows, cols, ls = _matrix(logits, "logits", dev, _TYPES)
+    if vocab_size is None and vocab_start:
+        raise _bad("vocab_start needs vocab_size")
+    given, top, temp = _teacher_args(ids, teacher, temperature, dev, rows, logits.shape[:-1], logits.dtype)
+    start, whole = _int64(vocab_start, "vocab_start"), cols if vocab_size is None else _int64(vocab_size, "vocab_size")
+    e = _vector(lse, "lse", dev, rows, (torch.float32,))
+    gl = _vector(grad_loss, "grad_loss", dev, rows, (torch.float32,))
+    res, gs = _grad_out(out, logits, dev, rows, cols)
+    _check(_ops().echo_distillation_grad(logits.data_ptr(), ls, _TYPES[logits.dtype], *given, rows, cols, top, start, whole, temp, e, gl,
+                                         res.data_ptr(), gs, dev.index, _stream(dev.index)))
+    if out is not None:
+        _written(out)
+    return res
+
+
+def _head(hidden, weight, vocab_start, vocab_size):
+    """(device, rows, leading shape, the library's matrices, sizes and shard) of a call of the output head."""
+    dev = _gpu(hidden, "hidden")
+    rows, cols, hs = _matrix(hidden, "hidden", dev, _TYPES)
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 2 or weight.shape[1] != cols:
+        raise _bad(f"weight must be a matrix with rows of {cols}")
+    vocab, _, ws = _matrix(weight, "weight", dev, (hidden.dtype,))
+    if vocab_size is None and vocab_start:
+        raise _bad("vocab_start needs vocab_size")
+    start, whole = _int64(vocab_start, "vocab_start"), vocab if vocab_size is None else _int64(vocab_size, "vocab_size")
+    return dev, rows, hidden.shape[:-1], (hidden.data_ptr(), hs, weight.data_ptr(), ws, _TYPES[hidden.dtype]), (rows, cols, vocab), (start, whole)
+
+
+def _head_grads(res, hidden, weight, dev, dtype, accumulate):
+    """Fills res with dhidden and dweight; their addresses, dweight's type and whether it is added to."""
+    if accumulate and "dweight" not in res:
+        raise _bad("accumulate adds to out's dweight")
+    if dtype is None:
+        dtype = res["dweight"].dtype if isinstance(res.get("dweight"), torch.Tensor) else weight.dtype
+    if dtype not in (weight.dtype, torch.float32):
+        raise _bad(f"dtype must be {weight.dtype} or torch.float32 (got {dtype})")
+    res["dhidden"] = _dense(res["dhidden"], "dhidden", dev, hidden.shape, hidden.dtype) if "dhidden" in res else _like(hidden)
+    res["dweight"] = (_dense(res["dweight"], "dweight", dev, weight.shape, dtype) if "dweight" in res
+                      else weight.new_empty(weight.shape, dtype=dtype))
+    return res["dhidden"].data_ptr(), res["dweight"].data_ptr(), _TYPES[dtype], int(bool(accumulate))
+
+
+def _linear_loss(call, names, hidden, weight, given, top, head, vocab_size, grad_loss, dtype, out, accumulate, workspace):
+    dev, rows, shape, mats, sizes, shard = head
+    if vocab_size is not None and grad_loss is not None:
+        raise _bad("a shard's gradients need the whole vocabulary's lse: use the gradient's call")
+    grads = grad_loss is not None
+    if not grads and (dtype is not None or accumulate):
+        raise _bad("dtype and accumulate are of the gradients: give grad_loss")
+    res = _only(out, names + (("dhidden", "dweight") if grads else ()))
+    lse, target, entropy, loss = _stats(res, names, hidden, dev, shape)
+    stats = (lse, target, entropy, loss) if top else (lse, target, loss)
+    gl, more = None, (None, None, mats[4], 0)
+    if grads:
+        gl = _vector(grad_loss, "grad_loss", dev, rows, (torch.float32,))
+        more = _head_grads(res, hidden, weight, dev, dtype, accumulate)
+    L = _ops()
+    space = _space(workspace, L.echo_linear_workspace(*mats, *sizes, len(top) and top[0], 1, int(grads)), hidden)
+    _check(getattr(L, call)(*mats, *given, *sizes, *top, *shard, *stats, gl, *more, *_space_args(space), dev.index, _stream(dev.index)))
+    if out:
+        _written([res[k] for k in out])
+    return res
+
+
+def _linear_grad(call, hidden, weight, given, top, head, lse, grad_loss, dtype, out, accumulate, workspace):
+    dev, rows, shape, mats, sizes, shard = head
+    e = _vector(lse, "lse", dev, rows, (torch.float32,))
+    gl = _vector(grad_loss, "grad_loss", dev, rows, (torch.float32,))
+    res = _only(out, ("dhidden", "dweight"))
+    more = _head_grads(res, hidden, weight, dev, dtype, accumulate)
+    L = _ops()
+    space = _space(workspace, L.echo_linear_workspace(*mats, *sizes, len(top) and top[0], 0, 1), hidden)
+    _check(getattr(L, call)(*mats, *given, *sizes, *top, *shard, e, gl, *more, *_space_args(space), dev.index, _stream(dev.index)))
+    if out:
+        _written([res[k] for k in out])
+    return res
+
+
+def _target_args(targets, dev, rows, shape):
+    if not isinstance(targets, torch.Tensor) or targets.shape != torch.Size(shape):
+        raise _bad("targets must have the leading shape of hidden")
+    return _vector(targets, "targets", dev, rows, _INDEX), _INDEX[targets.dtype]
+
+
+def linear_cross_entropy(hidden, weight, targets, *, vocab_start=0, vocab_size=None, grad_loss=None, dtype=None, out=None,
+                         accumulate=False, workspace=None):
+    """cross_entropy of the logits hidden @ weight.t(), which are not kept: weight is a matrix of the vocabulary's rows, of
+    hidden's type.
+
+    Whole vocabulary: a dict with 'loss' and 'lse' and, if grad_loss (float32, the gradient of each row's loss) is given,
+    'dhidden' like hidden and 'dweight' like weight or of `dtype` (float32).  `out` may supply tensors of those names;
+    with accumulate=True it has to supply 'dweight', which is added to.  A shard (vocab_size given): 'lse' and 'target', as
+    cross_entropy gives them; linear_cross_entropy_grad then gives each rank its gradients.
+
+    16-bit types: the logits' gradient is rounded to hidden's type before the gradients' products, relative to the
+    largest |grad_loss|."""
+    head = _head(hidden, weight, vocab_start, vocab_size)
+    given = _target_args(targets, head[0], head[1], head[2])
+    return _linear_loss("echo_linear_cross_entropy", ("loss", "lse") if vocab_size is None else ("lse", "target"), hidden, weight,
+                        given, (), head, vocab_size, grad_loss, dtype, out, accumulate, workspace)
+
+
+def linear_cross_entropy_grad(hidden, weight, targets, lse, grad_loss, *, vocab_start=0, vocab_size=None, dtype=None, out=None,
+                              accumulate=False, workspace=None):
+    """Gradients of linear_cross_entropy from the whole vocabulary's lse, for the rows of the table held here: a dict with
+    'dhidden' (this shard's share: the ranks' sum is the gradient) and 'dweight'."""
+    head = _head(hidden, weight, vocab_start, vocab_size)
+    given = _target_args(targets, head[0], head[1], head[2])
+    return _linear_grad("echo_linear_cross_entropy_grad", hidden, weight, given, (), head, lse, grad_loss, dtype, out, accumulate,
+                        workspace)
+
+
+def linear_distillation(hidden, weight, ids, teacher, *, temperature=1.0, vocab_start=0, vocab_size=None, grad_loss=None,
+                        dtype=None, out=None, accumulate=False, workspace=None):
+    """distillation of the logits hidden @ weight.t(), which are not kept; tensors and gradients as in
+    linear_cross_entropy, ids, teacher and the statistics of a shard as in distillation."""
+    head = _head(hidden, weight, vocab_start, vocab_size)
+    given, top, temp = _teacher_args(ids, teacher, temperature, head[0], head[1], head[2], hidden.dtype)
+    dev, rows, shape, mats, sizes, shard = head
+    head = dev, rows, shape, mats, sizes, shard + (temp,)
+    return _linear_loss("echo_linear_distillation", ("loss", "lse") if vocab_size is None else ("lse", "target", "entropy"), hidden,
+                        weight, given, (top,), head, vocab_size, grad_loss, dtype, out, accumulate, workspace)
+
+
+def linear_distillation_grad(hidden, weight, ids, teacher, lse, grad_loss, *, temperature=1.0, vocab_start=0, vocab_size=None,
+                             dtype=None, out=None, accumulate=False, workspace=None):
+    """Gradients of linear_distillation from the whole vocabulary's lse, as in linear_cross_entropy_grad."""
+    head = _head(hidden, weight, vocab_start, vocab_size)
+    given, top, temp = _teacher_args(ids, teacher, temperature, head[0], head[1], head[2], hidden.dtype)
+    dev, rows, shape, mats, sizes, shard = head
+    head = dev, rows, shape, mats, sizes, shard + (temp,)
+    return _linear_grad("echo_linear_distillation_grad", hidden, weight, given, (top,), head, lse, grad_loss, dtype, out, accumulate,
+                        workspace)
