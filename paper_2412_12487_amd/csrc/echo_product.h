@@ -75,7 +75,8 @@ struct Feed {
     }
     // starts the loads of a step and goes on to the next
     __device__ __forceinline__ void fetch(char *lds, int wave) {
-        const unsigned records = left > 0xffffffffll ? 0xffffffffu : (unsigned)left;
+        // a step may begin past the operand's end, where the other one is padded further
+        const unsigned records = left > 0xffffffffll ? 0xffffffffu : left < 0 ? 0u : (unsigned)left;
         const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p), 0, records, 0x00020000);
 #pragma unroll
         for (int n = 0; n < LOADS; ++n)
