@@ -84,24 +84,39 @@ struct Feed {
         p += advance;
         left -= advance;
     }
-    // Fragment of the 16 rows from `unit` * 16 and k = half * 32 .. + 31: lane l has row l % 16, k 8 * (l / 16) .. + 7.
-    __device__ __forceinline__ static H8<T> frag(const char *lds, int unit, int half, int lane) {
-        if constexpr (DEEP) {
-            const int r = lane % 16, c = (half * 4 + lane / 16) ^ (r & 7);
-            return *reinterpret_cast<const H8<T> *>(lds + (unit * 16 + r) * 128 + c * 16);
-        } else {
-#ifdef __HIP_DEVICE_COMPILE__      // the builtin is the GPU's
-            const int k = half * 32 + (lane / 16) * 8 + (lane % 16) / 4;
-            const char *at = lds + k * (R * 2) + ((unit ^ (turned(k) & (UNITS - 1))) << 5) + (lane % 4) * 8;
-            typedef __attribute__((address_space(3))) S4 *Lds4;
-            const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)at);
-            const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(at + 4 * R * 2));
-            return __builtin_bit_cast(H8<T>, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#else
-            return H8<T>{};
-#endif
+    // A lane's place in a fragment of 16 rows and 32 of k: it has row lane % 16 and k 8 * (lane / 16) .. + 7.  `first` is the
+    // wavefront's first unit of 16 rows.  Across k, fragments' addresses are xor-ed together where they are read: kept in
+    // registers for both buffers they did not fit (2048 x 51200 x 8192: 2.72 ms with the spills, MEASURED without).
+    struct Reader {
+        unsigned at, mix;
+        __device__ __forceinline__ Reader(int first, int lane) {
+            if constexpr (DEEP) {
+                at = (first * 16 + lane % 16) * 128;
+                mix = ((lane / 16) ^ (lane & 7)) * 16;      // the second half's piece is 4 further: the other one of a pair
+            } else {
+                const int k = (lane / 16) * 8 + (lane % 16) / 4;
+                at = k * (R * 2) + (lane % 4) * 8;
+                mix = ((turned(k) & (UNITS - 1)) ^ first) << 5;
+            }
         }
-    }
+        __device__ __forceinline__ H8<T> frag(const char *lds, int unit, int half) const {
+            if constexpr (DEEP) {
+                return *reinterpret_cast<const H8<T> *>(lds + (at + (mix ^ (half * 64))) + unit * 2048);
+            } else {
+#ifdef __HIP_DEVICE_COMPILE__      // the builtin is the GPU's
+                unsigned m = mix;
+                asm volatile("" : "+v"(m));      // not to be kept for every unit
+                const char *from = lds + (((unit << 5) ^ m) + at);
+                typedef __attribute__((address_space(3))) S4 *Lds4;
+                const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(from + half * (32 * R * 2)));
+                const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(from + half * (32 * R * 2) + 4 * R * 2));
+                return __builtin_bit_cast(H8<T>, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#else
+                return H8<T>{};
+#endif
+            }
+        }
+    };
 };
 
 template <int TI_, int TJ_, int WI_, int WJ_>
@@ -135,8 +150,8 @@ __device__ __forceinline__ void multiply(const Product &m, const Place &at, char
     using FB = Feed<T, S::TJ, BDEEP, S::WAVES>;
     FA fa(m.a, (int64_t)at.ti * S::TI, wave, lane);
     FB fb(m.b, (int64_t)at.tj * S::TJ, wave, lane);
-    const int all = m.steps * m.pairs, begin = (int)((int64_t)all * at.split / m.splits),
-              end = (int)((int64_t)all * (at.split + 1) / m.splits);
+    const int all = m.steps * m.pairs, begin = (int)((unsigned)all * (unsigned)at.split / (unsigned)m.splits),
+              end = (int)((unsigned)all * (unsigned)(at.split + 1) / (unsigned)m.splits);
     int pair = begin / m.steps, step = begin - pair * m.steps;
     fa.seek(plane_a(pair), step);
     fb.seek(plane_b(pair), step);
@@ -154,32 +169,55 @@ __device__ __forceinline__ void multiply(const Product &m, const Place &at, char
     for (int a = 0; a < S::BI; ++a)
 #pragma unroll
         for (int b = 0; b < S::BJ; ++b) acc[a][b] = 0.0f;
-    const auto half = [&](const char *t, int h) {
-        H8<T> x[S::BI], y[S::BJ];
+    const typename FA::Reader ra(wi * S::BI, lane);
+    const typename FB::Reader rb(wj * S::BJ, lane);
+    // A step is 2 * BI items, each a fragment of a with the BJ fragments of b of its half.  Fragments of a are read AHEAD items before
+    // their turn, those of b a half before; so the last items of a step read what follows.  In front of them stands
+    // the barrier, which says two things: the next step is in shared memory for everybody (each wavefront has waited for
+    // its own loads), and everybody has read all of this one, whose buffer takes the step after the next.
+    constexpr int ITEMS = 2 * S::BI, AHEAD = 4, HELD = 8;
+    static_assert(S::BJ == AHEAD && S::BI >= AHEAD && ITEMS % HELD == 0, "one fragment of b an item");
+    H8<T> x[HELD], y[2][S::BJ];
+    const auto turn = [&](char *mine, char *next, bool goes_on, bool more) {
 #pragma unroll
-        for (int a = 0; a < S::BI; ++a) x[a] = FA::frag(t, wi * S::BI + a, h, lane);
+        for (int i = 0; i < ITEMS; ++i) {
+            if (i == ITEMS - AHEAD && goes_on) {
+                __builtin_amdgcn_s_waitcnt(0x0070);      // vmcnt(0), lgkmcnt(0)
+                __syncthreads();
+            }
+            if (i < S::BJ) y[1][i] = rb.frag(mine + FA::BYTES, i, 1);
+            if (i < ITEMS - AHEAD) {
+                x[(i + AHEAD) % HELD] = ra.frag(mine, (i + AHEAD) % S::BI, (i + AHEAD) / S::BI);
+            } else if (goes_on) {
+                y[0][i - (ITEMS - AHEAD)] = rb.frag(next + FA::BYTES, i - (ITEMS - AHEAD), 0);
+                x[(i + AHEAD) % HELD] = ra.frag(next, i - (ITEMS - AHEAD), 0);
+            }
 #pragma unroll
-        for (int b = 0; b < S::BJ; ++b) y[b] = FB::frag(t + FA::BYTES, wj * S::BJ + b, h, lane);
-#pragma unroll
-        for (int a = 0; a < S::BI; ++a)
-#pragma unroll
-            for (int b = 0; b < S::BJ; ++b) acc[a][b] = mfma(x[a], y[b], acc[a][b]);
+            for (int b = 0; b < S::BJ; ++b)
+                acc[i % S::BI][b] = mfma(x[i % HELD], y[i / S::BI][b], acc[i % S::BI][b]);
+            if (i == ITEMS - AHEAD && more) fetch(mine);
+            __builtin_amdgcn_sched_barrier(0);      // the order is meant
+        }
     };
-    // The barrier says two things: the step that begins is in shared memory for everybody (each wavefront has waited for its own
-    // loads), and everybody has read the buffer that is filled next.
-    const auto turn = [&](char *mine, char *next, bool more) {
-        __syncthreads();
-        if (more) fetch(next);
-        half(mine, 0);
-        half(mine, 1);
-    };
-    if (begin < end) fetch(t0);
     int s = begin;
-    for (; s + 1 < end; s += 2) {
-        turn(t0, t1, true);
-        turn(t1, t0, s + 2 < end);
+    if (s < end) {
+        fetch(t0);
+        __builtin_amdgcn_s_waitcnt(0x0070);
+        __syncthreads();
+        if (s + 1 < end) fetch(t1);
+#pragma unroll
+        for (int b = 0; b < S::BJ; ++b) y[0][b] = rb.frag(t0 + FA::BYTES, b, 0);
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) x[a] = ra.frag(t0, a, 0);
     }
-    if (s < end) turn(t0, t1, false);
+    for (; s + 3 < end; s += 2) {
+        turn(t0, t1, true, true);
+        turn(t1, t0, true, true);
+    }
+    for (; s < end; s += 2) {
+        turn(t0, t1, s + 1 < end, s + 2 < end);
+        if (s + 1 < end) turn(t1, t0, s + 2 < end, false);
+    }
 }
 
 }  // namespace
