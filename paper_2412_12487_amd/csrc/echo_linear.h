@@ -16,19 +16,33 @@ struct HeadArgs {
     const int *local;             // [rows][top]: an entry's column here, or -1
     const float *q;               // [rows][top]
     const float2 *prior;          // [rows]: sum of q log q, and 1 where the row is trained on
-    float2 *stats;                // [tiles][rows]: maximum, and sum relative to it
+    float2 *stats;                // [parts][rows]: maximum, and sum relative to it, of a wavefront's columns
     float *hits;                  // logits of the target or of the entries
     const float *lse, *grad_loss, *scale;
-    char *prob;                   // [planes][prob_rows][prob_cols]
+    char *prob;                   // [planes][prob_rows][.]: the gradient's shares
     int64_t prob_stride, prob_plane;
-    int prob_rows, prob_cols;
+    int prob_rows, prob_cols;     // columns that are written, from the product's first on
+    void *kept;                   // [rows][kept_stride]: exponentials
+    int64_t kept_stride;
+};
+struct ShareArgs {
+    const float2 *stats, *prior;
+    const float *hits, *q, *lse, *grad_loss, *scale;
+    const int *local;
+    const void *targets, *kept;
+    int wide_index, top, rows, vocab, cols;
+    int64_t vocab_start, vocab_size;
+    int split, part0, part1;      // columns that a part of the statistics has, before `split` and from it on
+    char *prob;                   // [planes][prob_rows][cols]
+    int64_t prob_stride, prob_plane;
+    int prob_rows;
 };
 struct JoinArgs {
     const float2 *stats, *prior;
     const float *hits, *q;
     const int *local;
     const void *targets;
-    int wide_index, top, rows, vocab, tiles;
+    int wide_index, top, rows, vocab, parts;
     int64_t vocab_start, vocab_size;
     float square;                 // T^2
     float *lse, *target, *entropy, *loss;
@@ -55,6 +69,7 @@ struct OutArgs {
     const float *scale;
     float factor;
     float *parts;                 // [splits][nj][ni] of 32 bits, or null: D is whole
+    int64_t part;                 // elements from a part to the next
     bool add_parts;               // parts are added to
     void *out;                    // [nj][ni]
     bool accumulate;
@@ -79,6 +94,22 @@ template <class T>
 constexpr float kUnit = 1.0f;
 template <>
 constexpr float kUnit<f16> = 16384.0f;
+// What the exponentials of a row are kept as between the loss's pass and the gradient's: of bfloat16 as half
+// precision, 2^15 times as large, whose rounding of 2^-11 is small beside that to bfloat16 (2^-8) and
+// whose smallest step is 2^-39; of the others in 32 bits, since a second rounding of half precision would
+// be as large as the first.
+template <class T, int PLANES>
+struct KeptOf {
+    using type = float;
+};
+template <>
+struct KeptOf<bf16, 1> {
+    using type = f16;
+};
+template <class T, int PLANES>
+using Kept = typename KeptOf<T, PLANES>::type;
+template <class T, int PLANES>
+constexpr float kKeptUnit = sizeof(Kept<T, PLANES>) == 2 ? 32768.0f : 1.0f;
 }  // namespace
 
 // deep: b's sum runs along its rows (the hidden states' gradient), or across them (the table's)

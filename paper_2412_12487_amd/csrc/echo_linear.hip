@@ -53,9 +53,11 @@ struct Cells {
 };
 
 // Tiles of logits, i over the vocabulary and j over the rows.
-//   GRAD false: each row's maximum and sum of exponentials over the tile's columns, and the logits of its target or entries.
-//   GRAD true: the gradient's share of each logit, (exp(x / T - lse) - q) * grad_loss / scale, rounded to T.
-template <class T, class S, bool GRAD, int PLANES>
+//   kLoss: each row's maximum and sum of exponentials over a wavefront's columns, and the logits of its target or entries.
+//   kKeep: the same, and the exponentials, relative to that maximum.
+//   kGrad: the gradient's share of each logit, (exp(x / T - lse) - q) * grad_loss / scale, rounded to T.
+enum { kLoss, kKeep, kGrad };
+template <class T, class S, int MODE, int PLANES>
 __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArgs a) {
     __shared__ __attribute__((aligned(16))) char t0[S::BYTES];
     __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
@@ -66,15 +68,14 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
     const int wi = wave / S::WJ, wj = wave % S::WJ;
     const int i0 = at.ti * S::TI, j0 = at.tj * S::TJ, il = wi * S::BI * 16 + (lane / 16) * 4, jl = wj * S::BJ * 16 + lane % 16;
     const Cells<S> cells{t0, t1};
-    if (a.top) cells.fill(a, a.first + i0, j0);
+    if (a.top) cells.fill(a, a.first + i0, j0);      // entries' columns count from the shard's first id
     using Quad = __attribute__((ext_vector_type(4))) unsigned short;
-    if constexpr (!GRAD) {
-        float2 mine[S::BJ];
+    if constexpr (MODE != kGrad) {
 #pragma unroll
         for (int b = 0; b < S::BJ; ++b) {
             const int n = j0 + jl + b * 16;
             const bool live = n < a.rows;
-            const int hit = live && !a.top ? row_of(a, n).at : -1;
+            const int hit = live && !a.top ? row_of(a, n).at - a.first : -1;      // below 0 where it is not here
             float top = -kInf;
 #pragma unroll
             for (int k = 0; k < S::BI; ++k) {
@@ -98,30 +99,23 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
             const float base = top == -kInf ? 0.0f : top;
             float sum = 0.0f;
 #pragma unroll
-            for (int k = 0; k < S::BI; ++k)
+            for (int k = 0; k < S::BI; ++k) {
+                F4 d;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum += exp_of(acc[k][b][e] - base);
+                for (int e = 0; e < 4; ++e) sum += d[e] = exp_of(acc[k][b][e] - base);
+                if constexpr (MODE == kKeep) {
+                    using K = Kept<T, PLANES>;
+                    const int v = i0 + il + k * 16;
+                    if (live && v < a.prob_cols) {
+                        typedef __attribute__((ext_vector_type(4))) K K4;
+                        *reinterpret_cast<K4 *>(static_cast<K *>(a.kept) + n * a.kept_stride + v) =
+                            __builtin_convertvector(d * kKeptUnit<T, PLANES>, K4);
+                    }
+                }
+            }
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
-            mine[b] = make_float2(top, sum);
-        }
-        __syncthreads();
-        float2 *part = reinterpret_cast<float2 *>(t0);      // [WI][TJ]
-#pragma unroll
-        for (int b = 0; b < S::BJ; ++b)
-            if (lane < 16) part[wi * S::TJ + jl + b * 16] = mine[b];
-        __syncthreads();
-        for (int j = threadIdx.x; j < S::TJ; j += S::THREADS) {
-            if (j0 + j >= a.rows) continue;
-            float top = -kInf, sum = 0.0f;
-#pragma unroll
-            for (int w = 0; w < S::WI; ++w) top = fmaxf(top, part[w * S::TJ + j].x);
-#pragma unroll
-            for (int w = 0; w < S::WI; ++w) {
-                const float2 p = part[w * S::TJ + j];
-                sum += p.x == -kInf ? p.y : p.y * exp_of(p.x - top);      // p.y is 0 there, or NaN
-            }
-            a.stats[(int64_t)at.ti * a.rows + j0 + j] = make_float2(top, sum);
+            if (live && lane < 16) a.stats[((int64_t)at.ti * S::WI + wi) * a.rows + n] = make_float2(top, sum);
         }
     } else {
         const float scale = *a.scale;
@@ -133,8 +127,7 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
             float lse = 0.0f, g = 0.0f;
             if (live) {
                 const Row r = row_of(a, n);
-                hit = r.at - a.first;
-                if (r.at < 0) hit = -1;
+                hit = r.at - a.first;      // below 0 where it is not here
                 lse = a.lse[n];
                 live = r.trained && lse != -kInf;
                 g = a.grad_loss[n] / scale * kUnit<T>;
@@ -170,14 +163,81 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
     }
 }
 
-// Joins the tiles' statistics of 16 rows: lanes of 16 over the rows, 64 over the tiles.
+// The gradient's shares from the exponentials that the loss's pass kept, in place where they are of 16 bits; where the target
+// is or the teacher has a mass, from the logit itself.  A workgroup takes a stretch of one row.
+// Memory bounds it, and it spares the second product of the logits: MEASURED.
+constexpr int kSpan = 256 * 8 * 2;
+template <class T, int PLANES>
+__global__ __launch_bounds__(256) void k_shares(ShareArgs a) {
+    using K = Kept<T, PLANES>;
+    const int spans = (a.cols + kSpan - 1) / kSpan;
+    const float most = *a.scale;
+    for (int64_t id = blockIdx.x; id < (int64_t)a.prob_rows * spans; id += gridDim.x) {
+        const int n = (int)(id / spans), from = (int)(id - (int64_t)n * spans) * kSpan;
+        bool live = n < a.rows;
+        float lse = 0.0f, g = 0.0f;
+        int hit = -1;
+        if (live) {
+            lse = a.lse[n];
+            g = a.grad_loss[n] / most * kUnit<T>;
+            bool trained;
+            if (a.top) {
+                trained = a.prior[n].y > 0.0f;
+            } else {
+                const int64_t t = a.wide_index ? id_at<int64_t>(a.targets, n) : id_at<int32_t>(a.targets, n);
+                trained = t >= 0 && t < a.vocab_size;
+                hit = trained ? shard_row(t, a.vocab_start, a.vocab) : -1;
+            }
+            live = trained && lse != -kInf;
+        }
+        const auto put = [&](int c, auto d) {
+            constexpr int N = sizeof(d) / 4;
+            char *out = a.prob + n * a.prob_stride + c * 2;
+#pragma unroll
+            for (int plane = 0; plane < PLANES; ++plane) {
+                const V<T, N> h = round_to<T, N>(d);
+                *reinterpret_cast<V<T, N> *>(out + plane * a.prob_plane) = h;
+                if (plane + 1 < PLANES) d -= widen<T, N>(h);
+            }
+        };
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int c = from + (k * 256 + threadIdx.x) * 8;
+            if (c >= a.cols) continue;
+            F<8> d = 0.0f;
+            if (live) {
+                const int part = c < a.split ? c / a.part0 : a.split / a.part0 + (c - a.split) / a.part1;
+                const float top = a.stats[(int64_t)part * a.rows + n].x;
+                d = widen<K, 8>(*reinterpret_cast<const V<K, 8> *>(static_cast<const K *>(a.kept) + (int64_t)n * a.cols + c)) *
+                    (exp_of(top - lse) * g / kKeptUnit<T, PLANES>);
+                if ((unsigned)(hit - c) < 8u) {
+                    const float p = (exp_of(a.hits[n] - lse) - 1.0f) * g;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) d[j] = c + j == hit ? p : d[j];
+                }
+            }
+            put(c, d);
+        }
+        if (!a.top) continue;
+        __threadfence_block();
+        __syncthreads();      // what the entries are written over has arrived
+        if (!live) continue;
+        for (int k = threadIdx.x; k < a.top; k += 256) {
+            const int64_t e = (int64_t)n * a.top + k;
+            const int c = a.local[e];
+            if ((unsigned)(c - from) < (unsigned)kSpan && c >= 0) put(c, F<1>((exp_of(a.hits[e] - lse) - a.q[e]) * g));
+        }
+    }
+}
+
+// Joins the parts' statistics of 16 rows: lanes of 16 over the rows, 64 over the parts.
 __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
     __shared__ float2 part[64][17];
     const int r = threadIdx.x % 16, w = threadIdx.x / 16;
     const int n = blockIdx.x * 16 + r;
     float top = -kInf, sum = 0.0f;
     if (n < a.rows) {
-        for (int t = w; t < a.tiles; t += 64) {
+        for (int t = w; t < a.parts; t += 64) {
             const float2 p = a.stats[(int64_t)t * a.rows + n];
             const float m = fmaxf(top, p.x);
             sum = (top == -kInf ? sum : sum * exp_of(top - m)) + (p.x == -kInf ? p.y : p.y * exp_of(p.x - m));
@@ -303,13 +363,13 @@ __global__ __launch_bounds__(256) void k_layout(LayoutArgs a) {
     }
 }
 
-template <class T, bool GRAD, int PLANES>
+template <class T, int MODE, int PLANES>
 hipError_t logits(const HeadArgs &a, int shape, hipStream_t s) {
     const dim3 grid(a.m.tiles_i * a.m.tiles_j);
     switch (shape) {
-        case 0: return launch(k_logits<T, Wide, GRAD, PLANES>, grid, dim3(Wide::THREADS), s, a);
-        case 1: return launch(k_logits<T, Middle, GRAD, PLANES>, grid, dim3(Middle::THREADS), s, a);
-        default: return launch(k_logits<T, Thin, GRAD, PLANES>, grid, dim3(Thin::THREADS), s, a);
+        case 0: return launch(k_logits<T, Wide, MODE, PLANES>, grid, dim3(Wide::THREADS), s, a);
+        case 1: return launch(k_logits<T, Middle, MODE, PLANES>, grid, dim3(Middle::THREADS), s, a);
+        default: return launch(k_logits<T, Thin, MODE, PLANES>, grid, dim3(Thin::THREADS), s, a);
     }
 }
 template <class I>
@@ -322,10 +382,10 @@ hipError_t teacher(const TeacherArgs &a, int type, hipStream_t s) {
     }
 }
 
-hipError_t launch_logits(const HeadArgs &a, int type, bool grad, int shape, hipStream_t s) {
-    if (type == ECHO_F16) return grad ? logits<f16, true, 1>(a, shape, s) : logits<f16, false, 1>(a, shape, s);
-    if (!grad) return logits<bf16, false, 1>(a, shape, s);
-    return type == ECHO_F32 ? logits<bf16, true, 3>(a, shape, s) : logits<bf16, true, 1>(a, shape, s);
+template <class T, int PLANES>
+hipError_t logits(const HeadArgs &a, int mode, int shape, hipStream_t s) {
+    return mode == kGrad ? logits<T, kGrad, PLANES>(a, shape, s)
+                         : mode == kKeep ? logits<T, kKeep, PLANES>(a, shape, s) : logits<T, kLoss, 1>(a, shape, s);
 }
 hipError_t launch_join(const JoinArgs &a, hipStream_t s) { return launch(k_join, dim3((a.rows + 15) / 16), dim3(1024), s, a); }
 hipError_t launch_teacher(const TeacherArgs &a, int type, int index_type, hipStream_t s) {
@@ -343,21 +403,48 @@ hipError_t launch_layout(const LayoutArgs &a, int type, hipStream_t s) {
     }
 }
 
+hipError_t launch_shares(const ShareArgs &a, int type, hipStream_t s) {
+    const dim3 grid(grid_of((int64_t)a.prob_rows * ((a.cols + kSpan - 1) / kSpan)));
+    switch (type) {
+        case ECHO_F32: return launch(k_shares<bf16, 3>, grid, dim3(256), s, a);
+        case ECHO_F16: return launch(k_shares<f16, 1>, grid, dim3(256), s, a);
+        default: return launch(k_shares<bf16, 1>, grid, dim3(256), s, a);
+    }
+}
+
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 int tiles(int64_t n, int t) { return (int)((n + t - 1) / t); }
 
-// How full `wg` workgroups leave a launch's last round, of 256 or 512 at a time.
-double full(int64_t wg, int at_once) { return (double)wg / (double)up(wg, at_once); }
-// Shape of a product's tiles: wide ones do the most work for what they read, and middle ones fill the GPU where there
-// are few.  Thin ones (logits alone) are for up to 64 rows.
-int shape_of(int64_t ni, int64_t nj, bool thin) {
-    if (thin && nj <= 64) return 2;
-    const int64_t wide = (int64_t)tiles(ni, 256) * tiles(nj, 256), middle = (int64_t)tiles(ni, 128) * tiles(nj, 128);
-    return full(wide, 256) >= 0.75 * full(middle, 512) ? 0 : 1;
+// Shapes of a product's tiles along one of its sides: `shape0` up to `split`, `shape1` from there on.
+//
+// Wide tiles do the most work for what they read, one on a compute unit at a time; where they leave the launch's last round
+// mostly empty, what is left of the side after the full rounds takes middle ones, two on a compute unit.  Costs in
+// units of a wide tile's time: CALIBRATED.  Thin tiles (logits alone) are for up to 64 rows.
+struct Ranges {
+    int split, shape0, shape1;
+};
+int side(int shape) { return shape == 1 ? 128 : 256; }
+double middle_cost(int64_t n, int64_t other) {
+    const int64_t t = (int64_t)tiles(n, 128) * tiles(other, 128), rest = t % 512;
+    return (double)(t / 512) * 0.62 + (rest > 256 ? 0.62 : rest ? 0.42 : 0.0);
 }
-void tile(Product &m, int shape) {
-    m.tiles_i = tiles(m.ni, shape == 1 ? 128 : 256);
-    m.tiles_j = tiles(m.nj, shape == 0 ? 256 : shape == 1 ? 128 : 64);
+Ranges ranges_of(int64_t n, int64_t other) {
+    const int64_t across = tiles(other, 256), along = tiles(n, 256);
+    const double wide = (double)((along * across + 255) / 256), middle = middle_cost(n, other);
+    const int64_t whole = along * across / 256 * 256 / across;      // tiles along the side in full rounds
+    const double mixed = whole > 0 && whole < along
+                             ? (double)((whole * across + 255) / 256) + middle_cost(n - whole * 256, other) + 0.05
+                             : wide + middle;
+    if (middle < wide && middle <= mixed) return Ranges{(int)n, 1, 1};
+    return mixed < wide ? Ranges{(int)whole * 256, 0, 1} : Ranges{(int)n, 0, 0};
+}
+Ranges logits_ranges(int64_t n, int64_t rows) { return rows <= 64 ? Ranges{(int)n, 2, 2} : ranges_of(n, rows); }
+// Columns of a part of the logits' statistics: what one wavefront of a tile has.
+int part_of(int shape) { return shape == 0 ? Wide::TI / Wide::WI : shape == 1 ? Middle::TI / Middle::WI : Thin::TI / Thin::WI; }
+int parts_of(int n, int shape) { return shape == 1 ? tiles(n, 128) * Middle::WI : tiles(n, 256) * (shape ? Thin::WI : Wide::WI); }
+void tile(Product &m, int ni, int nj, int shape) {
+    m.tiles_i = tiles(ni, side(shape));
+    m.tiles_j = tiles(nj, shape == 2 ? 64 : side(shape));
 }
 
 constexpr int64_t kProbBytes = int64_t(1) << 30;      // of the logits' gradient at a time
@@ -368,11 +455,14 @@ struct Plan {
     int planes, pairs;
     int width;                     // hidden size in whole steps
     bool copy_hidden, copy_weight;
-    int logits_shape, stats_tiles; // the loss's
+    Ranges logits;                 // the loss's
+    int stats_parts;
+    bool keep;                     // the loss's pass keeps its exponentials for the gradient
     int64_t prob_rows, prob_cols, pieces;
-    int hidden_shape, splits;      // the hidden states' gradient
+    Ranges out;                    // the hidden states' gradient
+    int splits;
     bool parts;
-    int64_t hidden, weight, stats, hits, local, q, prior, scale, prob, part, bytes;
+    int64_t hidden, weight, stats, hits, local, q, prior, scale, prob, kept, part, bytes;
 };
 bool direct(const void *p, int64_t stride, int type, int cols) {
     return type != ECHO_F32 && cols % kDepth == 0 && stride % 8 == 0 && stride <= int64_t(1) << 22 && (uintptr_t)p % 16 == 0;
@@ -397,9 +487,10 @@ Plan plan_of(const LinearArgs &a) {
         p.prior = take(a.rows * 8);
     }
     if (a.forward) {
-        p.logits_shape = shape_of(a.vocab, a.rows, true);
-        p.stats_tiles = tiles(a.vocab, p.logits_shape == 1 ? 128 : 256);
-        p.stats = take(p.stats_tiles * a.rows * 8);
+        p.logits = logits_ranges(a.vocab, a.rows);
+        p.stats_parts = parts_of(p.logits.split, p.logits.shape0);
+        if (p.logits.split < a.vocab) p.stats_parts += parts_of(a.vocab - p.logits.split, p.logits.shape1);
+        p.stats = take(p.stats_parts * a.rows * 8);
         p.hits = take(a.rows * (a.top ? a.top : 1) * 4);
     }
     if (a.grads) {
@@ -411,12 +502,15 @@ Plan plan_of(const LinearArgs &a) {
         p.pieces = (whole + most - 1) / most;
         p.prob_cols = p.pieces == 1 ? whole : up((whole + p.pieces - 1) / p.pieces, 256);
         p.prob = take(p.prob_rows * p.prob_cols * 2 * p.planes);
-        p.hidden_shape = shape_of(a.cols, a.rows, false);
-        const int t = p.hidden_shape ? 128 : 256, at_once = p.hidden_shape ? 512 : 256;
-        const int64_t wg = (int64_t)tiles(a.cols, t) * tiles(a.rows, t), steps = p.prob_cols / kDepth * p.pairs;
-        int64_t splits = wg >= at_once ? 1 : at_once / wg;
+        p.keep = a.forward && p.pieces == 1;
+        if (p.keep) p.kept = a.type == ECHO_BF16 ? p.prob : take(a.rows * p.prob_cols * 4);
+        const int64_t middle = (int64_t)tiles(a.cols, 128) * tiles(a.rows, 128), steps = p.prob_cols / kDepth * p.pairs;
+        p.out = ranges_of(a.rows, a.cols);
+        // too few tiles to fill the GPU: workgroups take parts of the sum
+        int64_t splits = middle < 512 ? 512 / middle : 1;
         if (splits > steps / 4) splits = steps / 4;
         p.splits = splits < 1 ? 1 : (int)splits;
+        if (p.splits > 1) p.out = Ranges{(int)a.rows, 1, 1};
         p.parts = p.splits > 1 || p.pieces > 1;
         if (p.parts) p.part = take(p.splits * a.rows * a.cols * 4);
     }
@@ -432,6 +526,57 @@ int64_t linear_bytes(const LinearArgs &a) { return plan_of(a).bytes; }
         const hipError_t e_ = (call);         \
         if (e_ != hipSuccess) return e_;      \
     } while (0)
+
+namespace {
+
+// Logits of the columns from h.first on (h.m.a begins there): h.m.ni of them, and zeros of the gradient up to `cover`.
+hipError_t run_logits(const HeadArgs &head, int type, int mode, int cover, const Ranges &r, hipStream_t s) {
+    for (int from = 0, to; from < cover; from = to) {
+        to = from || r.split >= head.m.ni ? cover : r.split;
+        const int shape = from ? r.shape1 : r.shape0;
+        HeadArgs h = head;
+        h.m.a.p += from * h.m.a.stride;
+        h.m.a.rows -= from;
+        h.m.ni = (to < head.m.ni ? to : head.m.ni) - from;
+        h.first += from;
+        h.prob_cols = to - from;
+        if (h.prob) h.prob += (int64_t)from * 2;
+        if (h.kept) h.kept = static_cast<char *>(h.kept) + (int64_t)from * (type == ECHO_BF16 ? 2 : 4);
+        if (from) h.stats += (int64_t)parts_of(from, r.shape0) * h.rows;
+        tile(h.m, to - from, h.m.nj, shape);
+        hipError_t e;
+        switch (type) {
+            case ECHO_F32: e = logits<bf16, 3>(h, mode, shape, s); break;
+            case ECHO_F16: e = logits<f16, 1>(h, mode, shape, s); break;
+            default: e = logits<bf16, 1>(h, mode, shape, s); break;
+        }
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+// D of a product along j.
+hipError_t run_out(const OutArgs &all, int type, int out_type, bool deep, const Ranges &r, hipStream_t s) {
+    const int64_t elem = out_type == ECHO_F32 ? 4 : 2;
+    for (int from = 0, to; from < all.m.nj; from = to) {
+        to = from ? all.m.nj : r.split;
+        const int shape = from ? r.shape1 : r.shape0;
+        OutArgs o = all;
+        o.m.nj = to - from;
+        o.m.b.p += deep ? from * o.m.b.stride : (int64_t)from * 2;
+        if (deep)
+            o.m.b.rows -= from;
+        else
+            o.m.b.width -= from;
+        o.out = static_cast<char *>(o.out) + (int64_t)from * o.m.ni * elem;
+        if (o.parts) o.parts += (int64_t)from * o.m.ni;
+        tile(o.m, o.m.ni, o.m.nj, shape);
+        const hipError_t e = launch_out(o, type, out_type, deep, shape, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
 
 hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
     if (!a.rows) return launch_zero(a.dweight, (int64_t)a.vocab * a.cols * (a.grad_type == ECHO_F32 ? 4 : 2), s);
@@ -470,10 +615,11 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
     if (a.forward) {
         h.stats = reinterpret_cast<float2 *>(w + p.stats);
         h.hits = reinterpret_cast<float *>(w + p.hits);
-        tile(h.m, p.logits_shape);
-        ECHO_HIP(launch_logits(h, a.type, false, p.logits_shape, s));
+        h.kept = p.keep ? w + p.kept : nullptr;
+        h.kept_stride = p.prob_cols;
+        ECHO_HIP(run_logits(h, a.type, p.keep ? kKeep : kLoss, p.keep ? (int)p.prob_cols : a.vocab, p.logits, s));
         ECHO_HIP(launch_join(JoinArgs{h.stats, h.prior, h.hits, h.q, h.local, h.targets, h.wide_index, h.top, h.rows, h.vocab,
-                                      p.stats_tiles, h.vocab_start, h.vocab_size, a.temperature * a.temperature, a.lse, a.target,
+                                      p.stats_parts, h.vocab_start, h.vocab_size, a.temperature * a.temperature, a.lse, a.target,
                                       a.entropy, a.loss}, s));
     }
     if (!a.grads) return hipSuccess;
@@ -488,7 +634,6 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
     ECHO_HIP(launch_scale(a.grad_loss, h.rows, reinterpret_cast<float *>(w + p.scale), s));
     const Operand prob{h.prob, h.prob_stride, h.prob_plane, p.prob_rows, (int)p.prob_cols};
     const int64_t grad_elem = a.grad_type == ECHO_F32 ? 4 : 2;
-    const int out_type = a.type;
     float *parts = p.parts ? reinterpret_cast<float *>(w + p.part) : nullptr;
     for (int64_t piece = 0; piece < p.pieces; ++piece) {
         const int64_t first = piece * p.prob_cols, left = a.vocab - first;
@@ -499,33 +644,31 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         h.first = (int)first;
         h.m.a = table;
         h.m.ni = n;
-        // the tiles fill the piece's columns, past the vocabulary's end too
-        const int shape = shape_of(p.prob_cols, a.rows, true);
-        Product cover = h.m;
-        cover.ni = (int)p.prob_cols;
-        tile(cover, shape);
-        h.m.tiles_i = cover.tiles_i;
-        h.m.tiles_j = cover.tiles_j;
-        ECHO_HIP(launch_logits(h, a.type, true, shape, s));
+        if (p.keep) {
+            const ShareArgs c{h.stats, h.prior, h.hits, h.q, h.lse, h.grad_loss, h.scale, h.local, h.targets, w + p.kept, h.wide_index,
+                              h.top, h.rows, h.vocab, (int)p.prob_cols, h.vocab_start, h.vocab_size, p.logits.split,
+                              part_of(p.logits.shape0), part_of(p.logits.shape1), h.prob, h.prob_stride, h.prob_plane, h.prob_rows};
+            ECHO_HIP(launch_shares(c, a.type, s));
+        } else {
+            ECHO_HIP(run_logits(h, a.type, kGrad, (int)p.prob_cols, logits_ranges(p.prob_cols, a.rows), s));
+        }
         OutArgs o{};
         o.scale = h.scale;
         o.factor = a.temperature;
         o.m = Product{table, prob, a.cols, (int)a.rows, 0, 0, (int)(p.prob_cols / kDepth), p.pairs, p.splits};
         o.parts = parts;
+        o.part = a.rows * a.cols;
         o.add_parts = piece > 0;
         o.out = a.dhidden;
-        tile(o.m, p.hidden_shape);
-        ECHO_HIP(launch_out(o, a.type, out_type, true, p.hidden_shape, s));
+        ECHO_HIP(run_out(o, a.type, a.type, true, p.out, s));
         o.m = Product{hidden, prob, a.cols, n, 0, 0, (int)(p.prob_rows / kDepth), p.pairs, 1};
         o.parts = nullptr;
         o.out = static_cast<char *>(a.dweight) + first * a.cols * grad_elem;
         o.accumulate = a.accumulate;
-        const int table_shape = shape_of(a.cols, n, false);
-        tile(o.m, table_shape);
-        ECHO_HIP(launch_out(o, a.type, a.grad_type, false, table_shape, s));
+        ECHO_HIP(run_out(o, a.type, a.grad_type, false, ranges_of(n, a.cols), s));
     }
     if (parts)
-        ECHO_HIP(launch_gather(GatherArgs{parts, a.rows * a.cols, p.splits, h.scale, a.temperature, a.dhidden}, a.type, out_type, s));
+        ECHO_HIP(launch_gather(GatherArgs{parts, a.rows * a.cols, p.splits, h.scale, a.temperature, a.dhidden}, a.type, a.type, s));
     return hipSuccess;
 }
 

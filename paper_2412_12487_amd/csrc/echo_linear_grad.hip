@@ -41,7 +41,7 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_out(OutArgs a)
             if (i >= a.m.ni) continue;
             const F4 d = acc[k][b] * scale;
             if (a.parts)
-                put4(a.parts + ((int64_t)at.split * a.m.nj + j) * a.m.ni + i, a.m.ni - i, d, a.add_parts);
+                put4(a.parts + at.split * a.part + (int64_t)j * a.m.ni + i, a.m.ni - i, d, a.add_parts);
             else
                 put4(static_cast<U *>(a.out) + (int64_t)j * a.m.ni + i, a.m.ni - i, d, a.accumulate);
         }

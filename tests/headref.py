@@ -39,10 +39,11 @@ def teacher(ids, z, whole, temp):
     return q, q * rel, plogp.sum(1), e_prior, trained
 
 
-def loss(x, e_x, ids, q, e_q, prior, e_prior, trained, start, whole, temp, lse=None, grad_loss=None):
+def loss(x, e_x, ids, q, e_q, prior, e_prior, trained, start, whole, temp, lse=None, grad_loss=None, kept=False):
     """{name: (value, bound)} for logits x (already divided by temp) that are off by e_x, entries `ids` of masses q.
 
-    lse: the whole vocabulary's as given (32 bits, taken as it is), else the rows' own."""
+    lse: the whole vocabulary's as given (32 bits, taken as it is), else the rows' own.  kept: exponentials are held as half
+    precision (2^-11), 2^15 times as large (half a smallest step is 2^-40 of their part's largest, and that at most 1)."""
     rows, cols = x.shape
     own = torch.logsumexp(x, 1)
     top = torch.where(torch.isfinite(x), x, -math.inf).max(1).values
@@ -77,6 +78,8 @@ def loss(x, e_x, ids, q, e_q, prior, e_prior, trained, start, whole, temp, lse=N
         far = x - lse[:, None]
         p = torch.exp(far)
         e_p = torch.where(p > 0, p * (e_x + e_l[:, None] + 16 * U + 4 * U * far.abs() + 2 * U * x.abs()), 0.0)
+        if kept:
+            e_p = e_p + p * 2.0 ** -11 + 2.0 ** -40
         mass = torch.zeros_like(x).scatter_add_(1, at, torch.where(here, q, 0.0))
         e_mass = torch.zeros_like(x).scatter_add_(1, at, torch.where(here, e_q + 4 * U * q, 0.0))
         live = (trained & (lse != -math.inf))[:, None]
@@ -111,7 +114,7 @@ def linear(hidden, weight, given, start, whole, temp=1.0, lse=None, grad_loss=No
     x, e_x = product(h, w.t(), t)
     x, e_x = x / temp, e_x / temp + 2 * U * (x / temp).abs()
     e_x = torch.nan_to_num(e_x, nan=0.0, posinf=0.0)
-    out = loss(x, e_x, *given, start, whole, temp, lse, grad_loss)
+    out = loss(x, e_x, *given, start, whole, temp, lse, grad_loss, kept=t == torch.bfloat16 and lse is None)
     if grad_loss is None:
         return out
     d, e_d = out.pop("grad")
