@@ -2,68 +2,22 @@
 //
 // Per row, at temperature T: q = softmax of the teacher's logits / T over its ids in the vocabulary, p = softmax of the
 // logits / T over the vocabulary, loss = T^2 sum q (log q - log p), and the logits' gradient T (p - q) grad_loss.
-#include "echo_ops_device.h"
+#include "echo_teacher.h"
 
 namespace echo {
 namespace {
 
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
-
-// An entry of the teacher: its column here (or -1), the mass of its id, which the first entry of an id holds, and the
-// logit of it / T.  One wavefront prepares a row's entries, and each lane reads again only what it wrote itself.
-struct Entry {
-    int at;
-    float mass, x;
-};
-struct Teacher {
-    bool trained;      // an id of the vocabulary has a mass
-    float prior;       // sum of q log q
-};
-template <class T, class I, class Z>
-__device__ __forceinline__ Teacher teacher_of(const DistillArgs &a, int64_t row, float inv_t, int first, int cols, Entry *entries) {
-    const int lane = threadIdx.x % kWave;
-    const I *ids = static_cast<const I *>(a.ids) + row * a.top;
-    const Z *z = static_cast<const Z *>(a.teacher) + row * a.top;
-    const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
-    const auto logit = [&](int k) {
-        const int64_t id = (int64_t)ids[k];
-        return id >= 0 && id < a.vocab_size ? (float)z[k] * inv_t : -kInf;
-    };
-    float top = -kInf, sum = 0.0f, prior = 0.0f;
-    for (int k = lane; k < a.top; k += kWave) top = fmaxf(top, logit(k));
-    top = wave_max(top);
-    const float base = top == -kInf ? 0.0f : top;
-    for (int k = lane; k < a.top; k += kWave) sum += expf(logit(k) - base);
-    sum = wave_sum(sum);
-    const bool live = sum != 0.0f;      // NaN too
-    const float log_sum = logf(sum);
-    for (int k = lane; k < a.top; k += kWave) {
-        const int64_t id = (int64_t)ids[k];
-        const float d = logit(k) - base, q = live ? expf(d) / sum : 0.0f;
-        if (q != 0.0f) prior += q * (d - log_sum);
-        int at = q != 0.0f ? shard_row(id, a.vocab_start, a.cols) : -1;
-        if (at >= 0 && (unsigned)(at - first) >= (unsigned)cols) at = -1;
-        float mass = 0.0f;
-        if (at >= 0) {
-            for (int o = 0; o < a.top; ++o) {
-                if ((int64_t)ids[o] != id) continue;
-                const float more = expf(logit(o) - base) / sum;
-                if (o < k && more != 0.0f) at = -1;
-                mass += more;
-            }
-        }
-        entries[k] = Entry{at, at >= 0 ? mass : 0.0f, at >= 0 ? (float)l[at] * inv_t : 0.0f};
-    }
-    return Teacher{live, wave_sum(prior)};
+__device__ __forceinline__ TeacherIn teacher_in(const DistillArgs &a) {
+    return TeacherIn{a.ids, a.teacher, a.index_type, a.teacher_type, a.top, a.vocab_start, a.vocab_size, 1.0f / a.temperature};
 }
-// The entries' share of the loss's cross term, of logits taken from `from` on.
-__device__ __forceinline__ float cross_of(const Entry *entries, int top, float from) {
-    float cross = 0.0f;
-    for (int k = threadIdx.x % kWave; k < top; k += kWave) {
-        const Entry e = entries[k];
-        if (e.at >= 0) cross += e.mass * (e.x - from);
-    }
-    return wave_sum(cross);
+// The entries with the logits of their columns / T.
+template <class T>
+__device__ __forceinline__ Teacher entries_of(const DistillArgs &a, int64_t row, int first, int cols, Entry *entries) {
+    const TeacherIn in = teacher_in(a);
+    const Teacher t = teacher_of(in, row, first, cols, a.cols, entries);
+    const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
+    take_logits(entries, a.top, [&](int at) { return (float)l[at] * in.inv_t; });
+    return t;
 }
 // The gradient where the teacher has a mass, over what its row has there.
 template <class T>
@@ -97,7 +51,7 @@ __device__ __forceinline__ void settled() {
 // written over at the teacher's ids.
 template <class T, int THREADS, int E>
 constexpr int kDistillWaves = THREADS == 1024 && E * sizeof(T) <= 128 ? 8 : 1;
-template <class T, class I, class Z, int THREADS, int E, bool CUT>
+template <class T, int THREADS, int E, bool CUT>
 __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK), (kDistillWaves<T, THREADS, E>)) void k_distill(DistillArgs a) {
     using Q = Team<T, THREADS, E, CUT>;
     constexpr int N = Q::N, P = Q::P;
@@ -112,7 +66,7 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK), (kDistillWaves<T
         V<T, N> x[P];
         q.load(l, x, T(-kInf));
         Teacher t{};
-        if (q.wave == 0) t = teacher_of<T, I, Z>(a, row, inv_t, 0, a.cols, entries);
+        if (q.wave == 0) t = entries_of<T>(a, row, 0, a.cols, entries);
         float top = -kInf, sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < P; ++k) {
@@ -168,7 +122,7 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK), (kDistillWaves<T
 }
 
 // Rows too wide for registers, or of less than a piece: read once for the statistics and once more for the gradient.
-template <class T, class I, class Z>
+template <class T>
 __global__ __launch_bounds__(kWideBlock) void k_distill_wide(DistillArgs a) {
     constexpr int N = kN<T>, STEP = kWideBlock * N;
     extern __shared__ __attribute__((aligned(16))) char space[];
@@ -178,7 +132,7 @@ __global__ __launch_bounds__(kWideBlock) void k_distill_wide(DistillArgs a) {
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
         Teacher t{};
-        if (threadIdx.x < kWave) t = teacher_of<T, I, Z>(a, row, inv_t, 0, a.cols, entries);
+        if (threadIdx.x < kWave) t = entries_of<T>(a, row, 0, a.cols, entries);
         float top = -kInf, sum = 0.0f;
 #pragma unroll 4
         for (int c = threadIdx.x * N; c < a.cols; c += STEP) {
@@ -228,7 +182,7 @@ __global__ __launch_bounds__(kWideBlock) void k_distill_wide(DistillArgs a) {
 
 // The gradient alone, from the whole vocabulary's lse: a workgroup takes a stretch of one row, and the teacher's entries in it.
 constexpr int kGradPieces = 4;
-template <class T, class I, class Z>
+template <class T>
 __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
     constexpr int N = kN<T>, K = kGradPieces, SPAN = K * 256 * N;
     extern __shared__ __attribute__((aligned(16))) char space[];
@@ -249,7 +203,7 @@ __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
             if (from + k * 256 * N < a.cols) raw[k] = load<N>(l, from + k * 256 * N, a.cols);
         }
         if (threadIdx.x < kWave) {
-            const Teacher t = teacher_of<T, I, Z>(a, row, inv_t, first, SPAN, entries);
+            const Teacher t = entries_of<T>(a, row, first, SPAN, entries);
             if (threadIdx.x == 0) lds = t.trained;
         }
         __syncthreads();      // also: the teacher's logits have been read
@@ -277,43 +231,38 @@ hipError_t launch_with(void (*kernel)(A), unsigned grid, int block, size_t lds, 
     void *args[] = {&a};
     return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3(grid), dim3(block), args, lds, s);
 }
-template <class T, class I, class Z, bool CUT>
-hipError_t distill(const DistillArgs &a, hipStream_t s) {
+template <class T, bool CUT>
+hipError_t rows(const DistillArgs &a, hipStream_t s) {
     const size_t each = sizeof(Entry) * a.top;
     const auto run = [&](auto kernel, int threads) {
         const int teams = threads < 256 ? 256 / threads : 1;
         return launch_with(kernel, grid_of((a.rows + teams - 1) / teams), threads * teams, each * teams, s, a);
     };
     if (a.cols < kN<T> || a.cols > 1024 * 64)
-        return launch_with(k_distill_wide<T, I, Z>, grid_of(a.rows), kWideBlock, each, s, a);
-    if (a.cols <= 64 * 32) return run(k_distill<T, I, Z, 64, 32, CUT>, 64);
-    if (a.cols <= 256 * 32) return run(k_distill<T, I, Z, 256, 32, CUT>, 256);
-    if (a.cols <= 1024 * 32) return run(k_distill<T, I, Z, 1024, 32, CUT>, 1024);
-    return run(k_distill<T, I, Z, 1024, 64, CUT>, 1024);
+        return launch_with(k_distill_wide<T>, grid_of(a.rows), kWideBlock, each, s, a);
+    if (a.cols <= 64 * 8) return run(k_distill<T, 64, 8, CUT>, 64);
+    if (a.cols <= 64 * 32) return run(k_distill<T, 64, 32, CUT>, 64);
+    if (a.cols <= 256 * 32) return run(k_distill<T, 256, 32, CUT>, 256);
+    if (a.cols <= 512 * 32) return run(k_distill<T, 512, 32, CUT>, 512);
+    if (a.cols <= 1024 * 32) return run(k_distill<T, 1024, 32, CUT>, 1024);
+    if (a.cols <= 1024 * 48) return run(k_distill<T, 1024, 48, CUT>, 1024);
+    return run(k_distill<T, 1024, 64, CUT>, 1024);
 }
-template <class T, class I, class Z>
+template <class T>
 hipError_t distill(const DistillArgs &a, hipStream_t s) {
     if (a.lse_in) {
         constexpr int SPAN = kGradPieces * 256 * kN<T>;
-        return launch_with(k_distill_grad<T, I, Z>, grid_of(a.rows * ((a.cols + SPAN - 1) / SPAN)), 256, sizeof(Entry) * a.top, s, a);
+        return launch_with(k_distill_grad<T>, grid_of(a.rows * ((a.cols + SPAN - 1) / SPAN)), 256, sizeof(Entry) * a.top, s, a);
     }
-    return a.cols % kN<T> ? distill<T, I, Z, true>(a, s) : distill<T, I, Z, false>(a, s);
+    return a.cols % kN<T> ? rows<T, true>(a, s) : rows<T, false>(a, s);
 }
-template <class T>
-hipError_t distill(const DistillArgs &a, int index_type, int teacher_type, hipStream_t s) {
-    // the teacher's logits are the student's type or 32 bits
-    if (teacher_type == ECHO_F32)
-        return index_type == ECHO_I64 ? distill<T, int64_t, float>(a, s) : distill<T, int32_t, float>(a, s);
-    return index_type == ECHO_I64 ? distill<T, int64_t, T>(a, s) : distill<T, int32_t, T>(a, s);
-}
-
 }  // namespace
 
-hipError_t launch_distill(const DistillArgs &a, int type, int index_type, int teacher_type, hipStream_t s) {
+hipError_t launch_distill(const DistillArgs &a, int type, hipStream_t s) {
     switch (type) {
-        case ECHO_F32: return distill<float>(a, index_type, teacher_type, s);
-        case ECHO_F16: return distill<f16>(a, index_type, teacher_type, s);
-        default: return distill<bf16>(a, index_type, teacher_type, s);
+        case ECHO_F32: return distill<float>(a, s);
+        case ECHO_F16: return distill<f16>(a, s);
+        default: return distill<bf16>(a, s);
     }
 }
 

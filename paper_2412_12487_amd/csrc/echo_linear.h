@@ -2,6 +2,7 @@
 #pragma once
 
 #include "echo_product.h"
+#include "echo_teacher.h"
 
 namespace echo {
 
@@ -19,6 +20,7 @@ struct HeadArgs {
     float2 *stats;                // [parts][rows]: maximum, and sum relative to it, of a wavefront's columns
     float *hits;                  // logits of the target or of the entries
     const float *lse, *grad_loss, *scale;
+    float *scale_out;             // one workgroup more writes it, or null
     char *prob;                   // [planes][prob_rows][.]: the gradient's shares
     int64_t prob_stride, prob_plane;
     int prob_rows, prob_cols;     // columns that are written, from the product's first on
@@ -48,10 +50,9 @@ struct JoinArgs {
     float *lse, *target, *entropy, *loss;
 };
 struct TeacherArgs {
-    const void *ids, *teacher;
-    int64_t rows, vocab_start, vocab_size;
-    int top, vocab;
-    float inv_t;
+    TeacherIn in;
+    int64_t rows;
+    int vocab;
     int *local;
     float *q;
     float2 *prior;

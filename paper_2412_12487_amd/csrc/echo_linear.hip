@@ -5,8 +5,6 @@
 namespace echo {
 namespace {
 
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
-
 // A row's place in the loss: whether it is trained on, and with one target a row its column here or -1.
 struct Row {
     bool trained;
@@ -52,6 +50,21 @@ struct Cells {
     }
 };
 
+// The largest |grad_loss| of the rows, or 1 where that is 0 or not finite: what the gradient's shares are relative to, so that
+// rows of one weight have it exactly.
+template <int THREADS>
+__device__ __forceinline__ void write_scale(const float *grad_loss, int rows, float *scale, float *lds) {
+    float top = 0.0f;
+#pragma unroll 4
+    for (int n = threadIdx.x; n < rows; n += THREADS) top = fmaxf(top, fabsf(grad_loss[n]));
+    top = wave_max(top);
+    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = top;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < THREADS / kWave; ++w) top = fmaxf(top, lds[w]);
+    *scale = top > 0.0f && top < kInf ? top : 1.0f;
+}
+
 // Tiles of logits, i over the vocabulary and j over the rows.
 //   kLoss: each row's maximum and sum of exponentials over a wavefront's columns, and the logits of its target or entries.
 //   kKeep: the same, and the exponentials, relative to that maximum.
@@ -61,6 +74,9 @@ template <class T, class S, int MODE, int PLANES>
 __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArgs a) {
     __shared__ __attribute__((aligned(16))) char t0[S::BYTES];
     __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
+    if constexpr (MODE == kKeep)
+        if ((int)blockIdx.x == a.m.tiles_i * a.m.tiles_j)
+            return write_scale<S::THREADS>(a.grad_loss, a.rows, a.scale_out, reinterpret_cast<float *>(t0));
     const Place at = place_of(a.m);
     F4 acc[S::BI][S::BJ];
     multiply<T, true, true, S>(a.m, at, t0, t1, acc);
@@ -254,9 +270,26 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
         }
     }
     __syncthreads();
-    if (w || n >= a.rows) return;
     top = part[0][r].x;
     sum = part[0][r].y;
+    float cross = 0.0f;
+    if (a.top) {
+        // the loss takes logits from their maximum on
+        const float from = a.loss && top != -kInf && sum == sum ? top : 0.0f;
+        if (n < a.rows) {
+            for (int k = w; k < a.top; k += 64) {
+                const int64_t e = (int64_t)n * a.top + k;
+                if (a.local[e] >= 0) cross += a.q[e] * (a.hits[e] - from);
+            }
+        }
+        for (int by = 32; by; by /= 2) {
+            __syncthreads();
+            part[w][r].x = cross;
+            __syncthreads();
+            if (w < by) cross += part[w + by][r].x;
+        }
+    }
+    if (w || n >= a.rows) return;
     if (sum != sum) top = sum;      // a row of NaN alone has no maximum but a sum
     const float more = logf(sum), lse = top == -kInf ? -kInf : top + more;
     if (a.lse) a.lse[n] = lse;
@@ -270,75 +303,30 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
     }
     const float2 prior = a.prior[n];
     const bool trained = prior.y > 0.0f;
-    const float from = a.loss && lse != -kInf ? top : 0.0f;      // the loss takes logits from their maximum on
-    float cross = 0.0f;
-    for (int k = 0; k < a.top; ++k) {
-        const int64_t e = (int64_t)n * a.top + k;
-        const float q = a.q[e];
-        if (a.local[e] >= 0 && q != 0.0f) cross += q * (a.hits[e] - from);
-    }
     if (a.target) a.target[n] = cross;
     if (a.entropy) a.entropy[n] = -prior.x;
     if (a.loss) a.loss[n] = !trained ? 0.0f : lse == -kInf ? kInf : a.square * (prior.x - cross + more);
 }
 
-// The teacher's distribution of a row, a wavefront a row: masses over its ids in the vocabulary, entries of the same id
-// summed in the first of them, and the sum of q log q of the entries as given.
-template <class I, class Z>
+// The teacher's entries of every row, a wavefront a row.
 __global__ __launch_bounds__(256) void k_teacher(TeacherArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char space[];
     const int lane = threadIdx.x % kWave;
+    Entry *entries = reinterpret_cast<Entry *>(space) + threadIdx.x / kWave * a.in.top;
     for (int64_t n = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave; n < a.rows; n += (int64_t)gridDim.x * 4) {
-        const I *ids = static_cast<const I *>(a.ids) + n * a.top;
-        const Z *z = static_cast<const Z *>(a.teacher) + n * a.top;
-        const auto logit = [&](int k) {
-            const int64_t id = (int64_t)ids[k];
-            return id >= 0 && id < a.vocab_size ? (float)z[k] * a.inv_t : -kInf;
-        };
-        float top = -kInf, sum = 0.0f;
-        for (int k = lane; k < a.top; k += kWave) top = fmaxf(top, logit(k));
-        top = wave_max(top);
-        const float base = top == -kInf ? 0.0f : top;
-        for (int k = lane; k < a.top; k += kWave) sum += expf(logit(k) - base);
-        sum = wave_sum(sum);
-        const bool live = sum != 0.0f;      // a row of NaN has a sum
-        const float log_sum = logf(sum);
-        float prior = 0.0f;
-        for (int k = lane; k < a.top; k += kWave) {
-            const int64_t id = (int64_t)ids[k];
-            const float l = logit(k) - base, q = live ? expf(l) / sum : 0.0f;
-            if (q != 0.0f) prior += q * (l - log_sum);
-            float mass = 0.0f;
-            int at = q != 0.0f ? shard_row(id, a.vocab_start, a.vocab) : -1;
-            if (at >= 0) {
-                bool first = true;
-                for (int o = 0; o < a.top; ++o) {
-                    if ((int64_t)ids[o] != id) continue;
-                    const float more = expf(logit(o) - base) / sum;
-                    if (o < k && more != 0.0f) first = false;
-                    mass += more;
-                }
-                if (!first) at = -1;
-            }
-            a.local[n * a.top + k] = at;
-            a.q[n * a.top + k] = at >= 0 ? mass : 0.0f;
+        const Teacher t = teacher_of(a.in, n, 0, a.vocab, a.vocab, entries);
+        for (int k = lane; k < a.in.top; k += kWave) {
+            a.local[n * a.in.top + k] = entries[k].at;
+            a.q[n * a.in.top + k] = entries[k].mass;
         }
-        prior = wave_sum(prior);
-        if (lane == 0) a.prior[n] = make_float2(prior, live ? 1.0f : sum != sum ? 1.0f : 0.0f);
+        if (lane == 0) a.prior[n] = make_float2(t.prior, t.trained ? 1.0f : 0.0f);
     }
 }
 
-// The largest |grad_loss| of the rows, or 1 where that is 0 or not finite: what the gradient's shares are relative to, so that
-// rows of one weight have it exactly.
+// For a gradient whose loss was another call's; else the loss's launch has a workgroup for it.
 __global__ __launch_bounds__(1024) void k_scale(const float *grad_loss, int rows, float *scale) {
     __shared__ float lds[16];
-    float top = 0.0f;
-    for (int n = threadIdx.x; n < rows; n += 1024) top = fmaxf(top, fabsf(grad_loss[n]));
-    top = wave_max(top);
-    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = top;
-    __syncthreads();
-    if (threadIdx.x) return;
-    for (int w = 1; w < 16; ++w) top = fmaxf(top, lds[w]);
-    *scale = top > 0.0f && top < kInf ? top : 1.0f;
+    write_scale<1024>(grad_loss, rows, scale, lds);
 }
 
 // Rows laid out for the products: PLANES planes of 16 bits, rows filled up with zeros to whole steps.
@@ -350,10 +338,7 @@ __global__ __launch_bounds__(256) void k_layout(LayoutArgs a) {
         const int64_t row = id / pieces;
         const int c = (int)(id - row * pieces) * 8;
         const U *from = static_cast<const U *>(a.from) + row * a.stride;
-        F<8> f = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (c + j < a.cols) f[j] = (float)from[c + j];
+        F<8> f = widen<U, 8>(load<8>(from, c, a.cols));
 #pragma unroll
         for (int plane = 0; plane < PLANES; ++plane) {
             const V<T, 8> h = round_to<T, 8>(f);
@@ -365,31 +350,23 @@ __global__ __launch_bounds__(256) void k_layout(LayoutArgs a) {
 
 template <class T, int MODE, int PLANES>
 hipError_t logits(const HeadArgs &a, int shape, hipStream_t s) {
-    const dim3 grid(a.m.tiles_i * a.m.tiles_j);
+    const dim3 grid(a.m.tiles_i * a.m.tiles_j + (a.scale_out ? 1 : 0));
     switch (shape) {
         case 0: return launch(k_logits<T, Wide, MODE, PLANES>, grid, dim3(Wide::THREADS), s, a);
         case 1: return launch(k_logits<T, Middle, MODE, PLANES>, grid, dim3(Middle::THREADS), s, a);
         default: return launch(k_logits<T, Thin, MODE, PLANES>, grid, dim3(Thin::THREADS), s, a);
     }
 }
-template <class I>
-hipError_t teacher(const TeacherArgs &a, int type, hipStream_t s) {
-    const dim3 grid(grid_of((a.rows + 3) / 4));
-    switch (type) {
-        case ECHO_F32: return launch(k_teacher<I, float>, grid, dim3(256), s, a);
-        case ECHO_F16: return launch(k_teacher<I, f16>, grid, dim3(256), s, a);
-        default: return launch(k_teacher<I, bf16>, grid, dim3(256), s, a);
-    }
-}
-
 template <class T, int PLANES>
 hipError_t logits(const HeadArgs &a, int mode, int shape, hipStream_t s) {
     return mode == kGrad ? logits<T, kGrad, PLANES>(a, shape, s)
                          : mode == kKeep ? logits<T, kKeep, PLANES>(a, shape, s) : logits<T, kLoss, 1>(a, shape, s);
 }
 hipError_t launch_join(const JoinArgs &a, hipStream_t s) { return launch(k_join, dim3((a.rows + 15) / 16), dim3(1024), s, a); }
-hipError_t launch_teacher(const TeacherArgs &a, int type, int index_type, hipStream_t s) {
-    return index_type == ECHO_I64 ? teacher<int64_t>(a, type, s) : teacher<int32_t>(a, type, s);
+hipError_t launch_teacher(const TeacherArgs &a, hipStream_t s) {
+    void *args[] = {const_cast<TeacherArgs *>(&a)};
+    return hipLaunchKernel(reinterpret_cast<const void *>(k_teacher), dim3(grid_of((a.rows + 3) / 4)), dim3(256), args,
+                           4 * sizeof(Entry) * a.in.top, s);
 }
 hipError_t launch_scale(const float *grad_loss, int rows, float *scale, hipStream_t s) {
     return launch(k_scale, dim3(1), dim3(1024), s, grad_loss, rows, scale);
@@ -509,6 +486,7 @@ Plan plan_of(const LinearArgs &a) {
         // too few tiles to fill the GPU: workgroups take parts of the sum
         int64_t splits = middle < 512 ? 512 / middle : 1;
         if (splits > steps / 4) splits = steps / 4;
+        if (splits > 64) splits = 64;
         p.splits = splits < 1 ? 1 : (int)splits;
         if (p.splits > 1) p.out = Ranges{(int)a.rows, 1, 1};
         p.parts = p.splits > 1 || p.pieces > 1;
@@ -542,6 +520,7 @@ hipError_t run_logits(const HeadArgs &head, int type, int mode, int cover, const
         h.prob_cols = to - from;
         if (h.prob) h.prob += (int64_t)from * 2;
         if (h.kept) h.kept = static_cast<char *>(h.kept) + (int64_t)from * (type == ECHO_BF16 ? 2 : 4);
+        if (from) h.scale_out = nullptr;
         if (from) h.stats += (int64_t)parts_of(from, r.shape0) * h.rows;
         tile(h.m, to - from, h.m.nj, shape);
         hipError_t e;
@@ -603,10 +582,10 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
     h.vocab_start = a.vocab_start;
     h.vocab_size = a.vocab_size;
     if (a.top) {
-        const TeacherArgs t{a.targets, a.teacher, a.rows, a.vocab_start, a.vocab_size, a.top, a.vocab, h.inv_t,
-                            reinterpret_cast<int *>(w + p.local), reinterpret_cast<float *>(w + p.q),
+        const TeacherArgs t{{a.targets, a.teacher, a.index_type, a.teacher_type, a.top, a.vocab_start, a.vocab_size, h.inv_t},
+                            a.rows, a.vocab, reinterpret_cast<int *>(w + p.local), reinterpret_cast<float *>(w + p.q),
                             reinterpret_cast<float2 *>(w + p.prior)};
-        ECHO_HIP(launch_teacher(t, a.teacher_type, a.index_type, s));
+        ECHO_HIP(launch_teacher(t, s));
         h.local = t.local;
         h.q = t.q;
         h.prior = t.prior;
@@ -617,6 +596,8 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         h.hits = reinterpret_cast<float *>(w + p.hits);
         h.kept = p.keep ? w + p.kept : nullptr;
         h.kept_stride = p.prob_cols;
+        h.grad_loss = a.grad_loss;
+        h.scale_out = p.keep ? reinterpret_cast<float *>(w + p.scale) : nullptr;
         ECHO_HIP(run_logits(h, a.type, p.keep ? kKeep : kLoss, p.keep ? (int)p.prob_cols : a.vocab, p.logits, s));
         ECHO_HIP(launch_join(JoinArgs{h.stats, h.prior, h.hits, h.q, h.local, h.targets, h.wide_index, h.top, h.rows, h.vocab,
                                       p.stats_parts, h.vocab_start, h.vocab_size, a.temperature * a.temperature, a.lse, a.target,
@@ -631,7 +612,8 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
     h.prob_plane = p.prob_rows * h.prob_stride;
     h.prob_rows = (int)p.prob_rows;
     h.prob_cols = (int)p.prob_cols;
-    ECHO_HIP(launch_scale(a.grad_loss, h.rows, reinterpret_cast<float *>(w + p.scale), s));
+    h.scale_out = nullptr;
+    if (!p.keep) ECHO_HIP(launch_scale(a.grad_loss, h.rows, reinterpret_cast<float *>(w + p.scale), s));
     const Operand prob{h.prob, h.prob_stride, h.prob_plane, p.prob_rows, (int)p.prob_cols};
     const int64_t grad_elem = a.grad_type == ECHO_F32 ? 4 : 2;
     float *parts = p.parts ? reinterpret_cast<float *>(w + p.part) : nullptr;

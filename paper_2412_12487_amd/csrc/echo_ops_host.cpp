@@ -398,7 +398,7 @@ int distill(DistillArgs a, int32_t type, int32_t index_type, int32_t teacher_typ
     a.cols = (int)cols;
     a.top = (int)top;
     return on_device(hip_device, what, [&] {
-        return launch_distill(a, type, index_type, teacher_type, static_cast<hipStream_t>(hip_stream));
+        return launch_distill(a, type, static_cast<hipStream_t>(hip_stream));
     });
 }
 
@@ -466,8 +466,8 @@ int echo_distillation(const void *logits, int64_t logits_stride, int32_t type, c
                       float *entropy, float *loss, const float *grad_loss, void *grad, int64_t grad_stride,
                       int hip_device, void *hip_stream) {
     clear_error();
-    const DistillArgs a{logits, ids, teacher, logits_stride, rows, vocab_start, vocab_size, 0, 0, temperature, lse, target,
-                        entropy, loss, nullptr, grad_loss, grad, grad_stride};
+    const DistillArgs a{logits, ids, teacher, logits_stride, rows, vocab_start, vocab_size, 0, 0, index_type, teacher_type,
+                        temperature, lse, target, entropy, loss, nullptr, grad_loss, grad, grad_stride};
     return distill(a, type, index_type, teacher_type, cols, top, false, hip_device, hip_stream, "distillation");
 }
 
@@ -476,8 +476,8 @@ int echo_distillation_grad(const void *logits, int64_t logits_stride, int32_t ty
                            int64_t vocab_start, int64_t vocab_size, float temperature, const float *lse,
                            const float *grad_loss, void *grad, int64_t grad_stride, int hip_device, void *hip_stream) {
     clear_error();
-    const DistillArgs a{logits, ids, teacher, logits_stride, rows, vocab_start, vocab_size, 0, 0, temperature, nullptr, nullptr,
-                        nullptr, nullptr, lse, grad_loss, grad, grad_stride};
+    const DistillArgs a{logits, ids, teacher, logits_stride, rows, vocab_start, vocab_size, 0, 0, index_type, teacher_type,
+                        temperature, nullptr, nullptr, nullptr, nullptr, lse, grad_loss, grad, grad_stride};
     return distill(a, type, index_type, teacher_type, cols, top, true, hip_device, hip_stream, "distillation gradient");
 }
 

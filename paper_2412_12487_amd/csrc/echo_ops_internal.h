@@ -74,7 +74,7 @@ struct LinearArgs {
 struct DistillArgs {
     const void *logits, *ids, *teacher;
     int64_t logits_stride, rows, vocab_start, vocab_size;
-    int cols, top;
+    int cols, top, index_type, teacher_type;
     float temperature;
     float *lse, *target, *entropy, *loss;
     const float *lse_in, *grad_loss;
@@ -95,6 +95,6 @@ hipError_t launch_embed_grad(const EmbedGradArgs &a, int type, int index_type, i
 hipError_t launch_loss(const LossArgs &a, int type, int index_type, hipStream_t s);
 hipError_t launch_loss_grad(const LossArgs &a, int type, int index_type, hipStream_t s);
 hipError_t launch_linear(const LinearArgs &a, hipStream_t s);
-hipError_t launch_distill(const DistillArgs &a, int type, int index_type, int teacher_type, hipStream_t s);
+hipError_t launch_distill(const DistillArgs &a, int type, hipStream_t s);
 
 }  // namespace echo
