@@ -57,6 +57,27 @@ struct TeacherArgs {
     float *q;
     float2 *prior;
 };
+struct PartsArgs {
+    Product m;
+    float *parts;                 // [splits][rows][ld]
+    int64_t part;
+    int ld;
+    const float *grad_loss;
+    float *scale_out;             // one workgroup more writes it, or null
+};
+// Rows whose logits are in parts of the sum.
+struct RowsArgs {
+    const float *parts;           // [splits][rows][ld]
+    int64_t part;                 // elements from a part to the next
+    int splits, ld, rows, vocab, cols;      // cols: of the gradient's shares
+    TeacherIn in;                 // top is 0 with one target a row: its ids are the targets
+    float square;
+    float *lse, *target, *entropy, *loss;
+    const float *lse_in, *grad_loss, *scale;
+    char *prob;                   // or null
+    int64_t prob_stride, prob_plane;
+    int prob_rows;
+};
 struct LayoutArgs {
     const void *from;
     int64_t stride, rows;         // stride in elements
@@ -115,6 +136,8 @@ constexpr float kKeptUnit = sizeof(Kept<T, PLANES>) == 2 ? 32768.0f : 1.0f;
 
 // deep: b's sum runs along its rows (the hidden states' gradient), or across them (the table's)
 hipError_t launch_out(const OutArgs &a, int type, int out_type, bool deep, int shape, hipStream_t s);
+// both of them by middle tiles in one launch
+hipError_t launch_both(const OutArgs &dhidden, const OutArgs &dweight, int type, int grad_type, hipStream_t s);
 hipError_t launch_zero(void *out, int64_t bytes, hipStream_t s);
 hipError_t launch_gather(const GatherArgs &a, int type, int out_type, hipStream_t s);
 

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
     if constexpr (MODE == kKeep)
         if ((int)blockIdx.x == a.m.tiles_i * a.m.tiles_j)
             return write_scale<S::THREADS>(a.grad_loss, a.rows, a.scale_out, reinterpret_cast<float *>(t0));
-    const Place at = place_of(a.m);
+    const Place at = place_of(a.m, blockIdx.x);
     F4 acc[S::BI][S::BJ];
     multiply<T, true, true, S>(a.m, at, t0, t1, acc);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -176,6 +176,166 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
                 }
             }
         }
+    }
+}
+
+// A part of the sum of each logit, for products of few tiles: workgroups take parts of the hidden size.
+template <class T, class S>
+__global__ __launch_bounds__(S::THREADS, S::THREADS < 256 ? 1 : S::THREADS / 256) void k_parts(PartsArgs a) {
+    __shared__ __attribute__((aligned(16))) char t0[S::BYTES];
+    __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
+    if ((int)blockIdx.x == a.m.tiles_i * a.m.tiles_j * a.m.splits)
+        return write_scale<S::THREADS>(a.grad_loss, a.m.nj, a.scale_out, reinterpret_cast<float *>(t0));
+    const Place at = place_of(a.m, blockIdx.x);
+    F4 acc[S::BI][S::BJ];
+    multiply<T, true, true, S>(a.m, at, t0, t1, acc);
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int i0 = at.ti * S::TI + wave / S::WJ * S::BI * 16 + (lane / 16) * 4, j0 = at.tj * S::TJ + wave % S::WJ * S::BJ * 16 + lane % 16;
+#pragma unroll
+    for (int b = 0; b < S::BJ; ++b)
+#pragma unroll
+        for (int k = 0; k < S::BI; ++k)
+            if (j0 + b * 16 < a.m.nj && i0 + k * 16 < a.ld)
+                *reinterpret_cast<F4 *>(a.parts + at.split * a.part + (int64_t)(j0 + b * 16) * a.ld + i0 + k * 16) = acc[k][b];
+}
+
+// A workgroup a row of logits in parts: its statistics and loss, and the gradient's shares.  The parts are read again for the
+// shares, from the cache.
+constexpr int kRowBlock = 1024, kRowWaves = kRowBlock / kWave;
+template <class T, int PLANES>
+__global__ __launch_bounds__(kRowBlock) void k_rows(RowsArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char space[];
+    Entry *entries = reinterpret_cast<Entry *>(space);
+    __shared__ float4 lds[kRowWaves];
+    const int n = blockIdx.x;
+    const float *parts = a.parts + (int64_t)n * a.ld;
+    // Four columns in each of G groups from c on, kRowBlock * 4 apart: their parts are loaded together.
+    const auto logits4 = [&](int c, auto &d) {
+        constexpr int G = sizeof(d) / sizeof(F4);
+#pragma unroll
+        for (int g = 0; g < G; ++g) d[g] = 0.0f;
+#pragma unroll 2
+        for (int p = 0; p < a.splits; ++p)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+                if (c + g * kRowBlock * 4 < a.ld) d[g] += *reinterpret_cast<const F4 *>(parts + p * a.part + c + g * kRowBlock * 4);
+#pragma unroll
+        for (int g = 0; g < G; ++g) d[g] *= a.in.inv_t;
+    };
+    const auto logit = [&](int c) {
+        float d = 0.0f;
+#pragma unroll 8
+        for (int p = 0; p < a.splits; ++p) d += parts[p * a.part + c];
+        return d * a.in.inv_t;
+    };
+    char *prob = a.prob + n * a.prob_stride;
+    const auto put = [&](int c, auto d) {
+        constexpr int N = sizeof(d) / 4;
+#pragma unroll
+        for (int plane = 0; plane < PLANES; ++plane) {
+            const V<T, N> h = round_to<T, N>(d);
+            *reinterpret_cast<V<T, N> *>(prob + c * 2 + plane * a.prob_plane) = h;
+            if (plane + 1 < PLANES) d -= widen<T, N>(h);
+        }
+    };
+    if (n >= a.rows) {      // fills the last step of the table's gradient
+        for (int c = threadIdx.x * 4; c < a.cols; c += kRowBlock * 4) put(c, F<4>(0.0f));
+        return;
+    }
+    Teacher t{};
+    int at = -1;
+    if (!a.in.top) {
+        const int64_t id = index_at(a.in.ids, a.in.index_type, n);
+        t.trained = id >= 0 && id < a.in.vocab_size;
+        at = t.trained ? shard_row(id, a.in.vocab_start, a.vocab) : -1;
+    } else if (threadIdx.x < kWave) {
+        t = teacher_of(a.in, n, 0, a.vocab, a.vocab, entries);
+        take_logits(entries, a.in.top, logit);
+    }
+    float top = -kInf, sum = 0.0f;
+    if (!a.lse_in) {
+        constexpr int G = 4;
+        for (int c = threadIdx.x * 4; c < a.vocab; c += G * kRowBlock * 4) {
+            F4 x[G];
+            logits4(c, x);
+            float m = top;
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (c + g * kRowBlock * 4 + e >= a.vocab) x[g][e] = -kInf;
+                    m = fmaxf(m, x[g][e]);
+                }
+            const float base = m == -kInf ? 0.0f : m;
+            sum *= top == -kInf ? 1.0f : exp_of(top - base);      // before a first finite logit the sum is 0, or NaN
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += exp_of(x[g][e] - base);
+            top = m;
+        }
+        const float mine = top;
+        top = wave_max(top);
+        sum = wave_sum(mine == -kInf ? sum : sum * exp_of(mine - top));
+    }
+    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = make_float4(top, sum, t.trained ? 1.0f : 0.0f, 0.0f);
+    __syncthreads();
+    const bool trained = lds[0].z > 0.0f;
+    float lse;
+    if (a.lse_in) {
+        lse = a.lse_in[n];
+    } else {
+#pragma unroll
+        for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, lds[w].x);
+        sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kRowWaves; ++w) {
+            const float4 p = lds[w];
+            sum += p.x == -kInf ? p.y : p.y * exp_of(p.x - top);
+        }
+        if (sum != sum) top = sum;      // a row of NaN alone has no maximum but a sum
+        const float more = logf(sum);
+        lse = top == -kInf ? -kInf : top + more;
+        if (threadIdx.x < kWave) {
+            const float from = a.loss && lse != -kInf ? top : 0.0f;      // the loss takes logits from their maximum on
+            const float cross = a.in.top ? cross_of(entries, a.in.top, from) : at >= 0 ? logit(at) - from : 0.0f;
+            if (threadIdx.x == 0) {
+                if (a.lse) a.lse[n] = lse;
+                if (a.target) a.target[n] = cross;
+                if (a.entropy) a.entropy[n] = -t.prior;
+                if (a.loss) a.loss[n] = !trained ? 0.0f : lse == -kInf ? kInf : a.square * (t.prior - cross + more);
+            }
+        }
+    }
+    if (!a.prob) return;
+    const bool live = trained && lse != -kInf;
+    const float g_of_row = live ? a.grad_loss[n] / *a.scale * kUnit<T> : 0.0f;
+    constexpr int G = 2;
+    for (int c0 = threadIdx.x * 4; c0 < a.cols; c0 += G * kRowBlock * 4) {
+        F4 x[G];
+        if (live) logits4(c0, x);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const int c = c0 + g * kRowBlock * 4;
+            if (c >= a.cols) continue;
+            F<4> d = 0.0f;
+            if (live) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = exp_of(x[g][e] - lse) - (c + e == at ? 1.0f : 0.0f);
+                    d[e] = c + e < a.vocab ? p * g_of_row : 0.0f;
+                }
+            }
+            put(c, d);
+        }
+    }
+    if (!a.in.top || !live) return;
+    __threadfence_block();
+    __syncthreads();      // what the entries are written over has arrived
+    if (threadIdx.x >= kWave) return;
+    for (int k = threadIdx.x; k < a.in.top; k += kWave) {
+        const Entry e = entries[k];
+        if (e.at >= 0) put(e.at, F<1>((exp_of(e.x - lse) - e.mass) * g_of_row));
     }
 }
 
@@ -329,16 +489,19 @@ __global__ __launch_bounds__(1024) void k_scale(const float *grad_loss, int rows
     write_scale<1024>(grad_loss, rows, scale, lds);
 }
 
-// Rows laid out for the products: PLANES planes of 16 bits, rows filled up with zeros to whole steps.
+// Rows laid out for the products: PLANES planes of 16 bits, rows filled up with zeros to whole steps.  One launch for both
+// matrices; the second may have no rows.
 template <class U, class T, int PLANES>
-__global__ __launch_bounds__(256) void k_layout(LayoutArgs a) {
-    const int pieces = a.width / 8;
-    const int64_t all = a.rows * pieces;
+__global__ __launch_bounds__(256) void k_layout(LayoutArgs one, LayoutArgs two) {
+    const int pieces = one.width / 8;
+    const int64_t all = (one.rows + two.rows) * pieces;
     for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < all; id += (int64_t)gridDim.x * 256) {
-        const int64_t row = id / pieces;
+        int64_t row = id / pieces;
         const int c = (int)(id - row * pieces) * 8;
-        const U *from = static_cast<const U *>(a.from) + row * a.stride;
-        F<8> f = widen<U, 8>(load<8>(from, c, a.cols));
+        const bool second = row >= one.rows;
+        const LayoutArgs &a = second ? two : one;
+        if (second) row -= one.rows;
+        F<8> f = widen<U, 8>(load<8>(static_cast<const U *>(a.from) + row * a.stride, c, a.cols));
 #pragma unroll
         for (int plane = 0; plane < PLANES; ++plane) {
             const V<T, 8> h = round_to<T, 8>(f);
@@ -362,6 +525,22 @@ hipError_t logits(const HeadArgs &a, int mode, int shape, hipStream_t s) {
     return mode == kGrad ? logits<T, kGrad, PLANES>(a, shape, s)
                          : mode == kKeep ? logits<T, kKeep, PLANES>(a, shape, s) : logits<T, kLoss, 1>(a, shape, s);
 }
+template <class T>
+hipError_t parts(const PartsArgs &a, int shape, hipStream_t s) {
+    const dim3 grid(a.m.tiles_i * a.m.tiles_j * a.m.splits + (a.scale_out ? 1 : 0));
+    if (shape == 1) return launch(k_parts<T, Middle>, grid, dim3(Middle::THREADS), s, a);
+    return launch(k_parts<T, Thin>, grid, dim3(Thin::THREADS), s, a);
+}
+hipError_t launch_parts(const PartsArgs &a, int type, int shape, hipStream_t s) {
+    return type == ECHO_F16 ? parts<f16>(a, shape, s) : parts<bf16>(a, shape, s);
+}
+hipError_t launch_rows(const RowsArgs &a, int type, hipStream_t s) {
+    void *args[] = {const_cast<RowsArgs *>(&a)};
+    const void *kernel = type == ECHO_F32   ? reinterpret_cast<const void *>(k_rows<bf16, 3>)
+                         : type == ECHO_F16 ? reinterpret_cast<const void *>(k_rows<f16, 1>)
+                                            : reinterpret_cast<const void *>(k_rows<bf16, 1>);
+    return hipLaunchKernel(kernel, dim3(a.prob ? a.prob_rows : a.rows), dim3(kRowBlock), args, sizeof(Entry) * a.in.top, s);
+}
 hipError_t launch_join(const JoinArgs &a, hipStream_t s) { return launch(k_join, dim3((a.rows + 15) / 16), dim3(1024), s, a); }
 hipError_t launch_teacher(const TeacherArgs &a, hipStream_t s) {
     void *args[] = {const_cast<TeacherArgs *>(&a)};
@@ -371,12 +550,12 @@ hipError_t launch_teacher(const TeacherArgs &a, hipStream_t s) {
 hipError_t launch_scale(const float *grad_loss, int rows, float *scale, hipStream_t s) {
     return launch(k_scale, dim3(1), dim3(1024), s, grad_loss, rows, scale);
 }
-hipError_t launch_layout(const LayoutArgs &a, int type, hipStream_t s) {
-    const dim3 grid(grid_of((a.rows * (a.width / 8) + 255) / 256));
+hipError_t launch_layout(const LayoutArgs &a, const LayoutArgs &b, int type, hipStream_t s) {
+    const dim3 grid(grid_of(((a.rows + b.rows) * (a.width / 8) + 255) / 256));
     switch (type) {
-        case ECHO_F32: return launch(k_layout<float, bf16, 3>, grid, dim3(256), s, a);
-        case ECHO_F16: return launch(k_layout<f16, f16, 1>, grid, dim3(256), s, a);
-        default: return launch(k_layout<bf16, bf16, 1>, grid, dim3(256), s, a);
+        case ECHO_F32: return launch(k_layout<float, bf16, 3>, grid, dim3(256), s, a, b);
+        case ECHO_F16: return launch(k_layout<f16, f16, 1>, grid, dim3(256), s, a, b);
+        default: return launch(k_layout<bf16, bf16, 1>, grid, dim3(256), s, a, b);
     }
 }
 
@@ -389,6 +568,8 @@ hipError_t launch_shares(const ShareArgs &a, int type, hipStream_t s) {
     }
 }
 
+constexpr int64_t kProbBytes = int64_t(1) << 30;      // of the logits' gradient at a time
+constexpr int64_t kProbCols = int64_t(1) << 21;
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 int tiles(int64_t n, int t) { return (int)((n + t - 1) / t); }
 
@@ -424,9 +605,6 @@ void tile(Product &m, int ni, int nj, int shape) {
     m.tiles_j = tiles(nj, shape == 2 ? 64 : side(shape));
 }
 
-constexpr int64_t kProbBytes = int64_t(1) << 30;      // of the logits' gradient at a time
-constexpr int64_t kProbCols = int64_t(1) << 21;
-
 // Sizes of a call's products, and where its workspace has what.
 struct Plan {
     int planes, pairs;
@@ -434,12 +612,14 @@ struct Plan {
     bool copy_hidden, copy_weight;
     Ranges logits;                 // the loss's
     int stats_parts;
+    bool few;                      // few tiles of logits: their sum is split, and rows are worked on by themselves
+    int few_shape, few_splits;
     bool keep;                     // the loss's pass keeps its exponentials for the gradient
     int64_t prob_rows, prob_cols, pieces;
     Ranges out;                    // the hidden states' gradient
     int splits;
     bool parts;
-    int64_t hidden, weight, stats, hits, local, q, prior, scale, prob, kept, part, bytes;
+    int64_t hidden, weight, stats, hits, local, q, prior, scale, prob, kept, part, sums, bytes;
 };
 bool direct(const void *p, int64_t stride, int type, int cols) {
     return type != ECHO_F32 && cols % kDepth == 0 && stride % 8 == 0 && stride <= int64_t(1) << 22 && (uintptr_t)p % 16 == 0;
@@ -458,12 +638,30 @@ Plan plan_of(const LinearArgs &a) {
     };
     if (p.copy_hidden) p.hidden = take(a.rows * p.width * 2 * p.planes);
     if (p.copy_weight) p.weight = take((int64_t)a.vocab * p.width * 2 * p.planes);
-    if (a.top) {
+    p.few = false;
+    if (a.rows * up(a.vocab, kDepth) * 2 * p.planes <= kProbBytes) {
+        // Up to a workgroup a compute unit: a step takes such a launch 0.6 us whatever its tiles; parts of at least 8 steps, two
+        // workgroups a compute unit at most.
+        const int shape = a.rows <= 64 ? 2 : 1;
+        Product m{};
+        tile(m, a.vocab, (int)a.rows, shape);
+        const int64_t wg = (int64_t)m.tiles_i * m.tiles_j, steps = (int64_t)(p.width / kDepth) * p.pairs;
+        if (wg <= 256) {
+            int64_t splits = 512 / wg;
+            if (splits > steps / 8) splits = steps / 8;
+            if (splits > 32) splits = 32;
+            p.few = true;
+            p.few_shape = shape;
+            p.few_splits = splits < 1 ? 1 : (int)splits;
+            p.sums = take(p.few_splits * a.rows * up(a.vocab, kDepth) * 4);
+        }
+    }
+    if (a.top && !p.few) {
         p.local = take(a.rows * a.top * 4);
         p.q = take(a.rows * a.top * 4);
         p.prior = take(a.rows * 8);
     }
-    if (a.forward) {
+    if (a.forward && !p.few) {
         p.logits = logits_ranges(a.vocab, a.rows);
         p.stats_parts = parts_of(p.logits.split, p.logits.shape0);
         if (p.logits.split < a.vocab) p.stats_parts += parts_of(a.vocab - p.logits.split, p.logits.shape1);
@@ -479,7 +677,7 @@ Plan plan_of(const LinearArgs &a) {
         p.pieces = (whole + most - 1) / most;
         p.prob_cols = p.pieces == 1 ? whole : up((whole + p.pieces - 1) / p.pieces, 256);
         p.prob = take(p.prob_rows * p.prob_cols * 2 * p.planes);
-        p.keep = a.forward && p.pieces == 1;
+        p.keep = a.forward && p.pieces == 1 && !p.few;
         if (p.keep) p.kept = a.type == ECHO_BF16 ? p.prob : take(a.rows * p.prob_cols * 4);
         const int64_t middle = (int64_t)tiles(a.cols, 128) * tiles(a.rows, 128), steps = p.prob_cols / kDepth * p.pairs;
         p.out = ranges_of(a.rows, a.cols);
@@ -564,14 +762,17 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
     const int64_t row_bytes = (int64_t)p.width * 2;
     Operand hidden{static_cast<const char *>(a.hidden), a.hidden_stride * 2, 0, a.rows, p.width},
         weight{static_cast<const char *>(a.weight), a.weight_stride * 2, 0, a.vocab, p.width};
-    if (p.copy_hidden) {
-        hidden = Operand{w + p.hidden, row_bytes, a.rows * row_bytes, a.rows, p.width};
-        ECHO_HIP(launch_layout(LayoutArgs{a.hidden, a.hidden_stride, a.rows, a.cols, p.width, w + p.hidden, hidden.plane}, a.type, s));
-    }
+    LayoutArgs laid[2] = {};
+    int copies = 0;
     if (p.copy_weight) {
         weight = Operand{w + p.weight, row_bytes, a.vocab * row_bytes, a.vocab, p.width};
-        ECHO_HIP(launch_layout(LayoutArgs{a.weight, a.weight_stride, a.vocab, a.cols, p.width, w + p.weight, weight.plane}, a.type, s));
+        laid[copies++] = LayoutArgs{a.weight, a.weight_stride, a.vocab, a.cols, p.width, w + p.weight, weight.plane};
     }
+    if (p.copy_hidden) {
+        hidden = Operand{w + p.hidden, row_bytes, a.rows * row_bytes, a.rows, p.width};
+        laid[copies++] = LayoutArgs{a.hidden, a.hidden_stride, a.rows, a.cols, p.width, w + p.hidden, hidden.plane};
+    }
+    if (copies) ECHO_HIP(launch_layout(laid[0], laid[1], a.type, s));
     HeadArgs h{};
     h.rows = (int)a.rows;
     h.vocab = a.vocab;
@@ -581,9 +782,9 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
     h.top = a.top;
     h.vocab_start = a.vocab_start;
     h.vocab_size = a.vocab_size;
-    if (a.top) {
-        const TeacherArgs t{{a.targets, a.teacher, a.index_type, a.teacher_type, a.top, a.vocab_start, a.vocab_size, h.inv_t},
-                            a.rows, a.vocab, reinterpret_cast<int *>(w + p.local), reinterpret_cast<float *>(w + p.q),
+    const TeacherIn in{a.targets, a.teacher, a.index_type, a.teacher_type, a.top, a.vocab_start, a.vocab_size, h.inv_t};
+    if (a.top && !p.few) {
+        const TeacherArgs t{in, a.rows, a.vocab, reinterpret_cast<int *>(w + p.local), reinterpret_cast<float *>(w + p.q),
                             reinterpret_cast<float2 *>(w + p.prior)};
         ECHO_HIP(launch_teacher(t, s));
         h.local = t.local;
@@ -591,12 +792,35 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         h.prior = t.prior;
     }
     h.m = Product{weight, hidden, a.vocab, (int)a.rows, 0, 0, p.width / kDepth, p.pairs, 1};
-    if (a.forward) {
+    if (a.grads) {
+        h.scale = reinterpret_cast<float *>(w + p.scale);
+        h.prob = w + p.prob;
+        h.prob_stride = p.prob_cols * 2;
+        h.prob_plane = p.prob_rows * h.prob_stride;
+        h.prob_rows = (int)p.prob_rows;
+        h.prob_cols = (int)p.prob_cols;
+        h.grad_loss = a.grad_loss;
+    }
+    if (p.few) {
+        PartsArgs c{};
+        c.m = h.m;
+        c.m.splits = p.few_splits;
+        c.ld = (int)up(a.vocab, kDepth);
+        c.parts = reinterpret_cast<float *>(w + p.sums);
+        c.part = a.rows * c.ld;
+        c.grad_loss = a.grad_loss;
+        c.scale_out = a.grads ? reinterpret_cast<float *>(w + p.scale) : nullptr;
+        tile(c.m, a.vocab, h.rows, p.few_shape);
+        ECHO_HIP(launch_parts(c, a.type, p.few_shape, s));
+        ECHO_HIP(launch_rows(RowsArgs{c.parts, c.part, p.few_splits, c.ld, h.rows, a.vocab, (int)p.prob_cols, in,
+                                      a.temperature * a.temperature, a.lse, a.target, a.entropy, a.loss, a.forward ? nullptr : a.lse_in,
+                                      a.grad_loss, h.scale, a.grads ? h.prob : nullptr, h.prob_stride, h.prob_plane, h.prob_rows},
+                             a.type, s));
+    } else if (a.forward) {
         h.stats = reinterpret_cast<float2 *>(w + p.stats);
         h.hits = reinterpret_cast<float *>(w + p.hits);
         h.kept = p.keep ? w + p.kept : nullptr;
         h.kept_stride = p.prob_cols;
-        h.grad_loss = a.grad_loss;
         h.scale_out = p.keep ? reinterpret_cast<float *>(w + p.scale) : nullptr;
         ECHO_HIP(run_logits(h, a.type, p.keep ? kKeep : kLoss, p.keep ? (int)p.prob_cols : a.vocab, p.logits, s));
         ECHO_HIP(launch_join(JoinArgs{h.stats, h.prior, h.hits, h.q, h.local, h.targets, h.wide_index, h.top, h.rows, h.vocab,
@@ -605,15 +829,8 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
     }
     if (!a.grads) return hipSuccess;
     h.lse = a.forward ? a.lse : a.lse_in;
-    h.grad_loss = a.grad_loss;
-    h.scale = reinterpret_cast<float *>(w + p.scale);
-    h.prob = w + p.prob;
-    h.prob_stride = p.prob_cols * 2;
-    h.prob_plane = p.prob_rows * h.prob_stride;
-    h.prob_rows = (int)p.prob_rows;
-    h.prob_cols = (int)p.prob_cols;
     h.scale_out = nullptr;
-    if (!p.keep) ECHO_HIP(launch_scale(a.grad_loss, h.rows, reinterpret_cast<float *>(w + p.scale), s));
+    if (!p.keep && !p.few) ECHO_HIP(launch_scale(a.grad_loss, h.rows, reinterpret_cast<float *>(w + p.scale), s));
     const Operand prob{h.prob, h.prob_stride, h.prob_plane, p.prob_rows, (int)p.prob_cols};
     const int64_t grad_elem = a.grad_type == ECHO_F32 ? 4 : 2;
     float *parts = p.parts ? reinterpret_cast<float *>(w + p.part) : nullptr;
@@ -631,7 +848,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
                               h.top, h.rows, h.vocab, (int)p.prob_cols, h.vocab_start, h.vocab_size, p.logits.split,
                               part_of(p.logits.shape0), part_of(p.logits.shape1), h.prob, h.prob_stride, h.prob_plane, h.prob_rows};
             ECHO_HIP(launch_shares(c, a.type, s));
-        } else {
+        } else if (!p.few) {
             ECHO_HIP(run_logits(h, a.type, kGrad, (int)p.prob_cols, logits_ranges(p.prob_cols, a.rows), s));
         }
         OutArgs o{};
@@ -642,12 +859,21 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         o.part = a.rows * a.cols;
         o.add_parts = piece > 0;
         o.out = a.dhidden;
-        ECHO_HIP(run_out(o, a.type, a.type, true, p.out, s));
+        const Ranges table_out = ranges_of(n, a.cols);
+        const bool both = p.out.split == a.rows && p.out.shape0 == 1 && table_out.split == n && table_out.shape0 == 1;
+        OutArgs first_out = o;
+        tile(first_out.m, a.cols, h.rows, 1);
+        if (!both) ECHO_HIP(run_out(o, a.type, a.type, true, p.out, s));
         o.m = Product{hidden, prob, a.cols, n, 0, 0, (int)(p.prob_rows / kDepth), p.pairs, 1};
         o.parts = nullptr;
         o.out = static_cast<char *>(a.dweight) + first * a.cols * grad_elem;
         o.accumulate = a.accumulate;
-        ECHO_HIP(run_out(o, a.type, a.grad_type, false, ranges_of(n, a.cols), s));
+        if (both) {
+            tile(o.m, a.cols, n, 1);
+            ECHO_HIP(launch_both(first_out, o, a.type, a.grad_type, s));
+        } else {
+            ECHO_HIP(run_out(o, a.type, a.grad_type, false, table_out, s));
+        }
     }
     if (parts)
         ECHO_HIP(launch_gather(GatherArgs{parts, a.rows * a.cols, p.splits, h.scale, a.temperature, a.dhidden}, a.type, a.type, s));

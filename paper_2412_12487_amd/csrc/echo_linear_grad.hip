@@ -19,10 +19,8 @@ __device__ __forceinline__ void put4(U *out, int left, F4 d, bool add) {
 
 // i over the hidden size, across the rows of operand a; j over rows (deep) or over the vocabulary.
 template <class T, class U, class S, bool DEEP>
-__global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_out(OutArgs a) {
-    [[maybe_unused]] __shared__ __attribute__((aligned(16))) char t0[S::BYTES];
-    [[maybe_unused]] __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
-    const Place at = place_of(a.m);
+__device__ __forceinline__ void out_tile(const OutArgs &a, int id, [[maybe_unused]] char *t0, [[maybe_unused]] char *t1) {
+    const Place at = place_of(a.m, id);
     F4 acc[S::BI][S::BJ];
 #ifdef __HIP_DEVICE_COMPILE__      // reads shared memory transposed, which the host's pass does not know
     multiply<T, false, DEEP, S>(a.m, at, t0, t1, acc);
@@ -46,6 +44,23 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_out(OutArgs a)
                 put4(static_cast<U *>(a.out) + (int64_t)j * a.m.ni + i, a.m.ni - i, d, a.accumulate);
         }
     }
+}
+template <class T, class U, class S, bool DEEP>
+__global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_out(OutArgs a) {
+    __shared__ __attribute__((aligned(16))) char t0[S::BYTES];
+    __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
+    out_tile<T, U, S, DEEP>(a, blockIdx.x, t0, t1);
+}
+// Both gradients in one launch, where neither fills the GPU: the hidden states' of type U, the table's of type W.
+template <class T, class U, class W, class S>
+__global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_both(OutArgs hidden, OutArgs table) {
+    __shared__ __attribute__((aligned(16))) char t0[S::BYTES];
+    __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
+    const int first = hidden.m.tiles_i * hidden.m.tiles_j * hidden.m.splits;
+    if ((int)blockIdx.x < first)
+        out_tile<T, U, S, true>(hidden, blockIdx.x, t0, t1);
+    else
+        out_tile<T, W, S, false>(table, blockIdx.x - first, t0, t1);
 }
 
 // Sums the parts: four wavefronts take a quarter of them each, in their order, of 256 elements side by side.
@@ -98,6 +113,18 @@ hipError_t out(const OutArgs &a, bool deep, int shape, hipStream_t s) {
 hipError_t launch_out(const OutArgs &a, int type, int out_type, bool deep, int shape, hipStream_t s) {
     if (type == ECHO_F16) return out_type == ECHO_F32 ? out<f16, float>(a, deep, shape, s) : out<f16, f16>(a, deep, shape, s);
     return out_type == ECHO_F32 ? out<bf16, float>(a, deep, shape, s) : out<bf16, bf16>(a, deep, shape, s);
+}
+hipError_t launch_both(const OutArgs &a, const OutArgs &b, int type, int grad_type, hipStream_t s) {
+    const dim3 grid((unsigned)(a.m.tiles_i * a.m.tiles_j * a.m.splits + b.m.tiles_i * b.m.tiles_j)), block(Middle::THREADS);
+    const bool wide = grad_type == ECHO_F32;
+    switch (type) {
+        case ECHO_F32: return launch(k_both<bf16, float, float, Middle>, grid, block, s, a, b);
+        case ECHO_F16:
+            return wide ? launch(k_both<f16, f16, float, Middle>, grid, block, s, a, b) : launch(k_both<f16, f16, f16, Middle>, grid, block, s, a, b);
+        default:
+            return wide ? launch(k_both<bf16, bf16, float, Middle>, grid, block, s, a, b)
+                        : launch(k_both<bf16, bf16, bf16, Middle>, grid, block, s, a, b);
+    }
 }
 hipError_t launch_zero(void *out, int64_t bytes, hipStream_t s) {
     return launch(k_zero, dim3(grid_of((bytes / 2 + 255) / 256)), dim3(256), s, static_cast<unsigned short *>(out), bytes / 2);

@@ -130,8 +130,8 @@ struct Shape {
 struct Place {
     int ti, tj, split;
 };
-__device__ __forceinline__ Place place_of(const Product &m) {
-    const int tiles = m.tiles_i * m.tiles_j, all = tiles * m.splits, id = blockIdx.x;
+__device__ __forceinline__ Place place_of(const Product &m, int id) {
+    const int tiles = m.tiles_i * m.tiles_j, all = tiles * m.splits;
     const int die = id % 8, each = all / 8, more = all % 8;
     int t = die * each + (die < more ? die : more) + id / 8;
     const int split = t / tiles;

@@ -40,14 +40,16 @@ struct Teacher {
 };
 // The row's entries whose columns are in [first, first + cols).
 //
-// Latency bounds it: the ids are compared with each other, four at a time, out of shared memory, and only where one comes twice
-// are masses added up.  With loads from memory in that loop a row of 64 entries took 13 us and one of 128 51 us.
+// Latency bounds it: the ids are compared with each other as 64 lanes against each lane's in turn, and only where one comes
+// twice are masses added up.  With loads from memory in that loop a row of 64 entries took 13 us and one of 128 51 us, with
+// loads from shared memory 7 and 22 us.
 __device__ __forceinline__ Teacher teacher_of(const TeacherIn &t, int64_t row, int first, int cols, int vocab, Entry *entries) {
     const int lane = threadIdx.x % kWave;
     const int64_t from = row * t.top;
     const auto logit = [&](int k) {
         const int64_t id = index_at(t.ids, t.index_type, from + k);
-        return id >= 0 && id < t.vocab_size ? value_at(t.logits, t.type, from + k) * t.inv_t : -kInf;
+        const float z = value_at(t.logits, t.type, from + k);      // beside the id, not behind it
+        return id >= 0 && id < t.vocab_size ? z * t.inv_t : -kInf;
     };
     float top = -kInf, sum = 0.0f, prior = 0.0f;
     for (int k = lane; k < t.top; k += kWave) {
@@ -77,10 +79,9 @@ __device__ __forceinline__ Teacher teacher_of(const TeacherIn &t, int64_t row, i
     for (int k0 = 0; k0 < t.top; k0 += kWave) {
         const int k = k0 + lane, mine = k < t.top ? entries[k].at : -1;
         bool twice = false;
-        for (int o = 0; o < t.top; o += 4) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (o + j < t.top) twice |= o + j != k && entries[o + j].at == mine;
+        for (int o0 = 0; o0 < t.top; o0 += kWave) {
+            const int theirs = o0 + lane < t.top ? entries[o0 + lane].at : -1, n = t.top - o0 < kWave ? t.top - o0 : kWave;
+            for (int j = 0; j < n; ++j) twice |= __builtin_amdgcn_readlane(theirs, j) == mine && o0 + j != k;
         }
         if (!__builtin_amdgcn_ballot_w64(twice && mine >= 0)) continue;
         float mass = 0.0f;
