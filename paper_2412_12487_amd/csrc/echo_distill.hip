@@ -16,7 +16,7 @@ __device__ __forceinline__ Teacher entries_of(const DistillArgs &a, int64_t row,
     const TeacherIn in = teacher_in(a);
     const Teacher t = teacher_of(in, row, first, cols, a.cols, entries);
     const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
-    take_logits(entries, a.top, [&](int at) { return (float)l[at] * in.inv_t; });
+    take_logits(entries, a.top, [&](int at) ECHO_INLINE { return (float)l[at] * in.inv_t; });
     return t;
 }
 // The gradient where the teacher has a mass, over what its row has there.

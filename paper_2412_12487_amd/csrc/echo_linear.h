@@ -17,7 +17,7 @@ struct HeadArgs {
     const int *local;             // [rows][top]: an entry's column here, or -1
     const float *q;               // [rows][top]
     const float2 *prior;          // [rows]: sum of q log q, and 1 where the row is trained on
-    float2 *stats;                // [parts][rows]: maximum, and sum relative to it, of a wavefront's columns
+    float2 *stats;                // [parts][rows]: log2 of the largest exponential, and sum relative to it, of a wavefront's columns
     float *hits;                  // logits of the target or of the entries
     const float *lse, *grad_loss, *scale;
     float *scale_out;             // one workgroup more writes it, or null
@@ -67,7 +67,7 @@ struct PartsArgs {
 };
 // Rows whose logits are in parts of the sum.
 struct RowsArgs {
-    const float *parts;           // [splits][rows][ld]
+    float *parts;                 // [splits][rows][ld]
     int64_t part;                 // elements from a part to the next
     int splits, ld, rows, vocab, cols;      // cols: of the gradient's shares
     TeacherIn in;                 // top is 0 with one target a row: its ids are the targets

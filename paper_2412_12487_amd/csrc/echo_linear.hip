@@ -86,39 +86,57 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
     const Cells<S> cells{t0, t1};
     if (a.top) cells.fill(a, a.first + i0, j0);      // entries' columns count from the shard's first id
     using Quad = __attribute__((ext_vector_type(4))) unsigned short;
+    // Everything per element counts here, 128 of them a lane: a logit is a maximum, one fused multiplication and addition, an
+    // exponential and an addition.  Maxima are of the products, and statistics in powers of two: 2^(D k - base) with
+    // k = log2(e) / T, rounded once in the exponent.
+    const float k2 = a.inv_t * kLog2e;
+    if (i0 + S::TI > a.m.ni) {
+#pragma unroll
+        for (int k = 0; k < S::BI; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i0 + il + k * 16 + e >= a.m.ni)
+#pragma unroll
+                    for (int b = 0; b < S::BJ; ++b) acc[k][b][e] = -kInf;
+    }
     if constexpr (MODE != kGrad) {
 #pragma unroll
         for (int b = 0; b < S::BJ; ++b) {
             const int n = j0 + jl + b * 16;
             const bool live = n < a.rows;
-            const int hit = live && !a.top ? row_of(a, n).at - a.first : -1;      // below 0 where it is not here
             float top = -kInf;
 #pragma unroll
-            for (int k = 0; k < S::BI; ++k) {
-                const int i = il + k * 16, v = i0 + i;
-                Quad entry = 0;
-                if (a.top) entry = *reinterpret_cast<const Quad *>(cells.cell(jl + b * 16, i));
+            for (int k = 0; k < S::BI; ++k)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = v + e < a.m.ni ? acc[k][b][e] * a.inv_t : -kInf;
-                    acc[k][b][e] = x;
-                    if (a.top) {
-                        if (live && entry[e]) a.hits[(int64_t)n * a.top + entry[e] - 1] = x;
-                    } else if (v + e == hit) {
-                        a.hits[n] = x;
-                    }
-                    top = fmaxf(top, x);
+                for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[k][b][e]);
+            if (!a.top) {
+                const int hit = live ? row_of(a, n).at - a.first - (i0 + il) : -1;      // below 0 where it is not here
+                if (hit >= 0 && hit < S::BI * 16) {
+#pragma unroll
+                    for (int k = 0; k < S::BI; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (k * 16 + e == hit) a.hits[n] = acc[k][b][e] * a.inv_t;
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < S::BI; ++k) {
+                    const Quad entry = *reinterpret_cast<const Quad *>(cells.cell(jl + b * 16, il + k * 16));
+                    if (!__builtin_bit_cast(int64_t, entry) || !live) continue;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (entry[e]) a.hits[(int64_t)n * a.top + entry[e] - 1] = acc[k][b][e] * a.inv_t;
                 }
             }
             top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
+            top = fmaxf(top, __shfl_xor(top, 32)) * k2;
             const float base = top == -kInf ? 0.0f : top;
             float sum = 0.0f;
 #pragma unroll
             for (int k = 0; k < S::BI; ++k) {
                 F4 d;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum += d[e] = exp_of(acc[k][b][e] - base);
+                for (int e = 0; e < 4; ++e) sum += d[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[k][b][e], k2, -base));
                 if constexpr (MODE == kKeep) {
                     using K = Kept<T, PLANES>;
                     const int v = i0 + il + k * 16;
@@ -147,37 +165,53 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
                 lse = a.lse[n];
                 live = r.trained && lse != -kInf;
                 g = a.grad_loss[n] / scale * kUnit<T>;
+                lse *= kLog2e;
             }
             if (n >= a.prob_rows) continue;
+            char *row = a.prob + n * a.prob_stride;
 #pragma unroll
             for (int k = 0; k < S::BI; ++k) {
                 const int i = il + k * 16, v = i0 + i;
                 if (v >= a.prob_cols) continue;
-                Quad entry = 0;
-                if (a.top) entry = *reinterpret_cast<const Quad *>(cells.cell(jl + b * 16, i));
-                F4 d;
+                F4 d = 0.0f;
+                if (live) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float p = exp_of(acc[k][b][e] * a.inv_t - lse);
-                    if (a.top) {
-                        if (live && entry[e]) p -= a.q[(int64_t)n * a.top + entry[e] - 1];
-                    } else if (v + e == hit) {
-                        p -= 1.0f;
+                    for (int e = 0; e < 4; ++e) d[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[k][b][e], k2, -lse));
+                    if (!a.top) {
+                        if ((unsigned)(hit - v) < 4u) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) d[e] -= v + e == hit ? 1.0f : 0.0f;
+                        }
+                    } else {
+                        const Quad entry = *reinterpret_cast<const Quad *>(cells.cell(jl + b * 16, i));
+                        if (__builtin_bit_cast(int64_t, entry)) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (entry[e]) d[e] -= a.q[(int64_t)n * a.top + entry[e] - 1];
+                        }
                     }
-                    d[e] = live && v + e < a.m.ni ? p * g : 0.0f;
+                    d *= g;
+                    if (i0 + S::TI > a.m.ni) {      // past the vocabulary's end, where a logit of NaN would be one
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) d[e] = v + e < a.m.ni ? d[e] : 0.0f;
+                    }
                 }
-                char *out = a.prob + n * a.prob_stride + v * 2;
                 typedef __attribute__((ext_vector_type(4))) T T4;
 #pragma unroll
                 for (int plane = 0; plane < PLANES; ++plane) {
                     const T4 h = __builtin_convertvector(d, T4);
-                    *reinterpret_cast<T4 *>(out + plane * a.prob_plane) = h;
+                    *reinterpret_cast<T4 *>(row + v * 2 + plane * a.prob_plane) = h;
                     if (plane + 1 < PLANES) d -= __builtin_convertvector(h, F4);
                 }
             }
         }
     }
 }
+
+template <int N>
+struct Count {
+    static constexpr int value = N;
+};
 
 // A part of the sum of each logit, for products of few tiles: workgroups take parts of the hidden size.
 template <class T, class S>
@@ -199,49 +233,35 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS < 256 ? 1 : S::THREADS / 256
                 *reinterpret_cast<F4 *>(a.parts + at.split * a.part + (int64_t)(j0 + b * 16) * a.ld + i0 + k * 16) = acc[k][b];
 }
 
-// A workgroup a row of logits in parts: its statistics and loss, and the gradient's shares.  The parts are read again for the
-// shares, from the cache.
-constexpr int kRowBlock = 1024, kRowWaves = kRowBlock / kWave;
-template <class T, int PLANES>
-__global__ __launch_bounds__(kRowBlock) void k_rows(RowsArgs a) {
+// A workgroup a row of logits in parts: they are summed and give the row's statistics and its loss.  With a gradient the sums
+// take the first part's place, and a second pass gives its shares.
+template <class T, int PLANES, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
+    constexpr int WAVES = BLOCK / kWave, STEP = BLOCK * 4;
     extern __shared__ __attribute__((aligned(16))) char space[];
     Entry *entries = reinterpret_cast<Entry *>(space);
-    __shared__ float4 lds[kRowWaves];
-    const int n = blockIdx.x;
-    const float *parts = a.parts + (int64_t)n * a.ld;
-    // Four columns in each of G groups from c on, kRowBlock * 4 apart: their parts are loaded together.
-    const auto logits4 = [&](int c, auto &d) {
-        constexpr int G = sizeof(d) / sizeof(F4);
-#pragma unroll
-        for (int g = 0; g < G; ++g) d[g] = 0.0f;
-#pragma unroll 2
-        for (int p = 0; p < a.splits; ++p)
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-                if (c + g * kRowBlock * 4 < a.ld) d[g] += *reinterpret_cast<const F4 *>(parts + p * a.part + c + g * kRowBlock * 4);
-#pragma unroll
-        for (int g = 0; g < G; ++g) d[g] *= a.in.inv_t;
-    };
-    const auto logit = [&](int c) {
-        float d = 0.0f;
-#pragma unroll 8
-        for (int p = 0; p < a.splits; ++p) d += parts[p * a.part + c];
-        return d * a.in.inv_t;
-    };
+    __shared__ float4 lds[WAVES];
+    // what the lambdas use stands by itself: with the arguments captured whole they went to scratch memory, 30 us of
+    // 500 x 4099 in place of 13
+    const int n = blockIdx.x, splits = a.splits, ld = a.ld, vocab = a.vocab;
+    const bool keeps = a.prob != nullptr;
+    const int64_t part = a.part, plane_bytes = a.prob_plane;
+    const float inv_t = a.in.inv_t;
     char *prob = a.prob + n * a.prob_stride;
-    const auto put = [&](int c, auto d) {
+    const auto put = [&](int c, auto d) ECHO_INLINE {
         constexpr int N = sizeof(d) / 4;
 #pragma unroll
         for (int plane = 0; plane < PLANES; ++plane) {
             const V<T, N> h = round_to<T, N>(d);
-            *reinterpret_cast<V<T, N> *>(prob + c * 2 + plane * a.prob_plane) = h;
+            *reinterpret_cast<V<T, N> *>(prob + c * 2 + plane * plane_bytes) = h;
             if (plane + 1 < PLANES) d -= widen<T, N>(h);
         }
     };
     if (n >= a.rows) {      // fills the last step of the table's gradient
-        for (int c = threadIdx.x * 4; c < a.cols; c += kRowBlock * 4) put(c, F<4>(0.0f));
+        for (int c = threadIdx.x * 4; c < a.cols; c += STEP) put(c, F<4>(0.0f));
         return;
     }
+    float *x = a.parts + (int64_t)n * a.ld;
     Teacher t{};
     int at = -1;
     if (!a.in.top) {
@@ -250,46 +270,85 @@ __global__ __launch_bounds__(kRowBlock) void k_rows(RowsArgs a) {
         at = t.trained ? shard_row(id, a.in.vocab_start, a.vocab) : -1;
     } else if (threadIdx.x < kWave) {
         t = teacher_of(a.in, n, 0, a.vocab, a.vocab, entries);
-        take_logits(entries, a.in.top, logit);
     }
+    // G pieces of 4 columns together, P of their parts at a time: 16 loads are on their way
+    const auto sum_parts = [&](int c, auto &d) ECHO_INLINE {
+        constexpr int G = sizeof(d) / sizeof(F4), P = 16 / G;
+#pragma unroll
+        for (int g = 0; g < G; ++g) d[g] = 0.0f;
+        for (int p0 = 0; p0 < splits; p0 += P) {
+            F4 v[P][G];
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int g = 0; g < G; ++g) {      // no branch between them: past the end the last is read again
+                    const int which = p0 + p < splits ? p0 + p : splits - 1, at = c + g * STEP < ld ? c + g * STEP : ld - 4;
+                    v[p][g] = *reinterpret_cast<const F4 *>(x + (int64_t)which * part + at);
+                }
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+                    if (p0 + p < splits) d[g] += v[p][g];
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            d[g] *= inv_t;
+            if (keeps && c + g * STEP < ld) *reinterpret_cast<F4 *>(x + c + g * STEP) = d[g];
+        }
+    };
+    // a logit after the pass
+    const auto logit = [&](int c) ECHO_INLINE {
+        float d = x[c];
+        if (keeps) return d;
+#pragma unroll 8
+        for (int p = 1; p < splits; ++p) d += x[p * part + c];
+        return d * inv_t;
+    };
     float top = -kInf, sum = 0.0f;
-    if (!a.lse_in) {
-        constexpr int G = 4;
-        for (int c = threadIdx.x * 4; c < a.vocab; c += G * kRowBlock * 4) {
-            F4 x[G];
-            logits4(c, x);
+    const auto pass = [&](auto groups) ECHO_INLINE {
+        constexpr int G = decltype(groups)::value;
+        for (int c = threadIdx.x * 4; c < ld; c += G * STEP) {
+            F4 d[G];
+            sum_parts(c, d);
             float m = top;
 #pragma unroll
             for (int g = 0; g < G; ++g)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if (c + g * kRowBlock * 4 + e >= a.vocab) x[g][e] = -kInf;
-                    m = fmaxf(m, x[g][e]);
+                    if (c + g * STEP + e >= vocab) d[g][e] = -kInf;
+                    m = fmaxf(m, d[g][e]);
                 }
             const float base = m == -kInf ? 0.0f : m;
             sum *= top == -kInf ? 1.0f : exp_of(top - base);      // before a first finite logit the sum is 0, or NaN
 #pragma unroll
             for (int g = 0; g < G; ++g)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum += exp_of(x[g][e] - base);
+                for (int e = 0; e < 4; ++e) sum += exp_of(d[g][e] - base);
             top = m;
         }
-        const float mine = top;
-        top = wave_max(top);
-        sum = wave_sum(mine == -kInf ? sum : sum * exp_of(mine - top));
-    }
+    };
+    if (a.ld <= STEP)
+        pass(Count<1>{});
+    else
+        pass(Count<2>{});
+    const float mine = top;
+    top = wave_max(top);
+    sum = wave_sum(mine == -kInf ? sum : sum * exp_of(mine - top));
     if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = make_float4(top, sum, t.trained ? 1.0f : 0.0f, 0.0f);
-    __syncthreads();
+    __threadfence_block();
+    __syncthreads();      // also: the row's logits are where its first part was
     const bool trained = lds[0].z > 0.0f;
+    if (a.in.top && threadIdx.x < kWave) take_logits(entries, a.in.top, logit);
     float lse;
     if (a.lse_in) {
         lse = a.lse_in[n];
     } else {
 #pragma unroll
-        for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, lds[w].x);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, lds[w].x);
         sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kRowWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float4 p = lds[w];
             sum += p.x == -kInf ? p.y : p.y * exp_of(p.x - top);
         }
@@ -309,25 +368,19 @@ __global__ __launch_bounds__(kRowBlock) void k_rows(RowsArgs a) {
     }
     if (!a.prob) return;
     const bool live = trained && lse != -kInf;
-    const float g_of_row = live ? a.grad_loss[n] / *a.scale * kUnit<T> : 0.0f;
-    constexpr int G = 2;
-    for (int c0 = threadIdx.x * 4; c0 < a.cols; c0 += G * kRowBlock * 4) {
-        F4 x[G];
-        if (live) logits4(c0, x);
+    const float g = live ? a.grad_loss[n] / *a.scale * kUnit<T> : 0.0f;
+#pragma unroll 4
+    for (int c = threadIdx.x * 4; c < a.cols; c += STEP) {
+        F<4> d = 0.0f;
+        if (live) {
+            const F4 f = *reinterpret_cast<const F4 *>(x + c);
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const int c = c0 + g * kRowBlock * 4;
-            if (c >= a.cols) continue;
-            F<4> d = 0.0f;
-            if (live) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = exp_of(x[g][e] - lse) - (c + e == at ? 1.0f : 0.0f);
-                    d[e] = c + e < a.vocab ? p * g_of_row : 0.0f;
-                }
+            for (int e = 0; e < 4; ++e) {
+                const float p = exp_of(f[e] - lse) - (c + e == at ? 1.0f : 0.0f);
+                d[e] = c + e < a.vocab ? p * g : 0.0f;
             }
-            put(c, d);
         }
+        put(c, d);
     }
     if (!a.in.top || !live) return;
     __threadfence_block();
@@ -335,7 +388,7 @@ __global__ __launch_bounds__(kRowBlock) void k_rows(RowsArgs a) {
     if (threadIdx.x >= kWave) return;
     for (int k = threadIdx.x; k < a.in.top; k += kWave) {
         const Entry e = entries[k];
-        if (e.at >= 0) put(e.at, F<1>((exp_of(e.x - lse) - e.mass) * g_of_row));
+        if (e.at >= 0) put(e.at, F<1>((exp_of(e.x - lse) - e.mass) * g));
     }
 }
 
@@ -366,7 +419,7 @@ __global__ __launch_bounds__(256) void k_shares(ShareArgs a) {
             }
             live = trained && lse != -kInf;
         }
-        const auto put = [&](int c, auto d) {
+        const auto put = [&](int c, auto d) ECHO_INLINE {
             constexpr int N = sizeof(d) / 4;
             char *out = a.prob + n * a.prob_stride + c * 2;
 #pragma unroll
@@ -385,7 +438,7 @@ __global__ __launch_bounds__(256) void k_shares(ShareArgs a) {
                 const int part = c < a.split ? c / a.part0 : a.split / a.part0 + (c - a.split) / a.part1;
                 const float top = a.stats[(int64_t)part * a.rows + n].x;
                 d = widen<K, 8>(*reinterpret_cast<const V<K, 8> *>(static_cast<const K *>(a.kept) + (int64_t)n * a.cols + c)) *
-                    (exp_of(top - lse) * g / kKeptUnit<T, PLANES>);
+                    (__builtin_amdgcn_exp2f(top - lse * kLog2e) * g / kKeptUnit<T, PLANES>);
                 if ((unsigned)(hit - c) < 8u) {
                     const float p = (exp_of(a.hits[n] - lse) - 1.0f) * g;
 #pragma unroll
@@ -411,12 +464,14 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
     __shared__ float2 part[64][17];
     const int r = threadIdx.x % 16, w = threadIdx.x / 16;
     const int n = blockIdx.x * 16 + r;
+    // statistics are in powers of two
+    const auto moved = [](float2 p, float to) ECHO_INLINE { return p.x == -kInf ? p.y : p.y * __builtin_amdgcn_exp2f(p.x - to); };      // p.y is 0 there, or NaN
     float top = -kInf, sum = 0.0f;
     if (n < a.rows) {
         for (int t = w; t < a.parts; t += 64) {
             const float2 p = a.stats[(int64_t)t * a.rows + n];
             const float m = fmaxf(top, p.x);
-            sum = (top == -kInf ? sum : sum * exp_of(top - m)) + (p.x == -kInf ? p.y : p.y * exp_of(p.x - m));
+            sum = moved(make_float2(top, sum), m) + moved(p, m);
             top = m;
         }
     }
@@ -426,11 +481,11 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
         if (w < by) {
             const float2 p = part[w][r], o = part[w + by][r];
             const float m = fmaxf(p.x, o.x);
-            part[w][r] = make_float2(m, (p.x == -kInf ? p.y : p.y * exp_of(p.x - m)) + (o.x == -kInf ? o.y : o.y * exp_of(o.x - m)));
+            part[w][r] = make_float2(m, moved(p, m) + moved(o, m));
         }
     }
     __syncthreads();
-    top = part[0][r].x;
+    top = part[0][r].x * kLn2;
     sum = part[0][r].y;
     float cross = 0.0f;
     if (a.top) {
@@ -534,12 +589,17 @@ hipError_t parts(const PartsArgs &a, int shape, hipStream_t s) {
 hipError_t launch_parts(const PartsArgs &a, int type, int shape, hipStream_t s) {
     return type == ECHO_F16 ? parts<f16>(a, shape, s) : parts<bf16>(a, shape, s);
 }
-hipError_t launch_rows(const RowsArgs &a, int type, hipStream_t s) {
+template <class T, int PLANES>
+hipError_t rows(const RowsArgs &a, hipStream_t s) {
     void *args[] = {const_cast<RowsArgs *>(&a)};
-    const void *kernel = type == ECHO_F32   ? reinterpret_cast<const void *>(k_rows<bf16, 3>)
-                         : type == ECHO_F16 ? reinterpret_cast<const void *>(k_rows<f16, 1>)
-                                            : reinterpret_cast<const void *>(k_rows<bf16, 1>);
-    return hipLaunchKernel(kernel, dim3(a.prob ? a.prob_rows : a.rows), dim3(kRowBlock), args, sizeof(Entry) * a.in.top, s);
+    const int block = a.ld <= 1024 ? 256 : a.ld <= 16384 ? 512 : 1024;
+    const void *kernel = block == 256   ? reinterpret_cast<const void *>(k_rows<T, PLANES, 256>)
+                         : block == 512 ? reinterpret_cast<const void *>(k_rows<T, PLANES, 512>)
+                                        : reinterpret_cast<const void *>(k_rows<T, PLANES, 1024>);
+    return hipLaunchKernel(kernel, dim3(a.prob ? a.prob_rows : a.rows), dim3(block), args, sizeof(Entry) * a.in.top, s);
+}
+hipError_t launch_rows(const RowsArgs &a, int type, hipStream_t s) {
+    return type == ECHO_F32 ? rows<bf16, 3>(a, s) : type == ECHO_F16 ? rows<f16, 1>(a, s) : rows<bf16, 1>(a, s);
 }
 hipError_t launch_join(const JoinArgs &a, hipStream_t s) { return launch(k_join, dim3((a.rows + 15) / 16), dim3(1024), s, a); }
 hipError_t launch_teacher(const TeacherArgs &a, hipStream_t s) {
@@ -641,12 +701,13 @@ Plan plan_of(const LinearArgs &a) {
     p.few = false;
     if (a.rows * up(a.vocab, kDepth) * 2 * p.planes <= kProbBytes) {
         // Up to a workgroup a compute unit: a step takes such a launch 0.6 us whatever its tiles; parts of at least 8 steps, two
-        // workgroups a compute unit at most.
+        // workgroups a compute unit at most.  Long rows want long sums, since one workgroup reads a row again: one row of
+        // 1024 over 51200 ids takes 29 us with tiles alone and 32 so.
         const int shape = a.rows <= 64 ? 2 : 1;
         Product m{};
         tile(m, a.vocab, (int)a.rows, shape);
         const int64_t wg = (int64_t)m.tiles_i * m.tiles_j, steps = (int64_t)(p.width / kDepth) * p.pairs;
-        if (wg <= 256) {
+        if (wg <= 256 && (a.vocab <= 16384 || steps >= 32)) {
             int64_t splits = 512 / wg;
             if (splits > steps / 8) splits = steps / 8;
             if (splits > 32) splits = 32;

@@ -29,6 +29,18 @@ __device__ __forceinline__ void out_tile(const OutArgs &a, int id, [[maybe_unuse
     const int wi = wave / S::WJ, wj = wave % S::WJ;
     const int i0 = at.ti * S::TI + wi * S::BI * 16 + (lane / 16) * 4, j0 = at.tj * S::TJ + wj * S::BJ * 16 + lane % 16;
     const float scale = a.parts ? 1.0f : *a.scale * (a.factor / kUnit<T>);
+    if constexpr (sizeof(U) == 2) {
+        if (!a.parts && !a.accumulate) {
+            const Outgoing<S, U> outgoing(t0, t1, wave, lane);
+            __syncthreads();      // the last step has been read
+#pragma unroll
+            for (int b = 0; b < S::BJ; ++b)
+#pragma unroll
+                for (int k = 0; k < S::BI; ++k) outgoing.put(k, b, acc[k][b] * scale);
+            const int i = at.ti * S::TI + wi * S::BI * 16, j = at.tj * S::TJ + wj * S::BJ * 16;
+            return outgoing.flush(static_cast<U *>(a.out) + (int64_t)j * a.m.ni + i, a.m.ni, a.m.nj - j, a.m.ni - i);
+        }
+    }
 #pragma unroll
     for (int b = 0; b < S::BJ; ++b) {
         const int j = j0 + b * 16;

@@ -9,6 +9,9 @@
 
 #include "echo_ops_internal.h"
 
+// Kernels' lambdas that are called more than once: left as functions, what they capture goes through memory.
+#define ECHO_INLINE __attribute__((always_inline))
+
 namespace echo {
 namespace {
 

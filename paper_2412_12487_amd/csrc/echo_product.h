@@ -141,6 +141,44 @@ __device__ __forceinline__ Place place_of(const Product &m, int id) {
     return Place{t / wide, first + t % wide, split};
 }
 
+// A wavefront's part of D on its way out in 16 bits: four elements of a lane lie side by side, and 16 lanes with
+// them, 32 bytes; through shared memory a row of 128 or 256 bytes is written at once.  Pieces are exchanged within a row so that lanes meet
+// different banks.  The buffers have been read by everybody before put.
+template <class S, class K>
+struct Outgoing {
+    static constexpr int PITCH = S::BI * 32, PIECES = PITCH / 16, ROWS = S::BJ * 16, BYTES = ROWS * PITCH, AT_ONCE = kWave / PIECES;
+    static_assert(sizeof(K) == 2 && S::WAVES * BYTES <= 2 * S::BYTES && S::BYTES % BYTES == 0, "");
+    char *area;
+    int lane;
+    __device__ __forceinline__ Outgoing(char *t0, char *t1, int wave, int l) : lane(l) {
+        constexpr int EACH = S::BYTES / BYTES;
+        area = (wave < EACH ? t0 + wave * BYTES : t1 + (wave - EACH) * BYTES);
+    }
+    __device__ __forceinline__ void put(int k, int b, F4 d) const {
+        typedef __attribute__((ext_vector_type(4))) K K4;
+        const int row = b * 16 + lane % 16, piece = k * 2 + lane / 32;
+        *reinterpret_cast<K4 *>(area + row * PITCH + ((piece ^ (row & (PIECES - 1))) * 16) + (lane / 16 % 2) * 8) = __builtin_convertvector(d, K4);
+    }
+    // rows `stride` elements apart, of which `rows` and `cols` of this part exist
+    __device__ __forceinline__ void flush(K *out, int64_t stride, int rows, int cols) const {
+        const int piece = lane % PIECES, left = cols - piece * 8;
+#pragma unroll
+        for (int r0 = 0; r0 < ROWS; r0 += AT_ONCE) {
+            const int row = r0 + lane / PIECES;
+            const V<K, 8> v = *reinterpret_cast<const V<K, 8> *>(area + row * PITCH + ((piece ^ (row & (PIECES - 1))) * 16));
+            if (row >= rows) continue;
+            K *at = out + row * stride + piece * 8;
+            if (left >= 8) {
+                *reinterpret_cast<V<K, 8> *>(at) = v;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j < left) at[j] = v[j];
+            }
+        }
+    }
+};
+
 // D's tile in registers: acc[a][b][e] belongs to i = a * 16 + 4 * (lane / 16) + e and j = b * 16 + lane % 16 of the wavefront's part.
 template <class T, bool ADEEP, bool BDEEP, class S, class Acc>
 __device__ __forceinline__ void multiply(const Product &m, const Place &at, char *t0, char *t1, Acc &acc) {
@@ -155,7 +193,7 @@ __device__ __forceinline__ void multiply(const Product &m, const Place &at, char
     int pair = begin / m.steps, step = begin - pair * m.steps;
     fa.seek(plane_a(pair), step);
     fb.seek(plane_b(pair), step);
-    const auto fetch = [&](char *t) {
+    const auto fetch = [&](char *t) ECHO_INLINE {
         fa.fetch(t, wave);
         fb.fetch(t + FA::BYTES, wave);
         if (++step == m.steps) {
@@ -178,7 +216,7 @@ __device__ __forceinline__ void multiply(const Product &m, const Place &at, char
     constexpr int ITEMS = 2 * S::BI, AHEAD = 4, HELD = 8;
     static_assert(S::BJ == AHEAD && S::BI >= AHEAD && ITEMS % HELD == 0, "one fragment of b an item");
     H8<T> x[HELD], y[2][S::BJ];
-    const auto turn = [&](char *mine, char *next, bool goes_on, bool more) {
+    const auto turn = [&](char *mine, char *next, bool goes_on, bool more) ECHO_INLINE {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             if (i == ITEMS - AHEAD && goes_on) {

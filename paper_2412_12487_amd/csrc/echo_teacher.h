@@ -15,9 +15,11 @@ struct TeacherIn {
 
 namespace {
 
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
 // exp(x), x <= 0 but for a row's rounding: one multiplication and the hardware's 2^x.  The product's rounding
 // makes the result |x| 2^-24 of itself wrong, as does that of x itself.
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 __device__ __forceinline__ int64_t index_at(const void *ids, int index_type, int64_t at) {
     return index_type == ECHO_I64 ? id_at<int64_t>(ids, at) : id_at<int32_t>(ids, at);
@@ -46,7 +48,7 @@ struct Teacher {
 __device__ __forceinline__ Teacher teacher_of(const TeacherIn &t, int64_t row, int first, int cols, int vocab, Entry *entries) {
     const int lane = threadIdx.x % kWave;
     const int64_t from = row * t.top;
-    const auto logit = [&](int k) {
+    const auto logit = [&](int k) ECHO_INLINE {
         const int64_t id = index_at(t.ids, t.index_type, from + k);
         const float z = value_at(t.logits, t.type, from + k);      // beside the id, not behind it
         return id >= 0 && id < t.vocab_size ? z * t.inv_t : -kInf;
@@ -81,7 +83,10 @@ __device__ __forceinline__ Teacher teacher_of(const TeacherIn &t, int64_t row, i
         bool twice = false;
         for (int o0 = 0; o0 < t.top; o0 += kWave) {
             const int theirs = o0 + lane < t.top ? entries[o0 + lane].at : -1, n = t.top - o0 < kWave ? t.top - o0 : kWave;
-            for (int j = 0; j < n; ++j) twice |= __builtin_amdgcn_readlane(theirs, j) == mine && o0 + j != k;
+            for (int j = 0; j < n; j += 8) {      // -1 past the end
+#pragma unroll
+                for (int i = 0; i < 8; ++i) twice |= __builtin_amdgcn_readlane(theirs, j + i) == mine && o0 + j + i != k;
+            }
         }
         if (!__builtin_amdgcn_ballot_w64(twice && mine >= 0)) continue;
         float mass = 0.0f;
