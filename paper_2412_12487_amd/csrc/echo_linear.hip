@@ -137,7 +137,9 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
                 F4 d;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum += d[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[k][b][e], k2, -base));
-                if constexpr (MODE == kKeep) {
+                if constexpr (MODE == kKeep && sizeof(Kept<T, PLANES>) == 2) {
+                    acc[k][b] = d;
+                } else if constexpr (MODE == kKeep) {
                     using K = Kept<T, PLANES>;
                     const int v = i0 + il + k * 16;
                     if (live && v < a.prob_cols) {
@@ -150,6 +152,17 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (live && lane < 16) a.stats[((int64_t)at.ti * S::WI + wi) * a.rows + n] = make_float2(top, sum);
+        }
+        if constexpr (MODE == kKeep && sizeof(Kept<T, PLANES>) == 2) {
+            using K = Kept<T, PLANES>;
+            const Outgoing<S, K> outgoing(t0, t1, wave, lane);
+            __syncthreads();      // the last step and the cells have been read
+#pragma unroll
+            for (int b = 0; b < S::BJ; ++b)
+#pragma unroll
+                for (int k = 0; k < S::BI; ++k) outgoing.put(k, b, acc[k][b] * kKeptUnit<T, PLANES>);
+            const int v = i0 + wi * S::BI * 16, n = j0 + wj * S::BJ * 16;
+            outgoing.flush(static_cast<K *>(a.kept) + n * a.kept_stride + v, a.kept_stride, a.rows - n, a.prob_cols - v);
         }
     } else {
         const float scale = *a.scale;
@@ -167,12 +180,12 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
                 g = a.grad_loss[n] / scale * kUnit<T>;
                 lse *= kLog2e;
             }
-            if (n >= a.prob_rows) continue;
+            if (PLANES > 1 && n >= a.prob_rows) continue;
             char *row = a.prob + n * a.prob_stride;
 #pragma unroll
             for (int k = 0; k < S::BI; ++k) {
                 const int i = il + k * 16, v = i0 + i;
-                if (v >= a.prob_cols) continue;
+                if (PLANES > 1 && v >= a.prob_cols) continue;
                 F4 d = 0.0f;
                 if (live) {
 #pragma unroll
@@ -196,6 +209,10 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
                         for (int e = 0; e < 4; ++e) d[e] = v + e < a.m.ni ? d[e] : 0.0f;
                     }
                 }
+                if constexpr (PLANES == 1) {
+                    acc[k][b] = d;
+                    continue;
+                }
                 typedef __attribute__((ext_vector_type(4))) T T4;
 #pragma unroll
                 for (int plane = 0; plane < PLANES; ++plane) {
@@ -204,6 +221,16 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
                     if (plane + 1 < PLANES) d -= __builtin_convertvector(h, F4);
                 }
             }
+        }
+        if constexpr (PLANES == 1) {
+            const Outgoing<S, T> outgoing(t0, t1, wave, lane);
+            __syncthreads();      // the last step and the cells have been read
+#pragma unroll
+            for (int b = 0; b < S::BJ; ++b)
+#pragma unroll
+                for (int k = 0; k < S::BI; ++k) outgoing.put(k, b, acc[k][b]);
+            const int v = i0 + wi * S::BI * 16, n = j0 + wj * S::BJ * 16;
+            outgoing.flush(reinterpret_cast<T *>(a.prob + n * a.prob_stride) + v, a.prob_stride / 2, a.prob_rows - n, a.prob_cols - v);
         }
     }
 }
