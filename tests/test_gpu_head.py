@@ -60,7 +60,7 @@ def _close(out, ref, keys=None):
 
 # sizes: one element; below, at and over a step of the sum, a tile of every shape, a whole wave of workgroups
 SIZES = [(1, 1, 1), (1, 64, 1), (2, 7, 3), (5, 64, 255), (64, 64, 256), (65, 128, 257), (129, 100, 1000), (300, 192, 700),
-         (257, 320, 513), (520, 65, 3000), (33, 1031, 2050)]
+         (257, 320, 513), (520, 65, 3000), (33, 1031, 2050), (40, 128, 20000), (3, 2112, 17000), (700, 72, 12000)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -86,7 +86,7 @@ def test_linear_cross_entropy_sizes(rows, cols, vocab, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols,vocab,top", [(1, 1, 1, 1), (3, 64, 5, 2), (64, 64, 256, 7), (129, 100, 1000, 64), (300, 192, 700, 33),
-                                                 (70, 128, 3001, 1024)])
+                                                 (70, 128, 3001, 1024), (40, 128, 20000, 130), (700, 72, 12000, 5)])
 def test_linear_distillation_sizes(rows, cols, vocab, top, dtype):
     h, w, _, g = _case(rows, cols, vocab, dtype, rows + cols + vocab)
     index, temp = (torch.int32, 2.0) if rows % 2 else (torch.int64, 1.7)
@@ -209,8 +209,8 @@ def test_linear_table_past_32_bits():
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-def test_linear_gradients_added_up_and_in_32_bits(dtype):
-    rows, cols, vocab = 150, 192, 400
+@pytest.mark.parametrize("rows,cols,vocab", [(150, 192, 400), (1100, 512, 9000), (9, 2048, 9000)])
+def test_linear_gradients_added_up_and_in_32_bits(rows, cols, vocab, dtype):
     h, w, t, g = _case(rows, cols, vocab, dtype, 4)
     g = g * torch.linspace(-1, 2, rows, device="cuda")
     ref = R.linear(h, w, R.targets(t, vocab), 0, vocab, grad_loss=g)
@@ -515,3 +515,61 @@ def test_written_tensors_count_as_modified_and_graphs_are_refused():
         E.linear_cross_entropy(h, leaf, t)
     with torch.no_grad():
         E.linear_cross_entropy(h, leaf, t)
+
+
+def test_teachers_that_repeat_themselves():
+    """An id in every place, ids in pairs, an id of which one entry has no mass: the masses of an id add up in its first entry."""
+    rows, cols, vocab = 5, 64, 700
+    h, w, _, g = _case(rows, cols, vocab, F32, 1)
+    for top in (2, 65, 130, 1024):
+        gen = _gen(top)
+        ids = torch.randint(0, vocab, (rows, top), generator=gen, device="cuda")
+        z = _normal(gen, rows, top)
+        ids[0] = 7
+        ids[1, 1::2] = ids[1, 0::2][:ids[1, 1::2].numel()]
+        ids[2, top // 2:] = ids[2, 0]
+        z[2, 0] = -math.inf
+        ids[3] = torch.arange(top, device="cuda") % 3
+        ids[4, ::2] = -1
+        given = R.entries(ids, z, vocab, 1.0)
+        _close(E.linear_distillation(h, w, ids, z, grad_loss=g), R.linear(h, w, given, 0, vocab, grad_loss=g))
+        l = (h @ w.t()).contiguous()
+        _close(E.distillation(l, ids, z, grad_loss=g), R.distillation(l, ids, z, 0, vocab, 1.0, grad_loss=g))
+        wide = torch.cat([l, _normal(gen, rows, 9000)], 1)      # tiles with cells, not rows of parts
+        assert wide.shape[1] == vocab + 9000
+        _close(E.distillation(wide, ids, z, grad_loss=g), R.distillation(wide, ids, z, 0, vocab + 9000, 1.0, grad_loss=g))
+    rows, cols, vocab = 1030, 64, 6000
+    h, w, _, g = _case(rows, cols, vocab, BF16, 2)
+    ids, z = _teacher(rows, 300, vocab, 4)
+    ids[:, 100:200] = ids[:, :100]
+    _close(E.linear_distillation(h, w, ids, z, grad_loss=g), R.linear(h, w, R.entries(ids, z, vocab, 1.0), 0, vocab, grad_loss=g))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_step_with_the_head_in_one_call(dtype):
+    """The operators together, against the same step with a library product for the head: the loss, and gradients that differ by
+    the roundings of logits and their gradient to the activations' type alone."""
+    from workloads import measured
+
+    g = _gen(7)
+    vocab, cols, tokens = 600, 128, 96
+    table = _normal(g, vocab, cols, std=0.3, dtype=dtype)
+    norms = [(torch.ones(cols, device="cuda", dtype=dtype), torch.zeros(cols, device="cuda", dtype=dtype)) for _ in range(3)]
+    ids = torch.randint(0, vocab, (tokens,), generator=g, device="cuda")
+    targets = torch.randint(0, vocab, (tokens,), generator=g, device="cuda")
+    targets[::6] = -100
+    a = measured.training_step(ids, targets, table, norms)
+    b = measured.training_step(ids, targets, table, norms, fused=True)
+    unit = R.UNIT[dtype]
+    # logits of up to |l| < 16 are rounded to their type in the one and not in the other; so are the gradients
+    assert abs(float(a["loss"] - b["loss"])) <= 32 * unit + 1e-5
+    for x, y in [(a["table"], b["table"])] + [(x, y) for m, n in zip(a["norms"], b["norms"]) for x, y in zip(m, n)]:
+        assert float((x - y).norm()) <= (64 * unit + 1e-5) * float(x.norm())
+    again = measured.training_step(ids, targets, table, norms, fused=True)
+    assert torch.equal(again["table"], b["table"])
+    # a teacher beside the targets: the loss is their sum, and so are the gradients
+    tid, z = _teacher(tokens, 8, vocab, 3)
+    c = measured.training_step(ids, targets, table, norms, fused=True, teacher=(tid, z, 2.0))
+    h = measured.training_step(ids, torch.full_like(targets, -100), table, norms, fused=True, teacher=(tid, z, 2.0))
+    assert abs(float(c["loss"] - b["loss"] - h["loss"])) <= 1e-4 * (1 + abs(float(c["loss"])))
+    assert float((c["table"] - b["table"] - h["table"]).norm()) <= (64 * unit + 1e-5) * float(c["table"].norm())

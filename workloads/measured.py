@@ -19,14 +19,19 @@ import paper_2412_12487_amd as E
 from . import configs, gpt1f1b
 
 
-def training_step(ids, targets, table, norms, *, scale=1.0, eps=1e-5):
+def training_step(ids, targets, table, norms, *, scale=1.0, eps=1e-5, fused=False, teacher=None):
     """One forward and backward pass of: embedding, a chain of pre-norm blocks whose branch is the norm itself
     (h <- h + norm(h)), a last norm, logits over the same table, mean cross entropy over the trained tokens.
 
     ids, targets: [tokens]; table: [vocab, hidden]; norms: (weight, bias) of every block and of the last norm.
     Returns a dict: 'loss' (mean), 'table' (float32 gradient of the table, both uses added up; the product that gives the
     logits' use is rounded to the table's type first) and 'norms', a list of (weight gradient, bias gradient), float32.
-    Nothing waits for the GPU."""
+    Nothing waits for the GPU.
+
+    fused: the head and its loss are one operator, which keeps no logits; the logits' use is then added up in 32 bits.
+    teacher, with fused: (ids [tokens, top], logits, temperature) of a teacher whose mean distillation loss is added."""
+    if teacher is not None and not fused:
+        raise ValueError("a teacher needs the fused head")
     vocab = table.shape[0]
     h = E.embedding(ids, table, scale)
     saved, branch = [], None
@@ -35,14 +40,24 @@ def training_step(ids, targets, table, norms, *, scale=1.0, eps=1e-5):
         h = out.get("sum", h)                 # the residual stream, which the next block reads again
         saved.append((h, out["mean"], out["rstd"]))
         branch = out["y"]
-    # the matrix products are the library's, and round their results once to the activations' type
-    logits = branch @ table.t()
     trained = (targets >= 0) & (targets < vocab)
     grad_loss = trained.float() / trained.sum().clamp(min=1)
-    out = E.cross_entropy(logits, targets, grad_loss=grad_loss, out={"grad": logits})
-    loss = (out["loss"] * grad_loss).sum()
-    main = (out["grad"].t() @ branch).float()
-    dy, past, grads = out["grad"] @ table, None, []
+    past, grads = None, []
+    if fused:
+        out = E.linear_cross_entropy(branch, table, targets, grad_loss=grad_loss, dtype=torch.float32)
+        loss, main, dy = (out["loss"] * grad_loss).sum(), out["dweight"], out["dhidden"]
+        if teacher is not None:
+            even = torch.full_like(grad_loss, 1 / len(grad_loss))
+            out = E.linear_distillation(branch, table, teacher[0], teacher[1], temperature=teacher[2], grad_loss=even,
+                                        out={"dweight": main}, accumulate=True)
+            loss, dy = loss + (out["loss"] * even).sum(), dy + out["dhidden"]
+    else:
+        # the matrix products are the library's, and round their results once to the activations' type
+        logits = branch @ table.t()
+        out = E.cross_entropy(logits, targets, grad_loss=grad_loss, out={"grad": logits})
+        loss = (out["loss"] * grad_loss).sum()
+        main = (out["grad"].t() @ branch).float()
+        dy = out["grad"] @ table
     for (weight, _), (h, mean, rstd) in zip(reversed(norms), reversed(saved)):
         g = E.layer_norm_grad(dy, h, weight, mean, rstd, grad_residual=past, dtype=torch.float32)
         grads.append((g["dweight"], g["dbias"]))
