@@ -162,15 +162,17 @@ int echo_distillation_grad(const void *logits, int64_t logits_stride, int32_t ty
  * gradient of above:
  *   dhidden = d weight, [rows][cols] of `type`;   dweight = d^T hidden, [vocab][cols] of grad_type (`type` or ECHO_F32),
  *   written, or with accumulate != 0 added to.
- * Of 16-bit types d is rounded to `type` (relative to the largest |grad_loss|) before these products, as the logits'
- * gradient of echo_cross_entropy is; of 32 bits it is not.  Rows not trained on have d = 0.  A row whose hidden state has a NaN or
- * an infinity gives NaN to every row of dweight, trained on or not.
+ * Of 16-bit types d is rounded to `type` (relative to the largest |grad_loss|, of any row) before these products, as the
+ * logits' gradient of echo_cross_entropy is; of 32 bits it is held in 24.  Rows not trained on have d = 0.  A row whose hidden state
+ * has a NaN or an infinity gives NaN to every row of dweight, trained on or not.  Logits beyond 2^127 / T count as infinite, and
+ * 32-bit elements beyond the largest of bfloat16, infinities among them, as NaN.
  * echo_linear_cross_entropy gives loss and gradients with the whole vocabulary, or a shard's lse and target;
  * echo_linear_cross_entropy_grad is given the whole vocabulary's lse.  The distillations are their counterparts.
  * rows, vocab <= 2^24, cols <= 2^20, and the product of any two <= 2^38 (else ECHO_ERR_RANGE).
  * workspace: at least echo_linear_workspace(...) bytes for the same matrices, aligned to 16; top is 0 for the cross entropies,
- * loss and grads say which of the two the call computes.  It holds at most about 1 GiB of the logits' gradient at a time, besides
- * 32-bit sums of dhidden, and copies of matrices that the products do not take as they are: those of 32 bits, and those whose cols
+ * loss and grads say which of the two the call computes.  It holds at most about 1 GiB of the logits' gradient at a time (256 columns
+ * where those are more; once more in 32 bits for losses and gradients in one call of ECHO_F32 and ECHO_F16), besides
+ * 32-bit sums of dhidden, statistics, and copies of matrices that the products do not take as they are: those of 32 bits, and those whose cols
  * are no multiple of 64, whose rows do not begin at multiples of 16 bytes or whose stride passes 2^22.
  */
 int64_t echo_linear_workspace(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,

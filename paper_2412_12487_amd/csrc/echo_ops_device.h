@@ -1,6 +1,6 @@
 // echo_ops_device.h -- what the kernels of the training-step operators (echo_ops.h) share.
 //
-// All of them move bytes: nothing multiplies matrices, and every operator's floor is the time
+// All but the output head's (echo_product.h) move bytes: every operator's floor is the time
 // to read its inputs and write its outputs once.  A lane moves 16 bytes of activations at a time with the
 // alignment of one element (the hardware takes 16 bytes from any address), rows that fit stay in registers between
 // their statistics and their result, sums and statistics are held in 32 bits, and no result depends
