@@ -103,6 +103,7 @@ struct GatherArgs {
     const float *scale;
     float factor;
     void *out;
+    bool accumulate;
 };
 
 namespace {

@@ -497,6 +497,7 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
     const auto moved = [](float2 p, float to) ECHO_INLINE { return p.x == -kInf ? p.y : p.y * __builtin_amdgcn_exp2f(p.x - to); };      // p.y is 0 there, or NaN
     float top = -kInf, sum = 0.0f;
     if (n < a.rows) {
+#pragma unroll 4
         for (int t = w; t < a.parts; t += 64) {
             const float2 p = a.stats[(int64_t)t * a.rows + n];
             const float m = fmaxf(top, p.x);
@@ -686,6 +687,18 @@ Ranges ranges_of(int64_t n, int64_t other) {
     if (middle < wide && middle <= mixed) return Ranges{(int)n, 1, 1};
     return mixed < wide ? Ranges{(int)whole * 256, 0, 1} : Ranges{(int)n, 0, 0};
 }
+// Parts of the sum that the middle tiles behind full rounds take: 256 x 8192 of the table's gradient, 128 tiles, over 16384 rows take
+// 215 us whole.
+int tail_splits(int64_t n, int64_t other, int64_t steps) {
+    const int64_t t = (int64_t)tiles(n, 128) * tiles(other, 128);
+    int64_t splits = 512 / t;
+    if (splits > steps / 16) splits = steps / 16;
+    return splits > 8 ? 8 : splits < 1 ? 1 : (int)splits;
+}
+int64_t tail_bytes(const Ranges &r, int64_t n, int64_t other, int64_t steps) {
+    const int splits = r.split < n ? tail_splits(n - r.split, other, steps) : 1;
+    return splits > 1 ? splits * (n - r.split) * other * 4 : 0;
+}
 Ranges logits_ranges(int64_t n, int64_t rows) { return rows <= 64 ? Ranges{(int)n, 2, 2} : ranges_of(n, rows); }
 // Columns of a part of the logits' statistics: what one wavefront of a tile has.
 int part_of(int shape) { return shape == 0 ? Wide::TI / Wide::WI : shape == 1 ? Middle::TI / Middle::WI : Thin::TI / Thin::WI; }
@@ -709,7 +722,7 @@ struct Plan {
     Ranges out;                    // the hidden states' gradient
     int splits;
     bool parts;
-    int64_t hidden, weight, stats, hits, local, q, prior, scale, prob, kept, part, sums, bytes;
+    int64_t hidden, weight, stats, hits, local, q, prior, scale, prob, kept, part, sums, tail, bytes;
 };
 bool direct(const void *p, int64_t stride, int type, int cols) {
     return type != ECHO_F32 && cols % kDepth == 0 && stride % 8 == 0 && stride <= int64_t(1) << 22 && (uintptr_t)p % 16 == 0;
@@ -780,6 +793,14 @@ Plan plan_of(const LinearArgs &a) {
         if (p.splits > 1) p.out = Ranges{(int)a.rows, 1, 1};
         p.parts = p.splits > 1 || p.pieces > 1;
         if (p.parts) p.part = take(p.splits * a.rows * a.cols * 4);
+        // the last piece may be narrower than the others, and have another tail
+        const int64_t last = a.vocab - (p.pieces - 1) * p.prob_cols, each = p.pieces > 1 ? p.prob_cols : last, sum = p.prob_rows / kDepth * p.pairs;
+        int64_t tail = p.parts ? 0 : tail_bytes(p.out, a.rows, a.cols, steps);
+        for (const int64_t n : {each, last}) {
+            const int64_t b = tail_bytes(ranges_of(n, a.cols), n, a.cols, sum);
+            tail = tail < b ? b : tail;
+        }
+        p.tail = take(tail);
     }
     return p;
 }
@@ -823,7 +844,8 @@ hipError_t run_logits(const HeadArgs &head, int type, int mode, int cover, const
     return hipSuccess;
 }
 // D of a product along j.
-hipError_t run_out(const OutArgs &all, int type, int out_type, bool deep, const Ranges &r, hipStream_t s) {
+// The middle tiles behind full rounds take parts of a long sum, in `tail`, where they would leave compute units idle.
+hipError_t run_out(const OutArgs &all, int type, int out_type, bool deep, const Ranges &r, float *tail, hipStream_t s) {
     const int64_t elem = out_type == ECHO_F32 ? 4 : 2;
     for (int from = 0, to; from < all.m.nj; from = to) {
         to = from ? all.m.nj : r.split;
@@ -837,8 +859,16 @@ hipError_t run_out(const OutArgs &all, int type, int out_type, bool deep, const 
             o.m.b.width -= from;
         o.out = static_cast<char *>(o.out) + (int64_t)from * o.m.ni * elem;
         if (o.parts) o.parts += (int64_t)from * o.m.ni;
+        const int splits = from && !o.parts ? tail_splits(o.m.nj, o.m.ni, (int64_t)o.m.steps * o.m.pairs) : 1;
+        if (splits > 1) {
+            o.m.splits = splits;
+            o.parts = tail;
+            o.part = (int64_t)o.m.nj * o.m.ni;
+        }
         tile(o.m, o.m.ni, o.m.nj, shape);
-        const hipError_t e = launch_out(o, type, out_type, deep, shape, s);
+        hipError_t e = launch_out(o, type, out_type, deep, shape, s);
+        if (e == hipSuccess && splits > 1)
+            e = launch_gather(GatherArgs{tail, o.part, splits, o.scale, o.factor, o.out, o.accumulate}, type, out_type, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -924,7 +954,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
     if (!p.keep && !p.few) ECHO_HIP(launch_scale(a.grad_loss, h.rows, reinterpret_cast<float *>(w + p.scale), s));
     const Operand prob{h.prob, h.prob_stride, h.prob_plane, p.prob_rows, (int)p.prob_cols};
     const int64_t grad_elem = a.grad_type == ECHO_F32 ? 4 : 2;
-    float *parts = p.parts ? reinterpret_cast<float *>(w + p.part) : nullptr;
+    float *parts = p.parts ? reinterpret_cast<float *>(w + p.part) : nullptr, *tail = reinterpret_cast<float *>(w + p.tail);
     for (int64_t piece = 0; piece < p.pieces; ++piece) {
         const int64_t first = piece * p.prob_cols, left = a.vocab - first;
         const int n = (int)(left < p.prob_cols ? left : p.prob_cols);
@@ -954,7 +984,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         const bool both = p.out.split == a.rows && p.out.shape0 == 1 && table_out.split == n && table_out.shape0 == 1;
         OutArgs first_out = o;
         tile(first_out.m, a.cols, h.rows, 1);
-        if (!both) ECHO_HIP(run_out(o, a.type, a.type, true, p.out, s));
+        if (!both) ECHO_HIP(run_out(o, a.type, a.type, true, p.out, tail, s));
         o.m = Product{hidden, prob, a.cols, n, 0, 0, (int)(p.prob_rows / kDepth), p.pairs, 1};
         o.parts = nullptr;
         o.out = static_cast<char *>(a.dweight) + first * a.cols * grad_elem;
@@ -963,11 +993,11 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
             tile(o.m, a.cols, n, 1);
             ECHO_HIP(launch_both(first_out, o, a.type, a.grad_type, s));
         } else {
-            ECHO_HIP(run_out(o, a.type, a.grad_type, false, table_out, s));
+            ECHO_HIP(run_out(o, a.type, a.grad_type, false, table_out, tail, s));
         }
     }
     if (parts)
-        ECHO_HIP(launch_gather(GatherArgs{parts, a.rows * a.cols, p.splits, h.scale, a.temperature, a.dhidden}, a.type, a.type, s));
+        ECHO_HIP(launch_gather(GatherArgs{parts, a.rows * a.cols, p.splits, h.scale, a.temperature, a.dhidden, false}, a.type, a.type, s));
     return hipSuccess;
 }
 

@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256) void k_gather(GatherArgs a, float unit) {
         lds[wave][lane] = d;
         __syncthreads();
         if (wave || left <= 0) continue;
-        put4(static_cast<U *>(a.out) + at, left, (((lds[0][lane] + lds[1][lane]) + lds[2][lane]) + lds[3][lane]) * scale, false);
+        put4(static_cast<U *>(a.out) + at, left, (((lds[0][lane] + lds[1][lane]) + lds[2][lane]) + lds[3][lane]) * scale, a.accumulate);
     }
 }
 

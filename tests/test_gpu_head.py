@@ -117,14 +117,16 @@ def test_linear_losses_of_whole_tiles(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("rows,cols,vocab", [(2048, 128, 8900), (300, 2048, 8900), (2300, 8192, 300)])
+@pytest.mark.parametrize("rows,cols,vocab", [(2048, 128, 8900), (300, 2048, 8900), (2300, 8192, 300), (2300, 2048, 8900), (2300, 8192, 2100)])
 def test_linear_losses_of_two_shapes_of_tiles(rows, cols, vocab, dtype):
-    """A full launch of wide tiles and some middle ones behind it: of the logits, of the table's and of the hidden states' gradient."""
+    """A full launch of wide tiles and some middle ones behind it: of the logits, of the table's and of the hidden states' gradient;
+    with longer sums, of which the middle tiles take parts."""
     h, w, t, g = _case(rows, cols, vocab, dtype, 5)
     out = E.linear_cross_entropy(h, w, t, grad_loss=g)
     _close(out, R.linear(h, w, R.targets(t, vocab), 0, vocab, grad_loss=g))
-    got = E.linear_cross_entropy_grad(h, w, t, out["lse"], g)
-    _close(got, R.linear(h, w, R.targets(t, vocab), 0, vocab, lse=out["lse"], grad_loss=g))
+    old = _normal(_gen(1), vocab, cols, std=1e-3, dtype=dtype)
+    got = E.linear_cross_entropy_grad(h, w, t, out["lse"], g, out={"dweight": old.clone()}, accumulate=True)
+    _close(got, R.linear(h, w, R.targets(t, vocab), 0, vocab, lse=out["lse"], grad_loss=g, old=old))
     ids, z = _teacher(rows, 70, vocab, 7)
     _close(E.linear_distillation(h, w, ids, z, grad_loss=g, temperature=2.0),
            R.linear(h, w, R.entries(ids, z, vocab, 2.0), 0, vocab, 2.0, grad_loss=g))
