@@ -10,11 +10,9 @@ struct Row {
     bool trained;
     int at;
 };
-__device__ __forceinline__ Row row_of(const HeadArgs &a, int n) {
-    if (a.top) return Row{a.prior[n].y > 0.0f, -1};
-    const int64_t t = a.wide_index ? id_at<int64_t>(a.targets, n) : id_at<int32_t>(a.targets, n);
-    const bool trained = t >= 0 && t < a.vocab_size;
-    return Row{trained, trained ? shard_row(t, a.vocab_start, a.vocab) : -1};
+__device__ __forceinline__ Row row_of(const HeadArgs &a, int64_t target) {
+    const bool trained = target >= 0 && target < a.vocab_size;
+    return Row{trained, trained ? shard_row(target, a.vocab_start, a.vocab) : -1};
 }
 
 // The teacher's entries of a tile: a cell of 16 bits for each of its logits, 0 or the entry's number and one more.  Cells of
@@ -88,11 +86,24 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
         if ((int)blockIdx.x == a.m.tiles_i * a.m.tiles_j)
             return write_scale<S::THREADS>(a.grad_loss, a.rows, a.scale_out, reinterpret_cast<float *>(t0));
     const Place at = place_of(a.m, blockIdx.x);
-    F4 acc[S::BI][S::BJ];
-    multiply<T, true, true, S>(a.m, at, t0, t1, acc);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wi = wave / S::WJ, wj = wave % S::WJ;
     const int i0 = at.ti * S::TI, j0 = at.tj * S::TJ, il = wi * S::BI * 16 + (lane / 16) * 4, jl = wj * S::BJ * 16 + lane % 16;
+    F4 acc[S::BI][S::BJ];
+    multiply<T, true, true, S>(a.m, at, t0, t1, acc);
+    // What a lane's rows need, all loads together; of rows past the end, the last one's.
+    int64_t target[S::BJ];
+    float lse_of[S::BJ], grad_of[S::BJ], mass_of[S::BJ];
+#pragma unroll
+    for (int b = 0; b < S::BJ; ++b) {
+        const int n = j0 + jl + b * 16 < a.rows ? j0 + jl + b * 16 : a.rows - 1;
+        if (!a.top) target[b] = a.wide_index ? id_at<int64_t>(a.targets, n) : id_at<int32_t>(a.targets, n);
+        if constexpr (MODE == kGrad) {
+            lse_of[b] = a.lse[n];
+            grad_of[b] = a.grad_loss[n];
+            if (a.top) mass_of[b] = a.prior[n].y;
+        }
+    }
     const Cells<S> cells{t0, t1};
     if (a.top) cells.fill(a, a.first + i0, j0);      // entries' columns count from the shard's first id
     using Quad = __attribute__((ext_vector_type(4))) unsigned short;
@@ -120,7 +131,7 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[k][b][e]);
             if (!a.top) {
-                const int hit = live ? row_of(a, n).at - a.first - (i0 + il) : -1;      // below 0 where it is not here
+                const int hit = live ? row_of(a, target[b]).at - a.first - (i0 + il) : -1;      // below 0 where it is not here
                 if (hit >= 0 && hit < S::BI * 16) {
 #pragma unroll
                     for (int k = 0; k < S::BI; ++k)
@@ -183,11 +194,11 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
             int hit = -1;
             float lse = 0.0f, g = 0.0f;
             if (live) {
-                const Row r = row_of(a, n);
+                const Row r = a.top ? Row{mass_of[b] > 0.0f, -1} : row_of(a, target[b]);
                 hit = r.at - a.first;      // below 0 where it is not here
-                lse = a.lse[n];
+                lse = lse_of[b];
                 live = r.trained && lse != -kInf;
-                g = a.grad_loss[n] / scale * kUnit<T>;
+                g = grad_of[b] / scale * kUnit<T>;
                 lse *= kLog2e;
             }
             if (PLANES > 1 && n >= a.prob_rows) continue;
