@@ -64,16 +64,18 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_out(OutArgs a)
     __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
     out_tile<T, U, S, DEEP>(a, blockIdx.x, t0, t1);
 }
-// Both gradients in one launch, where neither fills the GPU (8 rows of 6592, 256 ids: 6 us in place of 12): the hidden states' of type U, the table's of type W.
+// Both gradients in one launch, where neither fills the GPU (8 rows of 6592, 256 ids: 6 us in place of 12), the longer
+// sums first: the hidden states' of type U, the table's of type W.
 template <class T, class U, class W, class S>
-__global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_both(OutArgs hidden, OutArgs table) {
+__global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_both(OutArgs hidden, OutArgs table, int table_first) {
     __shared__ __attribute__((aligned(16))) char t0[S::BYTES];
     __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
-    const int first = hidden.m.tiles_i * hidden.m.tiles_j * hidden.m.splits;
-    if ((int)blockIdx.x < first)
-        out_tile<T, U, S, true>(hidden, blockIdx.x, t0, t1);
+    const int of_hidden = hidden.m.tiles_i * hidden.m.tiles_j * hidden.m.splits, of_table = table.m.tiles_i * table.m.tiles_j;
+    const int id = table_first ? (int)blockIdx.x - of_table : (int)blockIdx.x;
+    if (table_first ? id >= 0 : id < of_hidden)
+        out_tile<T, U, S, true>(hidden, id, t0, t1);
     else
-        out_tile<T, W, S, false>(table, blockIdx.x - first, t0, t1);
+        out_tile<T, W, S, false>(table, table_first ? (int)blockIdx.x : id - of_hidden, t0, t1);
 }
 
 // Sums the parts: four wavefronts take a quarter of them each, in their order, of 256 elements side by side.
@@ -130,13 +132,14 @@ hipError_t launch_out(const OutArgs &a, int type, int out_type, bool deep, int s
 hipError_t launch_both(const OutArgs &a, const OutArgs &b, int type, int grad_type, hipStream_t s) {
     const dim3 grid((unsigned)(a.m.tiles_i * a.m.tiles_j * a.m.splits + b.m.tiles_i * b.m.tiles_j)), block(Middle::THREADS);
     const bool wide = grad_type == ECHO_F32;
+    const int t = (int64_t)b.m.steps * a.m.splits > a.m.steps;
     switch (type) {
-        case ECHO_F32: return launch(k_both<bf16, float, float, Middle>, grid, block, s, a, b);
+        case ECHO_F32: return launch(k_both<bf16, float, float, Middle>, grid, block, s, a, b, t);
         case ECHO_F16:
-            return wide ? launch(k_both<f16, f16, float, Middle>, grid, block, s, a, b) : launch(k_both<f16, f16, f16, Middle>, grid, block, s, a, b);
+            return wide ? launch(k_both<f16, f16, float, Middle>, grid, block, s, a, b, t) : launch(k_both<f16, f16, f16, Middle>, grid, block, s, a, b, t);
         default:
-            return wide ? launch(k_both<bf16, bf16, float, Middle>, grid, block, s, a, b)
-                        : launch(k_both<bf16, bf16, bf16, Middle>, grid, block, s, a, b);
+            return wide ? launch(k_both<bf16, bf16, float, Middle>, grid, block, s, a, b, t)
+                        : launch(k_both<bf16, bf16, bf16, Middle>, grid, block, s, a, b, t);
     }
 }
 hipError_t launch_zero(void *out, int64_t bytes, hipStream_t s) {
