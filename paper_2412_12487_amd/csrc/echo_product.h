@@ -42,7 +42,6 @@ using F4 = __attribute__((ext_vector_type(4))) float;
 template <class T>
 using H8 = __attribute__((ext_vector_type(8))) T;
 using S4 = __attribute__((ext_vector_type(4))) short;
-using S8 = __attribute__((ext_vector_type(8))) short;
 using LdsPtr = __attribute__((address_space(3))) void *;
 
 constexpr int kDepth = 64;
