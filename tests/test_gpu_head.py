@@ -189,6 +189,23 @@ def test_linear_pieces_of_the_vocabulary(dtype):
     _close(out, R.linear(h, w, R.entries(ids, z, vocab, 1.0), 0, vocab, grad_loss=g))
 
 
+def test_linear_many_rows():
+    """Pieces of the vocabulary whose shares of the gradient are a gigabyte each, and sums over a million rows."""
+    rows, cols, vocab, chunk = 1_100_000, 64, 1000, 100_000
+    h, w, t, _ = _case(rows, cols, vocab, F16, 4)
+    g = torch.ones(rows, device="cuda")
+    out = E.linear_cross_entropy(h, w, t, grad_loss=g, dtype=F32)
+    value = bound = 0
+    for i in range(0, rows, chunk):
+        at = slice(i, i + chunk)
+        ref = R.linear(h[at], w, R.targets(t[at], vocab), 0, vocab, grad_loss=g[at])
+        v, e = ref.pop("dweight")
+        # a chunk's bound has 2 U chunk times the sum of its terms' sizes, the whole sum's 2 U rows times it
+        value, bound = value + v, bound + e * (rows / chunk)
+        _close({k: out[k][at] for k in ref if k in out}, ref, [k for k in ref if k in out])
+    R.close(out["dweight"], value, bound, "dweight")
+
+
 def test_linear_table_past_32_bits():
     rows, cols, vocab = 3, 2048, 1_100_000      # 4.5 GB of bf16
     g = _gen(3)
