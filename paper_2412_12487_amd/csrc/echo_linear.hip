@@ -708,17 +708,19 @@ Ranges ranges_of(int64_t n, int64_t other) {
     if (middle < wide && middle <= mixed) return Ranges{(int)n, 1, 1};
     return mixed < wide ? Ranges{(int)whole * 256, 0, 1} : Ranges{(int)n, 0, 0};
 }
-// Parts of the sum that the middle tiles behind full rounds take: 256 x 8192 of the table's gradient, 128 tiles, over 16384 rows take
-// 215 us whole.
+// Parts of the sum that middle tiles take where they leave compute units idle: behind full rounds of wide ones (256 x 8192 of the
+// table's gradient, 128 tiles, over 16384 rows: 217 us whole and 103 in parts), or by themselves (224 x 1346 of it over 7320 rows of
+// 32 bits, 22 tiles of 690 steps, took 550 us whole).
 int tail_splits(int64_t n, int64_t other, int64_t steps) {
     const int64_t t = (int64_t)tiles(n, 128) * tiles(other, 128);
     int64_t splits = 512 / t;
     if (splits > steps / 16) splits = steps / 16;
-    return splits > 8 ? 8 : splits < 1 ? 1 : (int)splits;
+    return splits > 32 ? 32 : splits < 1 ? 1 : (int)splits;
 }
 int64_t tail_bytes(const Ranges &r, int64_t n, int64_t other, int64_t steps) {
-    const int splits = r.split < n ? tail_splits(n - r.split, other, steps) : 1;
-    return splits > 1 ? splits * (n - r.split) * other * 4 : 0;
+    const int64_t middle = n - (r.shape0 == 1 ? 0 : r.split);
+    const int splits = middle > 0 ? tail_splits(middle, other, steps) : 1;
+    return splits > 1 ? splits * middle * other * 4 : 0;
 }
 Ranges logits_ranges(int64_t n, int64_t rows) { return rows <= 64 ? Ranges{(int)n, 2, 2} : ranges_of(n, rows); }
 // Columns of a part of the logits' statistics: what one wavefront of a tile has.
@@ -865,7 +867,7 @@ hipError_t run_logits(const HeadArgs &head, int type, int mode, int cover, const
     return hipSuccess;
 }
 // D of a product along j.
-// The middle tiles behind full rounds take parts of a long sum, in `tail`, where they would leave compute units idle.
+// Middle tiles take parts of a long sum, in `tail`, where they would leave compute units idle.
 hipError_t run_out(const OutArgs &all, int type, int out_type, bool deep, const Ranges &r, float *tail, hipStream_t s) {
     const int64_t elem = out_type == ECHO_F32 ? 4 : 2;
     for (int from = 0, to; from < all.m.nj; from = to) {
@@ -880,11 +882,12 @@ hipError_t run_out(const OutArgs &all, int type, int out_type, bool deep, const 
             o.m.b.width -= from;
         o.out = static_cast<char *>(o.out) + (int64_t)from * o.m.ni * elem;
         if (o.parts) o.parts += (int64_t)from * o.m.ni;
-        const int splits = from && !o.parts ? tail_splits(o.m.nj, o.m.ni, (int64_t)o.m.steps * o.m.pairs) : 1;
+        const int splits = shape == 1 && !o.parts ? tail_splits(o.m.nj, o.m.ni, (int64_t)o.m.steps * o.m.pairs) : 1;
         if (splits > 1) {
             o.m.splits = splits;
             o.parts = tail;
             o.part = (int64_t)o.m.nj * o.m.ni;
+            o.add_parts = false;
         }
         tile(o.m, o.m.ni, o.m.nj, shape);
         hipError_t e = launch_out(o, type, out_type, deep, shape, s);
@@ -1011,8 +1014,17 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         o.out = static_cast<char *>(a.dweight) + first * a.cols * grad_elem;
         o.accumulate = a.accumulate;
         if (both) {
+            const int splits = tail_splits(n, a.cols, (int64_t)o.m.steps * o.m.pairs);
             tile(o.m, a.cols, n, 1);
+            if (splits > 1) {
+                o.m.splits = splits;
+                o.parts = tail;
+                o.part = (int64_t)n * a.cols;
+                o.add_parts = false;
+            }
             ECHO_HIP(launch_both(first_out, o, a.type, a.grad_type, s));
+            if (splits > 1)
+                ECHO_HIP(launch_gather(GatherArgs{tail, o.part, splits, o.scale, o.factor, o.out, o.accumulate}, a.type, a.grad_type, s));
         } else {
             ECHO_HIP(run_out(o, a.type, a.grad_type, false, table_out, tail, s));
         }

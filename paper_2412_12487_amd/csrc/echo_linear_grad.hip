@@ -70,7 +70,7 @@ template <class T, class U, class W, class S>
 __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_both(OutArgs hidden, OutArgs table, int table_first) {
     __shared__ __attribute__((aligned(16))) char t0[S::BYTES];
     __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
-    const int of_hidden = hidden.m.tiles_i * hidden.m.tiles_j * hidden.m.splits, of_table = table.m.tiles_i * table.m.tiles_j;
+    const int of_hidden = hidden.m.tiles_i * hidden.m.tiles_j * hidden.m.splits, of_table = table.m.tiles_i * table.m.tiles_j * table.m.splits;
     const int id = table_first ? (int)blockIdx.x - of_table : (int)blockIdx.x;
     if (table_first ? id >= 0 : id < of_hidden)
         out_tile<T, U, S, true>(hidden, id, t0, t1);
@@ -130,9 +130,9 @@ hipError_t launch_out(const OutArgs &a, int type, int out_type, bool deep, int s
     return out_type == ECHO_F32 ? out<bf16, float>(a, deep, shape, s) : out<bf16, bf16>(a, deep, shape, s);
 }
 hipError_t launch_both(const OutArgs &a, const OutArgs &b, int type, int grad_type, hipStream_t s) {
-    const dim3 grid((unsigned)(a.m.tiles_i * a.m.tiles_j * a.m.splits + b.m.tiles_i * b.m.tiles_j)), block(Middle::THREADS);
+    const dim3 grid((unsigned)(a.m.tiles_i * a.m.tiles_j * a.m.splits + b.m.tiles_i * b.m.tiles_j * b.m.splits)), block(Middle::THREADS);
     const bool wide = grad_type == ECHO_F32;
-    const int t = (int64_t)b.m.steps * a.m.splits > a.m.steps;
+    const int t = (int64_t)b.m.steps * a.m.splits > (int64_t)a.m.steps * b.m.splits;
     switch (type) {
         case ECHO_F32: return launch(k_both<bf16, float, float, Middle>, grid, block, s, a, b, t);
         case ECHO_F16:

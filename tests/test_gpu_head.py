@@ -133,6 +133,28 @@ def test_linear_losses_of_two_shapes_of_tiles(rows, cols, vocab, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,vocab", [(7320, 130, 224), (3000, 896, 1283), (5000, 3000, 700)])
+def test_linear_losses_of_many_rows_and_few_ids(rows, cols, vocab, dtype):
+    """The table's gradient has few tiles and a long sum, of which workgroups take parts."""
+    h, w, t, g = _case(rows, cols, vocab, dtype, 5)
+    old = _normal(_gen(1), vocab, cols, std=1e-3, dtype=dtype)
+    got = E.linear_cross_entropy(h, w, t, grad_loss=g, out={"dweight": old.clone()}, accumulate=True)
+    _close(got, R.linear(h, w, R.targets(t, vocab), 0, vocab, grad_loss=g, old=old))
+    lse = got["lse"]
+    got = E.linear_cross_entropy_grad(h, w, t, lse, g, dtype=F32)
+    _close(got, R.linear(h, w, R.targets(t, vocab), 0, vocab, lse=lse, grad_loss=g))
+
+
+def test_linear_pieces_with_two_shapes_of_tiles():
+    """Pieces of the vocabulary after the first, of whose table's gradient the middle tiles take parts."""
+    rows, cols, vocab = 40000, 1024, 26000
+    h, w, t, g = _case(rows, cols, vocab, BF16, 5)
+    lse = E.linear_cross_entropy(h, w, t, vocab_start=0, vocab_size=vocab)["lse"]
+    got = E.linear_cross_entropy_grad(h, w, t, lse, g)
+    _close(got, R.linear(h, w, R.targets(t, vocab), 0, vocab, lse=lse, grad_loss=g))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols,vocab", [(512, 512, 4096), (2048, 128, 9000), (200, 2048, 300), (40, 128, 60000)])
 def test_products_without_rounding(rows, cols, vocab, dtype):
     """Small whole numbers: every product and every sum is exact, so that logits are the plain form's to the last bit and the
