@@ -649,8 +649,9 @@ hipError_t rows(const RowsArgs &a, hipStream_t s) {
                                         : reinterpret_cast<const void *>(k_rows<T, PLANES, 1024>);
     return hipLaunchKernel(kernel, dim3(a.prob ? a.prob_rows : a.rows), dim3(block), args, sizeof(Entry) * a.in.top, s);
 }
-hipError_t launch_rows(const RowsArgs &a, int type, hipStream_t s) {
-    return type == ECHO_F32 ? rows<bf16, 3>(a, s) : type == ECHO_F16 ? rows<f16, 1>(a, s) : rows<bf16, 1>(a, s);
+hipError_t launch_rows(const RowsArgs &a, int type, int planes, hipStream_t s) {
+    if (type == ECHO_F16) return planes == 2 ? rows<f16, 2>(a, s) : rows<f16, 1>(a, s);
+    return planes == 3 ? rows<bf16, 3>(a, s) : planes == 2 ? rows<bf16, 2>(a, s) : rows<bf16, 1>(a, s);
 }
 hipError_t launch_join(const JoinArgs &a, hipStream_t s) { return launch(k_join, dim3((a.rows + 15) / 16), dim3(1024), s, a); }
 hipError_t launch_teacher(const TeacherArgs &a, hipStream_t s) {
@@ -733,7 +734,8 @@ void tile(Product &m, int ni, int nj, int shape) {
 
 // Sizes of a call's products, and where its workspace has what.
 struct Plan {
-    int planes, pairs;
+    int planes, pairs;             // of the logits' products
+    int share_planes, share_pairs; // of the gradients'
     int width;                     // hidden size in whole steps
     bool copy_hidden, copy_weight;
     Ranges logits;                 // the loss's
@@ -797,16 +799,20 @@ Plan plan_of(const LinearArgs &a) {
     }
     if (a.grads) {
         p.scale = take(4);
+        // Of few rows a single rounding of a share to 16 bits may be most of an output's error (two rows of half precision: 1.75
+        // times the plain form's): they are held in two planes, at no cost that counts there.
+        p.share_planes = a.type == ECHO_F32 ? 3 : p.few && a.rows <= 64 ? 2 : 1;
+        p.share_pairs = a.type == ECHO_F32 ? 6 : p.share_planes;
         p.prob_rows = up(a.rows, kDepth);
         const int64_t whole = up(a.vocab, kDepth);
-        int64_t most = kProbBytes / (p.prob_rows * 2 * p.planes) / 256 * 256;
+        int64_t most = kProbBytes / (p.prob_rows * 2 * p.share_planes) / 256 * 256;
         most = most < 256 ? 256 : most > kProbCols ? kProbCols : most;
         p.pieces = (whole + most - 1) / most;
         p.prob_cols = p.pieces == 1 ? whole : up((whole + p.pieces - 1) / p.pieces, 256);
-        p.prob = take(p.prob_rows * p.prob_cols * 2 * p.planes);
+        p.prob = take(p.prob_rows * p.prob_cols * 2 * p.share_planes);
         p.keep = a.forward && p.pieces == 1 && !p.few;
         if (p.keep) p.kept = a.type == ECHO_BF16 ? p.prob : take(a.rows * p.prob_cols * 4);
-        const int64_t middle = (int64_t)tiles(a.cols, 128) * tiles(a.rows, 128), steps = p.prob_cols / kDepth * p.pairs;
+        const int64_t middle = (int64_t)tiles(a.cols, 128) * tiles(a.rows, 128), steps = p.prob_cols / kDepth * p.share_pairs;
         p.out = ranges_of(a.rows, a.cols);
         // too few tiles to fill the GPU: workgroups take parts of the sum
         int64_t splits = middle < 512 ? 512 / middle : 1;
@@ -817,7 +823,7 @@ Plan plan_of(const LinearArgs &a) {
         p.parts = p.splits > 1 || p.pieces > 1;
         if (p.parts) p.part = take(p.splits * a.rows * a.cols * 4);
         // the last piece may be narrower than the others, and have another tail
-        const int64_t last = a.vocab - (p.pieces - 1) * p.prob_cols, each = p.pieces > 1 ? p.prob_cols : last, sum = p.prob_rows / kDepth * p.pairs;
+        const int64_t last = a.vocab - (p.pieces - 1) * p.prob_cols, each = p.pieces > 1 ? p.prob_cols : last, sum = p.prob_rows / kDepth * p.share_pairs;
         int64_t tail = p.parts ? 0 : tail_bytes(p.out, a.rows, a.cols, steps);
         for (const int64_t n : {each, last}) {
             const int64_t b = tail_bytes(ranges_of(n, a.cols), n, a.cols, sum);
@@ -960,7 +966,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         ECHO_HIP(launch_rows(RowsArgs{c.parts, c.part, p.few_splits, c.ld, h.rows, a.vocab, (int)p.prob_cols, in,
                                       a.temperature * a.temperature, a.lse, a.target, a.entropy, a.loss, a.forward ? nullptr : a.lse_in,
                                       a.grad_loss, h.scale, a.grads ? h.prob : nullptr, h.prob_stride, h.prob_plane, h.prob_rows},
-                             a.type, s));
+                             a.type, p.share_planes, s));
     } else if (a.forward) {
         h.stats = reinterpret_cast<float2 *>(w + p.stats);
         h.hits = reinterpret_cast<float *>(w + p.hits);
@@ -999,7 +1005,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         OutArgs o{};
         o.scale = h.scale;
         o.factor = a.temperature;
-        o.m = Product{table, prob, a.cols, (int)a.rows, 0, 0, (int)(p.prob_cols / kDepth), p.pairs, p.splits};
+        o.m = Product{table, prob, a.cols, (int)a.rows, 0, 0, (int)(p.prob_cols / kDepth), p.share_pairs, p.splits};
         o.parts = parts;
         o.part = a.rows * a.cols;
         o.add_parts = piece > 0;
@@ -1009,7 +1015,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         OutArgs first_out = o;
         tile(first_out.m, a.cols, h.rows, 1);
         if (!both) ECHO_HIP(run_out(o, a.type, a.type, true, p.out, tail, s));
-        o.m = Product{hidden, prob, a.cols, n, 0, 0, (int)(p.prob_rows / kDepth), p.pairs, 1};
+        o.m = Product{hidden, prob, a.cols, n, 0, 0, (int)(p.prob_rows / kDepth), p.share_pairs, 1};
         o.parts = nullptr;
         o.out = static_cast<char *>(a.dweight) + first * a.cols * grad_elem;
         o.accumulate = a.accumulate;

@@ -31,7 +31,7 @@ struct Product {
     int ni, nj;               // size of D
     int tiles_i, tiles_j;
     int steps;                // of 64 along k, in a plane
-    int pairs;                // products of planes that are summed: 1, or 6 of 3 planes each
+    int pairs;                // products of planes that are summed: 1, 2 of two planes of b, or 6 of 3 planes each
     int splits;               // parts of the steps, each in a workgroup of its own
 };
 // 3 planes of 8 significant bits each make 24: the products that matter, of planes (a, b).
