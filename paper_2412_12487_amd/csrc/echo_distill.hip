@@ -29,10 +29,12 @@ __device__ __forceinline__ void put_entries(T *grad, const Entry *entries, int t
 }
 __device__ __forceinline__ float finish_row(const DistillArgs &a, int64_t row, const Teacher &t, const Entry *entries, float top, float sum) {
     const float more = logf(sum), lse = top == -kInf ? -kInf : top + more;
-    const float cross = cross_of(entries, a.top, a.loss && lse != -kInf ? top : 0.0f);
+    // the loss takes logits from their maximum on, the target as they are
+    const float cross = a.loss ? cross_of(entries, a.top, lse != -kInf ? top : 0.0f) : 0.0f;
+    const float target = a.target ? cross_of(entries, a.top, 0.0f) : 0.0f;
     if (threadIdx.x % kWave == 0) {
         if (a.lse) a.lse[row] = lse;
-        if (a.target) a.target[row] = cross;
+        if (a.target) a.target[row] = target;
         if (a.entropy) a.entropy[row] = -t.prior;
         if (a.loss)
             a.loss[row] = !t.trained ? 0.0f : lse == -kInf ? kInf : a.temperature * a.temperature * (t.prior - cross + more);

@@ -404,11 +404,14 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
         const float more = logf(sum);
         lse = top == -kInf ? -kInf : top + more;
         if (threadIdx.x < kWave) {
-            const float from = a.loss && lse != -kInf ? top : 0.0f;      // the loss takes logits from their maximum on
-            const float cross = a.in.top ? cross_of(entries, a.in.top, from) : at >= 0 ? logit(at) - from : 0.0f;
+            // the loss takes logits from their maximum on, the target as they are
+            const auto sum_from = [&](float from) ECHO_INLINE {
+                return a.in.top ? cross_of(entries, a.in.top, from) : at >= 0 ? logit(at) - from : 0.0f;
+            };
+            const float cross = a.loss ? sum_from(lse != -kInf ? top : 0.0f) : 0.0f, target = a.target ? sum_from(0.0f) : 0.0f;
             if (threadIdx.x == 0) {
                 if (a.lse) a.lse[n] = lse;
-                if (a.target) a.target[n] = cross;
+                if (a.target) a.target[n] = target;
                 if (a.entropy) a.entropy[n] = -t.prior;
                 if (a.loss) a.loss[n] = !trained ? 0.0f : lse == -kInf ? kInf : a.square * (t.prior - cross + more);
             }
@@ -537,21 +540,28 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
     __syncthreads();
     top = part[0][r].x * kLn2;
     sum = part[0][r].y;
-    float cross = 0.0f;
+    float cross = 0.0f, target = 0.0f;
     if (a.top) {
-        // the loss takes logits from their maximum on
-        const float from = a.loss && top != -kInf && sum == sum ? top : 0.0f;
+        // the loss takes logits from their maximum on, the target as they are
+        const float from = top != -kInf && sum == sum ? top : 0.0f;
         if (n < a.rows) {
             for (int k = w; k < a.top; k += 64) {
                 const int64_t e = (int64_t)n * a.top + k;
-                if (a.local[e] >= 0) cross += a.q[e] * (a.hits[e] - from);
+                if (a.local[e] < 0) continue;
+                const float q = a.q[e], x = a.hits[e];
+                cross += q * (x - from);
+                target += q * x;
             }
         }
         for (int by = 32; by; by /= 2) {
             __syncthreads();
-            part[w][r].x = cross;
+            part[w][r] = make_float2(cross, target);
             __syncthreads();
-            if (w < by) cross += part[w + by][r].x;
+            if (w < by) {
+                const float2 o = part[w + by][r];
+                cross += o.x;
+                target += o.y;
+            }
         }
     }
     if (w || n >= a.rows) return;
@@ -568,7 +578,7 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
     }
     const float2 prior = a.prior[n];
     const bool trained = prior.y > 0.0f;
-    if (a.target) a.target[n] = cross;
+    if (a.target) a.target[n] = target;
     if (a.entropy) a.entropy[n] = -prior.x;
     if (a.loss) a.loss[n] = !trained ? 0.0f : lse == -kInf ? kInf : a.square * (prior.x - cross + more);
 }
