@@ -17,8 +17,8 @@ struct HeadArgs {
     const int *local;             // [rows][top]: an entry's column here, or -1
     const float *q;               // [rows][top]
     const float2 *prior;          // [rows]: sum of q log q, and 1 where the row is trained on
-    float2 *stats;                // [parts][rows]: log2 of the largest exponential, and sum relative to it, of a wavefront's columns
-    float *hits;                  // logits of the target or of the entries
+    float2 *stats;                // [parts][rows]: largest product, and sum of exponentials relative to it, of a wavefront's columns
+    float *hits;                  // products of the target or of the entries
     const float *lse, *grad_loss, *scale;
     float *scale_out;             // one workgroup more writes it, or null
     char *prob;                   // [planes][prob_rows][.]: the gradient's shares
@@ -34,6 +34,7 @@ struct ShareArgs {
     const void *targets, *kept;
     int wide_index, top, rows, vocab, cols;
     int64_t vocab_start, vocab_size;
+    float inv_t;
     int split, part0, part1;      // columns that a part of the statistics has, before `split` and from it on
     char *prob;                   // [planes][prob_rows][cols]
     int64_t prob_stride, prob_plane;
@@ -46,7 +47,7 @@ struct JoinArgs {
     const void *targets;
     int wide_index, top, rows, vocab, parts;
     int64_t vocab_start, vocab_size;
-    float square;                 // T^2
+    float inv_t, square;          // 1 / T, T^2
     float *lse, *target, *entropy, *loss;
 };
 struct TeacherArgs {

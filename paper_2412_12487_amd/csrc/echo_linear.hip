@@ -107,9 +107,9 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
     const Cells<S> cells{t0, t1};
     if (a.top) cells.fill(a, a.first + i0, j0);      // entries' columns count from the shard's first id
     using Quad = __attribute__((ext_vector_type(4))) unsigned short;
-    // Everything per element counts here, 128 of them a lane: a logit is a maximum, one fused multiplication and addition, an
-    // exponential and an addition.  Maxima are of the products, and statistics in powers of two: 2^(D k - base) with
-    // k = log2(e) / T, rounded once in the exponent.
+    // Everything per element counts here, 128 of them a lane.  Maxima are of the products, and exponentials 2^((D - top) k) with
+    // k = log2(e) / T: distances between numbers of one size are exact, so that the maximum's own is 1 whatever the logits' size.
+    // (2^(D k - top k) in one fused operation has the rounding of top k in its exponent: 0.06 at logits of 2^20, 4 at 2^27.)
     const float k2 = a.inv_t * kLog2e;
     if (i0 + S::TI > a.m.ni) {
 #pragma unroll
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
                     for (int k = 0; k < S::BI; ++k)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (k * 16 + e == hit) a.hits[n] = acc[k][b][e] * a.inv_t;
+                            if (k * 16 + e == hit) a.hits[n] = acc[k][b][e];
                 }
             } else {
 #pragma unroll
@@ -146,18 +146,18 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
                     if (!__builtin_bit_cast(int64_t, entry) || !live) continue;
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (entry[e]) a.hits[(int64_t)n * a.top + entry[e] - 1] = acc[k][b][e] * a.inv_t;
+                        if (entry[e]) a.hits[(int64_t)n * a.top + entry[e] - 1] = acc[k][b][e];
                 }
             }
             top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32)) * k2;
+            top = fmaxf(top, __shfl_xor(top, 32));
             const float base = top == -kInf ? 0.0f : top;
             float sum = 0.0f;
 #pragma unroll
             for (int k = 0; k < S::BI; ++k) {
                 F4 d;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum += d[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[k][b][e], k2, -base));
+                for (int e = 0; e < 4; ++e) sum += d[e] = __builtin_amdgcn_exp2f((acc[k][b][e] - base) * k2);
                 if constexpr (MODE == kKeep && sizeof(Kept<T, PLANES>) == 2) {
                     acc[k][b] = d;
                 } else if constexpr (MODE == kKeep) {
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
     const int n = blockIdx.x, splits = a.splits, ld = a.ld, vocab = a.vocab;
     const bool keeps = a.prob != nullptr;
     const int64_t part = a.part, plane_bytes = a.prob_plane;
-    const float inv_t = a.in.inv_t;
+    const float inv_t = a.in.inv_t, k2 = inv_t * kLog2e;
     char *prob = a.prob + n * a.prob_stride;
     const auto put = [&](int c, auto d) ECHO_INLINE {
         constexpr int N = sizeof(d) / 4;
@@ -340,19 +340,19 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
                     if (p0 + p < splits) d[g] += v[p][g];
         }
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            d[g] *= inv_t;
+        for (int g = 0; g < G; ++g)
             if (keeps && c + g * STEP < ld) *reinterpret_cast<F4 *>(x + c + g * STEP) = d[g];
-        }
     };
-    // a logit after the pass
-    const auto logit = [&](int c) ECHO_INLINE {
+    // a logit's product after the pass
+    const auto product = [&](int c) ECHO_INLINE {
         float d = x[c];
         if (keeps) return d;
 #pragma unroll 8
         for (int p = 1; p < splits; ++p) d += x[p * part + c];
-        return d * inv_t;
+        return d;
     };
+    // relative to products, as in the tiles
+    const auto exp_from = [&](float d, float base) ECHO_INLINE { return __builtin_amdgcn_exp2f((d - base) * k2); };
     float top = -kInf, sum = 0.0f;
     const auto pass = [&](auto groups) ECHO_INLINE {
         constexpr int G = decltype(groups)::value;
@@ -368,11 +368,11 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
                     m = fmaxf(m, d[g][e]);
                 }
             const float base = m == -kInf ? 0.0f : m;
-            sum *= top == -kInf ? 1.0f : exp_of(top - base);      // before a first finite logit the sum is 0, or NaN
+            sum *= top == -kInf ? 1.0f : exp_from(top, base);      // before a first finite logit the sum is 0, or NaN
 #pragma unroll
             for (int g = 0; g < G; ++g)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum += exp_of(d[g][e] - base);
+                for (int e = 0; e < 4; ++e) sum += exp_from(d[g][e], base);
             top = m;
         }
     };
@@ -382,12 +382,12 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
         pass(Count<2>{});
     const float mine = top;
     top = wave_max(top);
-    sum = wave_sum(mine == -kInf ? sum : sum * exp_of(mine - top));
+    sum = wave_sum(mine == -kInf ? sum : sum * exp_from(mine, top));
     if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = make_float4(top, sum, t.trained ? 1.0f : 0.0f, 0.0f);
     __threadfence_block();
     __syncthreads();      // also: the row's logits are where its first part was
     const bool trained = lds[0].z > 0.0f;
-    if (a.in.top && threadIdx.x < kWave) take_logits(entries, a.in.top, logit);
+    if (a.in.top && threadIdx.x < kWave) take_logits(entries, a.in.top, product);
     float lse;
     if (a.lse_in) {
         lse = a.lse_in[n];
@@ -398,15 +398,15 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
             const float4 p = lds[w];
-            sum += p.x == -kInf ? p.y : p.y * exp_of(p.x - top);
+            sum += p.x == -kInf ? p.y : p.y * exp_from(p.x, top);
         }
         if (sum != sum) top = sum;      // a row of NaN alone has no maximum but a sum
         const float more = logf(sum);
-        lse = top == -kInf ? -kInf : top + more;
+        lse = top == -kInf ? -kInf : top * inv_t + more;
         if (threadIdx.x < kWave) {
             // the loss takes logits from their maximum on, the target as they are
             const auto sum_from = [&](float from) ECHO_INLINE {
-                return a.in.top ? cross_of(entries, a.in.top, from) : at >= 0 ? logit(at) - from : 0.0f;
+                return (a.in.top ? cross_of(entries, a.in.top, from) : at >= 0 ? product(at) - from : 0.0f) * inv_t;
             };
             const float cross = a.loss ? sum_from(lse != -kInf ? top : 0.0f) : 0.0f, target = a.target ? sum_from(0.0f) : 0.0f;
             if (threadIdx.x == 0) {
@@ -427,7 +427,7 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
             const F4 f = *reinterpret_cast<const F4 *>(x + c);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float p = exp_of(f[e] - lse) - (c + e == at ? 1.0f : 0.0f);
+                const float p = exp_of(f[e] * inv_t - lse) - (c + e == at ? 1.0f : 0.0f);
                 d[e] = c + e < a.vocab ? p * g : 0.0f;
             }
         }
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
     if (threadIdx.x >= kWave) return;
     for (int k = threadIdx.x; k < a.in.top; k += kWave) {
         const Entry e = entries[k];
-        if (e.at >= 0) put(e.at, F<1>((exp_of(e.x - lse) - e.mass) * g));
+        if (e.at >= 0) put(e.at, F<1>((exp_of(e.x * inv_t - lse) - e.mass) * g));
     }
 }
 
@@ -490,9 +490,9 @@ __global__ __launch_bounds__(256) void k_shares(ShareArgs a) {
                 const int part = c < a.split ? c / a.part0 : a.split / a.part0 + (c - a.split) / a.part1;
                 const float top = a.stats[(int64_t)part * a.rows + n].x;
                 d = widen<K, 8>(*reinterpret_cast<const V<K, 8> *>(static_cast<const K *>(a.kept) + (int64_t)n * a.cols + c)) *
-                    (__builtin_amdgcn_exp2f(top - lse * kLog2e) * g / kKeptUnit<T, PLANES>);
+                    (exp_of(top * a.inv_t - lse) * g / kKeptUnit<T, PLANES>);
                 if ((unsigned)(hit - c) < 8u) {
-                    const float p = (exp_of(a.hits[n] - lse) - 1.0f) * g;
+                    const float p = (exp_of(a.hits[n] * a.inv_t - lse) - 1.0f) * g;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) d[j] = c + j == hit ? p : d[j];
                 }
@@ -506,7 +506,7 @@ __global__ __launch_bounds__(256) void k_shares(ShareArgs a) {
         for (int k = threadIdx.x; k < a.top; k += 256) {
             const int64_t e = (int64_t)n * a.top + k;
             const int c = a.local[e];
-            if ((unsigned)(c - from) < (unsigned)kSpan && c >= 0) put(c, F<1>((exp_of(a.hits[e] - lse) - a.q[e]) * g));
+            if ((unsigned)(c - from) < (unsigned)kSpan && c >= 0) put(c, F<1>((exp_of(a.hits[e] * a.inv_t - lse) - a.q[e]) * g));
         }
     }
 }
@@ -516,8 +516,9 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
     __shared__ float2 part[64][17];
     const int r = threadIdx.x % 16, w = threadIdx.x / 16;
     const int n = blockIdx.x * 16 + r;
-    // statistics are in powers of two
-    const auto moved = [](float2 p, float to) ECHO_INLINE { return p.x == -kInf ? p.y : p.y * __builtin_amdgcn_exp2f(p.x - to); };      // p.y is 0 there, or NaN
+    // maxima and hits are of the products
+    const float inv_t = a.inv_t, k2 = inv_t * kLog2e;
+    const auto moved = [&](float2 p, float to) ECHO_INLINE { return p.x == -kInf ? p.y : p.y * __builtin_amdgcn_exp2f((p.x - to) * k2); };      // p.y is 0 there, or NaN
     float top = -kInf, sum = 0.0f;
     if (n < a.rows) {
 #pragma unroll 4
@@ -538,7 +539,7 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
         }
     }
     __syncthreads();
-    top = part[0][r].x * kLn2;
+    top = part[0][r].x;
     sum = part[0][r].y;
     float cross = 0.0f, target = 0.0f;
     if (a.top) {
@@ -549,8 +550,8 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
                 const int64_t e = (int64_t)n * a.top + k;
                 if (a.local[e] < 0) continue;
                 const float q = a.q[e], x = a.hits[e];
-                cross += q * (x - from);
-                target += q * x;
+                cross += q * ((x - from) * inv_t);
+                target += q * (x * inv_t);
             }
         }
         for (int by = 32; by; by /= 2) {
@@ -566,14 +567,14 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
     }
     if (w || n >= a.rows) return;
     if (sum != sum) top = sum;      // a row of NaN alone has no maximum but a sum
-    const float more = logf(sum), lse = top == -kInf ? -kInf : top + more;
+    const float more = logf(sum), lse = top == -kInf ? -kInf : top * inv_t + more;
     if (a.lse) a.lse[n] = lse;
     if (!a.top) {
         const int64_t t = a.wide_index ? id_at<int64_t>(a.targets, n) : id_at<int32_t>(a.targets, n);
         const bool trained = t >= 0 && t < a.vocab_size;
         const float hit = trained && shard_row(t, a.vocab_start, a.vocab) >= 0 ? a.hits[n] : 0.0f;
-        if (a.target) a.target[n] = hit;
-        if (a.loss) a.loss[n] = !trained ? 0.0f : lse == -kInf ? kInf : (top - hit) + more;
+        if (a.target) a.target[n] = hit * inv_t;
+        if (a.loss) a.loss[n] = !trained ? 0.0f : lse == -kInf ? kInf : (top - hit) * inv_t + more;
         return;
     }
     const float2 prior = a.prior[n];
@@ -985,7 +986,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         h.scale_out = p.keep ? reinterpret_cast<float *>(w + p.scale) : nullptr;
         ECHO_HIP(run_logits(h, a.type, p.keep ? kKeep : kLoss, p.keep ? (int)p.prob_cols : a.vocab, p.logits, s));
         ECHO_HIP(launch_join(JoinArgs{h.stats, h.prior, h.hits, h.q, h.local, h.targets, h.wide_index, h.top, h.rows, h.vocab,
-                                      p.stats_parts, h.vocab_start, h.vocab_size, a.temperature * a.temperature, a.lse, a.target,
+                                      p.stats_parts, h.vocab_start, h.vocab_size, h.inv_t, a.temperature * a.temperature, a.lse, a.target,
                                       a.entropy, a.loss}, s));
     }
     if (!a.grads) return hipSuccess;
@@ -1006,7 +1007,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         h.m.ni = n;
         if (p.keep) {
             const ShareArgs c{h.stats, h.prior, h.hits, h.q, h.lse, h.grad_loss, h.scale, h.local, h.targets, w + p.kept, h.wide_index,
-                              h.top, h.rows, h.vocab, (int)p.prob_cols, h.vocab_start, h.vocab_size, p.logits.split,
+                              h.top, h.rows, h.vocab, (int)p.prob_cols, h.vocab_start, h.vocab_size, h.inv_t, p.logits.split,
                               part_of(p.logits.shape0), part_of(p.logits.shape1), h.prob, h.prob_stride, h.prob_plane, h.prob_rows};
             ECHO_HIP(launch_shares(c, a.type, s));
         } else if (!p.few) {

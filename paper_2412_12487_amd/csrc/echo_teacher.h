@@ -15,7 +15,7 @@ struct TeacherIn {
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kLog2e = 1.44269504088896341f;
 
 // exp(x), x <= 0 but for a row's rounding: one multiplication and the hardware's 2^x.  The product's rounding
 // makes the result |x| 2^-24 of itself wrong, as does that of x itself.

@@ -122,3 +122,119 @@ def test_the_head_gives_every_statistic_together(rows, cols, vocab, dtype, teach
     _close(_linear_all(h, w, t, z, temp, gl), ref)
     for name in alone:
         assert torch.equal(_linear_all(h, w, t, z, temp, names=(name,))[name], alone[name]), name
+
+
+# ---------------------------------------------------------------- logits far from zero
+
+def _far(rows, cols, vocab, dtype, e, seed):
+    """Hidden states and table whose products are sign 2^e plus small multiples of that number's last place in 32 bits: every product and
+    every sum is exact in them.  Their first column alone is large."""
+    g = _gen(seed)
+    a, b = 2.0 ** (e - e // 2), 2.0 ** (e // 2)
+    unit = 2.0 ** (e - 23)
+    h = torch.randint(-1, 2, (rows, cols), generator=g, device="cuda").float()
+    w = torch.randint(-2, 3, (vocab, cols), generator=g, device="cuda").float() * unit
+    h[:, 0], w[:, 0] = a, b
+    h[::2, 0] = -a
+    # numbers below 2^e have a last place of half the size, so that sums of both signs of the rest are exact
+    t = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    t[1::7] = -100
+    h, w = h.to(dtype), w.to(dtype)
+    x = h.double() @ w.double().t()
+    assert torch.equal(x, x.float().double())
+    return h, w, t, x
+
+
+def _exp(d):
+    """exp(d) and its bound, d the exact distance of each logit from what its exponential is relative to: the product of d and
+    log2(e) / T is off by 3 roundings, the exponential by 2."""
+    p = torch.exp(d)
+    return p, p * R.U * (4 * d.abs() + 2)
+
+
+def _softmax(x, dtype):
+    """(largest logit, sum of exponentials relative to it and its bound, probabilities and theirs) of exact logits x in one call; tiles'
+    sums move some exponentials more, and exponentials of bfloat16 may be kept as half precision of 2^15 times their size."""
+    top = x.max(1, keepdim=True).values
+    s, e_s = _exp(x - top)
+    total = s.sum(1, keepdim=True)
+    e_total = e_s.sum(1, keepdim=True) + R.U * (R.chain(x.shape[1]) + 128) * total
+    e = s * 2.0 ** -11 + 2.0 ** -40 if dtype == BF16 else 0.0
+    return top, total[:, 0], e_total[:, 0], s / total, (e_s + e + s * (e_total / total + 16 * R.U)) / total
+
+
+def _check_far(got, h, w, x, q, gl, temp, p, e_p, dtype):
+    """Gradients of the columns that are small, where nothing of the first one's size cancels."""
+    trained = (q.sum(1) > 0)[:, None]
+    g = gl.double()[:, None] * temp
+    d = torch.where(trained, (p - q) * g, 0.0)
+    rel, least = R.SHARE[dtype]
+    e_d = torch.where(trained, g.abs() * (e_p + 4 * R.U * (p + q)), 0.0)
+    e_d = e_d + (d.abs() + e_d) * (rel + 8 * R.U) + least * float(gl.abs().max()) * temp
+    for name, (v, e) in (("dhidden", R.product(d, w.double()[:, 1:], dtype, e_d)),
+                         ("dweight", R.product(d.t(), h.double()[:, 1:], dtype, e_d.t()))):
+        assert torch.isfinite(got[name]).all(), name
+        R.close(got[name][:, 1:].contiguous(), v, e + 4 * R.U * v.abs(), name)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,vocab", [FEW, TILES])
+@pytest.mark.parametrize("e", [10, 20, 24, 27])
+@pytest.mark.parametrize("what", ["loss"])
+def test_logits_far_from_zero(rows, cols, vocab, e, dtype, what):
+    """Logits of 2^e and both signs, whose distances from each other 32 bits hold exactly: a row's loss and probabilities follow from
+    those distances, whatever the logits' own size.  From a given lse, which is a number of 32 bits, probabilities follow from the exact
+    distances from that number."""
+    h, w, t, x = _far(rows, cols, vocab, dtype, e, e)
+    gl = torch.full((rows,), 1 / rows, device="cuda")
+    top, total, e_total, p, e_p = _softmax(x, dtype)
+    trained = t >= 0
+    q = torch.zeros_like(x).scatter_(1, t.clamp(min=0)[:, None], trained.double()[:, None])
+    full = E.linear_cross_entropy(h, w, t, grad_loss=gl)
+    more, e_more = torch.log(total), e_total / total + 4 * R.U * (torch.log(total) + 1)
+    loss = torch.where(trained, more + (top - x.gather(1, t.clamp(min=0)[:, None]))[:, 0], 0.0)
+    R.close(full["loss"], loss, torch.where(trained, e_more + 4 * R.U * loss, 0.0), "loss")
+    R.close(full["lse"], top[:, 0] + more, e_more, "lse")
+    if what == "one call":
+        _check_far(full, h, w, x, q, gl, 1.0, p, e_p, dtype)
+    elif what == "given lse":
+        p, e_p = _exp(x - full["lse"].double()[:, None])
+        alone = E.linear_cross_entropy_grad(h, w, t, full["lse"], gl)
+        _check_far(alone, h, w, x, q, gl, 1.0, p, e_p + 16 * R.U * p, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,vocab", [FEW, TILES])
+@pytest.mark.parametrize("power", [-7, -19])
+@pytest.mark.parametrize("what", ["loss"])
+def test_small_temperatures(rows, cols, vocab, power, dtype, what):
+    """Logits of about 16 over a temperature of 2^-7 or 2^-19, nearly the smallest that is taken: 2^11 and 2^23.  As in _far, products
+    and sums are exact; the elements are normal numbers of every type."""
+    g = _gen(power)
+    temp = 2.0 ** power
+    h = torch.randint(-1, 2, (rows, cols), generator=g, device="cuda").float() * 2.0 ** -6
+    w = torch.randint(-2, 3, (vocab, cols), generator=g, device="cuda").float() * 2.0 ** (power + 7)
+    h[:, 0], w[:, 0] = 4, 4
+    h, w = h.to(dtype), w.to(dtype)
+    x = h.double() @ w.double().t()
+    assert torch.equal(x, x.float().double())
+    x = x / temp
+    ids = torch.randint(0, vocab // 4, (rows, 4), generator=g, device="cuda") * 4 + torch.arange(4, device="cuda")      # no id twice
+    z = torch.randint(-2, 3, (rows, 4), generator=g, device="cuda").float() * temp
+    gl = torch.full((rows,), 1 / rows, device="cuda")
+    mass, e_mass, prior, e_prior, trained = R.teacher(ids, z, vocab, temp)
+    assert trained.all()
+    top, total, e_total, p, e_p = _softmax(x, dtype)
+    q, e_q = torch.zeros_like(x).scatter_(1, ids, mass), torch.zeros_like(x).scatter_(1, ids, e_mass)
+    full = E.linear_distillation(h, w, ids, z, temperature=temp, grad_loss=gl)
+    far = top - x.gather(1, ids)
+    more, cross = torch.log(total), (mass * far).sum(1)
+    loss = temp * temp * (prior + more + cross)
+    bound = temp * temp * (e_prior + e_total / total + (e_mass * far).sum(1) + 16 * R.U * (prior.abs() + cross + more + 1))
+    R.close(full["loss"], loss, bound, "loss")
+    if what == "one call":
+        _check_far(full, h, w, x, q, gl, temp, p, e_p + e_q, dtype)
+    elif what == "given lse":
+        p, e_p = _exp(x - full["lse"].double()[:, None])
+        alone = E.linear_distillation_grad(h, w, ids, z, full["lse"], gl, temperature=temp)
+        _check_far(alone, h, w, x, q, gl, temp, p, e_p + 16 * R.U * p + e_q, dtype)
