@@ -28,8 +28,8 @@ struct HeadArgs {
     int64_t kept_stride;
 };
 struct ShareArgs {
-    const float2 *stats, *prior;
-    const float *hits, *q, *lse, *grad_loss, *scale;
+    const float2 *stats, *whole, *prior;      // whole [rows]: largest product and sum of exponentials relative to it
+    const float *hits, *q, *grad_loss, *scale;
     const int *local;
     const void *targets, *kept;
     int wide_index, top, rows, vocab, cols;
@@ -49,6 +49,7 @@ struct JoinArgs {
     int64_t vocab_start, vocab_size;
     float inv_t, square;          // 1 / T, T^2
     float *lse, *target, *entropy, *loss;
+    float2 *whole;                // or null
 };
 struct TeacherArgs {
     TeacherIn in;

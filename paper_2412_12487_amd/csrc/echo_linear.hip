@@ -418,8 +418,12 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
         }
     }
     if (!a.prob) return;
-    const bool live = trained && lse != -kInf;
+    // Probabilities of a loss's own call are 2^((D - top) k) / sum, of a given lse exp(x - lse): the lse of 32 bits would make them off by
+    // its own rounding, 0.03 at logits of 2^20.
+    const bool given = a.lse_in, live = trained && (given ? lse != -kInf : sum != 0.0f);
     const float g = live ? a.grad_loss[n] / *a.scale * kUnit<T> : 0.0f;
+    const float times = given ? inv_t : 1.0f, base = given ? lse : top, k = given ? kLog2e : k2, part_of_sum = given ? 1.0f : 1.0f / sum;
+    const auto share = [&](float d) ECHO_INLINE { return __builtin_amdgcn_exp2f(__builtin_fmaf(d, times, -base) * k) * part_of_sum; };
 #pragma unroll 4
     for (int c = threadIdx.x * 4; c < a.cols; c += STEP) {
         F<4> d = 0.0f;
@@ -427,7 +431,7 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
             const F4 f = *reinterpret_cast<const F4 *>(x + c);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float p = exp_of(f[e] * inv_t - lse) - (c + e == at ? 1.0f : 0.0f);
+                const float p = share(f[e]) - (c + e == at ? 1.0f : 0.0f);
                 d[e] = c + e < a.vocab ? p * g : 0.0f;
             }
         }
@@ -439,7 +443,7 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
     if (threadIdx.x >= kWave) return;
     for (int k = threadIdx.x; k < a.in.top; k += kWave) {
         const Entry e = entries[k];
-        if (e.at >= 0) put(e.at, F<1>((exp_of(e.x * inv_t - lse) - e.mass) * g));
+        if (e.at >= 0) put(e.at, F<1>((share(e.x) - e.mass) * g));
     }
 }
 
@@ -452,14 +456,15 @@ template <class T, int PLANES>
 __global__ __launch_bounds__(256) void k_shares(ShareArgs a) {
     using K = Kept<T, PLANES>;
     const int spans = (a.cols + kSpan - 1) / kSpan;
-    const float most = *a.scale;
+    const float most = *a.scale, k2 = a.inv_t * kLog2e;
     for (int64_t id = blockIdx.x; id < (int64_t)a.prob_rows * spans; id += gridDim.x) {
         const int n = (int)(id / spans), from = (int)(id - (int64_t)n * spans) * kSpan;
         bool live = n < a.rows;
-        float lse = 0.0f, g = 0.0f;
+        float2 row = make_float2(0.0f, 1.0f);      // largest product and sum of exponentials
+        float g = 0.0f;
         int hit = -1;
         if (live) {
-            lse = a.lse[n];
+            row = a.whole[n];
             g = a.grad_loss[n] / most * kUnit<T>;
             bool trained;
             if (a.top) {
@@ -469,8 +474,9 @@ __global__ __launch_bounds__(256) void k_shares(ShareArgs a) {
                 trained = t >= 0 && t < a.vocab_size;
                 hit = trained ? shard_row(t, a.vocab_start, a.vocab) : -1;
             }
-            live = trained && lse != -kInf;
+            live = trained && row.y != 0.0f;      // a row of NaN has a sum of NaN
         }
+        const auto share = [&](float product) ECHO_INLINE { return __builtin_amdgcn_exp2f((product - row.x) * k2) / row.y; };
         const auto put = [&](int c, auto d) ECHO_INLINE {
             constexpr int N = sizeof(d) / 4;
             char *out = a.prob + n * a.prob_stride + c * 2;
@@ -490,9 +496,9 @@ __global__ __launch_bounds__(256) void k_shares(ShareArgs a) {
                 const int part = c < a.split ? c / a.part0 : a.split / a.part0 + (c - a.split) / a.part1;
                 const float top = a.stats[(int64_t)part * a.rows + n].x;
                 d = widen<K, 8>(*reinterpret_cast<const V<K, 8> *>(static_cast<const K *>(a.kept) + (int64_t)n * a.cols + c)) *
-                    (exp_of(top * a.inv_t - lse) * g / kKeptUnit<T, PLANES>);
+                    (share(top) * g / kKeptUnit<T, PLANES>);
                 if ((unsigned)(hit - c) < 8u) {
-                    const float p = (exp_of(a.hits[n] * a.inv_t - lse) - 1.0f) * g;
+                    const float p = (share(a.hits[n]) - 1.0f) * g;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) d[j] = c + j == hit ? p : d[j];
                 }
@@ -506,7 +512,7 @@ __global__ __launch_bounds__(256) void k_shares(ShareArgs a) {
         for (int k = threadIdx.x; k < a.top; k += 256) {
             const int64_t e = (int64_t)n * a.top + k;
             const int c = a.local[e];
-            if ((unsigned)(c - from) < (unsigned)kSpan && c >= 0) put(c, F<1>((exp_of(a.hits[e] * a.inv_t - lse) - a.q[e]) * g));
+            if ((unsigned)(c - from) < (unsigned)kSpan && c >= 0) put(c, F<1>((share(a.hits[e]) - a.q[e]) * g));
         }
     }
 }
@@ -569,6 +575,7 @@ __global__ __launch_bounds__(1024) void k_join(JoinArgs a) {
     if (sum != sum) top = sum;      // a row of NaN alone has no maximum but a sum
     const float more = logf(sum), lse = top == -kInf ? -kInf : top * inv_t + more;
     if (a.lse) a.lse[n] = lse;
+    if (a.whole) a.whole[n] = make_float2(top, sum);
     if (!a.top) {
         const int64_t t = a.wide_index ? id_at<int64_t>(a.targets, n) : id_at<int32_t>(a.targets, n);
         const bool trained = t >= 0 && t < a.vocab_size;
@@ -758,7 +765,7 @@ struct Plan {
     Ranges out;                    // the hidden states' gradient
     int splits;
     bool parts;
-    int64_t hidden, weight, stats, hits, local, q, prior, scale, prob, kept, part, sums, tail, bytes;
+    int64_t hidden, weight, stats, whole, hits, local, q, prior, scale, prob, kept, part, sums, tail, bytes;
 };
 bool direct(const void *p, int64_t stride, int type, int cols) {
     return type != ECHO_F32 && cols % kDepth == 0 && stride % 8 == 0 && stride <= int64_t(1) << 22 && (uintptr_t)p % 16 == 0;
@@ -822,6 +829,7 @@ Plan plan_of(const LinearArgs &a) {
         p.prob_cols = p.pieces == 1 ? whole : up((whole + p.pieces - 1) / p.pieces, 256);
         p.prob = take(p.prob_rows * p.prob_cols * 2 * p.share_planes);
         p.keep = a.forward && p.pieces == 1 && !p.few;
+        if (p.keep) p.whole = take(a.rows * 8);
         if (p.keep) p.kept = a.type == ECHO_BF16 ? p.prob : take(a.rows * p.prob_cols * 4);
         const int64_t middle = (int64_t)tiles(a.cols, 128) * tiles(a.rows, 128), steps = p.prob_cols / kDepth * p.share_pairs;
         p.out = ranges_of(a.rows, a.cols);
@@ -987,7 +995,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         ECHO_HIP(run_logits(h, a.type, p.keep ? kKeep : kLoss, p.keep ? (int)p.prob_cols : a.vocab, p.logits, s));
         ECHO_HIP(launch_join(JoinArgs{h.stats, h.prior, h.hits, h.q, h.local, h.targets, h.wide_index, h.top, h.rows, h.vocab,
                                       p.stats_parts, h.vocab_start, h.vocab_size, h.inv_t, a.temperature * a.temperature, a.lse, a.target,
-                                      a.entropy, a.loss}, s));
+                                      a.entropy, a.loss, p.keep ? reinterpret_cast<float2 *>(w + p.whole) : nullptr}, s));
     }
     if (!a.grads) return hipSuccess;
     h.lse = a.forward ? a.lse : a.lse_in;
@@ -1006,7 +1014,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         h.m.a = table;
         h.m.ni = n;
         if (p.keep) {
-            const ShareArgs c{h.stats, h.prior, h.hits, h.q, h.lse, h.grad_loss, h.scale, h.local, h.targets, w + p.kept, h.wide_index,
+            const ShareArgs c{h.stats, reinterpret_cast<float2 *>(w + p.whole), h.prior, h.hits, h.q, h.grad_loss, h.scale, h.local, h.targets, w + p.kept, h.wide_index,
                               h.top, h.rows, h.vocab, (int)p.prob_cols, h.vocab_start, h.vocab_size, h.inv_t, p.logits.split,
                               part_of(p.logits.shape0), part_of(p.logits.shape1), h.prob, h.prob_stride, h.prob_plane, h.prob_rows};
             ECHO_HIP(launch_shares(c, a.type, s));
