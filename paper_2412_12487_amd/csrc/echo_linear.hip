@@ -199,7 +199,6 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
                 lse = lse_of[b];
                 live = r.trained && lse != -kInf;
                 g = grad_of[b] / scale * kUnit<T>;
-                lse *= kLog2e;
             }
             if (PLANES > 1 && n >= a.prob_rows) continue;
             char *row = a.prob + n * a.prob_stride;
@@ -210,7 +209,7 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
                 F4 d = 0.0f;
                 if (live) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) d[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[k][b][e], k2, -lse));
+                    for (int e = 0; e < 4; ++e) d[e] = exp_of(__builtin_fmaf(acc[k][b][e], a.inv_t, -lse));      // the distance is rounded once
                     if (!a.top) {
                         if ((unsigned)(hit - v) < 4u) {
 #pragma unroll

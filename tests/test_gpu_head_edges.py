@@ -180,7 +180,7 @@ def _check_far(got, h, w, x, q, gl, temp, p, e_p, dtype):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols,vocab", [FEW, TILES])
 @pytest.mark.parametrize("e", [10, 20, 24, 27])
-@pytest.mark.parametrize("what", ["loss", "one call"])
+@pytest.mark.parametrize("what", ["loss", "one call", "given lse"])
 def test_logits_far_from_zero(rows, cols, vocab, e, dtype, what):
     """Logits of 2^e and both signs, whose distances from each other 32 bits hold exactly: a row's loss and probabilities follow from
     those distances, whatever the logits' own size.  From a given lse, which is a number of 32 bits, probabilities follow from the exact
@@ -206,7 +206,7 @@ def test_logits_far_from_zero(rows, cols, vocab, e, dtype, what):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols,vocab", [FEW, TILES])
 @pytest.mark.parametrize("power", [-7, -19])
-@pytest.mark.parametrize("what", ["loss", "one call"])
+@pytest.mark.parametrize("what", ["loss", "one call", "given lse"])
 def test_small_temperatures(rows, cols, vocab, power, dtype, what):
     """Logits of about 16 over a temperature of 2^-7 or 2^-19, nearly the smallest that is taken: 2^11 and 2^23.  As in _far, products
     and sums are exact; the elements are normal numbers of every type."""
