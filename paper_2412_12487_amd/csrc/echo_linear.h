@@ -19,6 +19,7 @@ struct HeadArgs {
     const float2 *prior;          // [rows]: sum of q log q, and 1 where the row is trained on
     float2 *stats;                // [parts][rows]: largest product, and sum of exponentials relative to it, of a wavefront's columns
     float *hits;                  // products of the target or of the entries
+    const float2 *whole;          // [rows]: largest product and sum of exponentials relative to it, or null: lse is given
     const float *lse, *grad_loss, *scale;
     float *scale_out;             // one workgroup more writes it, or null
     char *prob;                   // [planes][prob_rows][.]: the gradient's shares

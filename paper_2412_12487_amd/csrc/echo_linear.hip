@@ -93,13 +93,14 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
     multiply<T, true, true, S>(a.m, at, t0, t1, acc);
     // What a lane's rows need, all loads together; of rows past the end, the last one's.
     int64_t target[S::BJ];
-    float lse_of[S::BJ], grad_of[S::BJ], mass_of[S::BJ];
+    float2 whole_of[S::BJ];
+    float grad_of[S::BJ], mass_of[S::BJ];
 #pragma unroll
     for (int b = 0; b < S::BJ; ++b) {
         const int n = j0 + jl + b * 16 < a.rows ? j0 + jl + b * 16 : a.rows - 1;
         if (!a.top) target[b] = a.wide_index ? id_at<int64_t>(a.targets, n) : id_at<int32_t>(a.targets, n);
         if constexpr (MODE == kGrad) {
-            lse_of[b] = a.lse[n];
+            whole_of[b] = a.whole ? a.whole[n] : make_float2(a.lse[n], 1.0f);
             grad_of[b] = a.grad_loss[n];
             if (a.top) mass_of[b] = a.prior[n].y;
         }
@@ -186,19 +187,21 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
             outgoing.flush(static_cast<K *>(a.kept) + n * a.kept_stride + v, a.kept_stride, a.rows - n, a.prob_cols - v);
         }
     } else {
-        const float scale = *a.scale;
+        // In a loss's own call probabilities are 2^((D - top) k) / sum, from a given lse exp(D / T - lse).  A distance is rounded once.
+        const float scale = *a.scale, times = a.whole ? 1.0f : a.inv_t, k2_of = a.whole ? k2 : kLog2e;
 #pragma unroll
         for (int b = 0; b < S::BJ; ++b) {
             const int n = j0 + jl + b * 16;
             bool live = n < a.rows;
             int hit = -1;
-            float lse = 0.0f, g = 0.0f;
+            float base = 0.0f, g = 0.0f, each = 0.0f;
             if (live) {
                 const Row r = a.top ? Row{mass_of[b] > 0.0f, -1} : row_of(a, target[b]);
                 hit = r.at - a.first;      // below 0 where it is not here
-                lse = lse_of[b];
-                live = r.trained && lse != -kInf;
+                base = whole_of[b].x;
+                live = r.trained && (a.whole ? whole_of[b].y != 0.0f : base != -kInf);
                 g = grad_of[b] / scale * kUnit<T>;
+                each = g / whole_of[b].y;
             }
             if (PLANES > 1 && n >= a.prob_rows) continue;
             char *row = a.prob + n * a.prob_stride;
@@ -209,21 +212,20 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
                 F4 d = 0.0f;
                 if (live) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) d[e] = exp_of(__builtin_fmaf(acc[k][b][e], a.inv_t, -lse));      // the distance is rounded once
+                    for (int e = 0; e < 4; ++e) d[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[k][b][e], times, -base) * k2_of) * each;
                     if (!a.top) {
                         if ((unsigned)(hit - v) < 4u) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) d[e] -= v + e == hit ? 1.0f : 0.0f;
+                            for (int e = 0; e < 4; ++e) d[e] -= v + e == hit ? g : 0.0f;
                         }
                     } else {
                         const Quad entry = *reinterpret_cast<const Quad *>(cells.cell(jl + b * 16, i));
                         if (__builtin_bit_cast(int64_t, entry)) {
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                if (entry[e]) d[e] -= a.q[(int64_t)n * a.top + entry[e] - 1];
+                                if (entry[e]) d[e] -= a.q[(int64_t)n * a.top + entry[e] - 1] * g;
                         }
                     }
-                    d *= g;
                     if (i0 + S::TI > a.m.ni) {      // past the vocabulary's end, where a logit of NaN would be one
 #pragma unroll
                         for (int e = 0; e < 4; ++e) d[e] = v + e < a.m.ni ? d[e] : 0.0f;
@@ -828,7 +830,7 @@ Plan plan_of(const LinearArgs &a) {
         p.prob_cols = p.pieces == 1 ? whole : up((whole + p.pieces - 1) / p.pieces, 256);
         p.prob = take(p.prob_rows * p.prob_cols * 2 * p.share_planes);
         p.keep = a.forward && p.pieces == 1 && !p.few;
-        if (p.keep) p.whole = take(a.rows * 8);
+        if (a.forward && !p.few) p.whole = take(a.rows * 8);
         if (p.keep) p.kept = a.type == ECHO_BF16 ? p.prob : take(a.rows * p.prob_cols * 4);
         const int64_t middle = (int64_t)tiles(a.cols, 128) * tiles(a.rows, 128), steps = p.prob_cols / kDepth * p.share_pairs;
         p.out = ranges_of(a.rows, a.cols);
@@ -994,10 +996,11 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         ECHO_HIP(run_logits(h, a.type, p.keep ? kKeep : kLoss, p.keep ? (int)p.prob_cols : a.vocab, p.logits, s));
         ECHO_HIP(launch_join(JoinArgs{h.stats, h.prior, h.hits, h.q, h.local, h.targets, h.wide_index, h.top, h.rows, h.vocab,
                                       p.stats_parts, h.vocab_start, h.vocab_size, h.inv_t, a.temperature * a.temperature, a.lse, a.target,
-                                      a.entropy, a.loss, p.keep ? reinterpret_cast<float2 *>(w + p.whole) : nullptr}, s));
+                                      a.entropy, a.loss, a.grads ? reinterpret_cast<float2 *>(w + p.whole) : nullptr}, s));
     }
     if (!a.grads) return hipSuccess;
-    h.lse = a.forward ? a.lse : a.lse_in;
+    h.whole = a.forward && !p.few ? reinterpret_cast<float2 *>(w + p.whole) : nullptr;
+    h.lse = a.lse_in;
     h.scale_out = nullptr;
     if (!p.keep && !p.few) ECHO_HIP(launch_scale(a.grad_loss, h.rows, reinterpret_cast<float *>(w + p.scale), s));
     const Operand prob{h.prob, h.prob_stride, h.prob_plane, p.prob_rows, (int)p.prob_cols};
@@ -1013,7 +1016,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         h.m.a = table;
         h.m.ni = n;
         if (p.keep) {
-            const ShareArgs c{h.stats, reinterpret_cast<float2 *>(w + p.whole), h.prior, h.hits, h.q, h.grad_loss, h.scale, h.local, h.targets, w + p.kept, h.wide_index,
+            const ShareArgs c{h.stats, h.whole, h.prior, h.hits, h.q, h.grad_loss, h.scale, h.local, h.targets, w + p.kept, h.wide_index,
                               h.top, h.rows, h.vocab, (int)p.prob_cols, h.vocab_start, h.vocab_size, h.inv_t, p.logits.split,
                               part_of(p.logits.shape0), part_of(p.logits.shape1), h.prob, h.prob_stride, h.prob_plane, h.prob_rows};
             ECHO_HIP(launch_shares(c, a.type, s));

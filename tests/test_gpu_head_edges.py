@@ -203,6 +203,17 @@ def test_logits_far_from_zero(rows, cols, vocab, e, dtype, what):
         _check_far(alone, h, w, x, q, gl, 1.0, p, e_p + 16 * R.U * p, dtype)
 
 
+@pytest.mark.parametrize("e", [20, 24])
+def test_logits_far_from_zero_in_pieces(e):
+    """More than 1 GiB of the logits' gradient, whose pieces' logits are made anew in the same call."""
+    rows, cols, vocab = 8192, 64, 25000
+    h, w, t, x = _far(rows, cols, vocab, F32, e, e)
+    gl = torch.full((rows,), 1 / rows, device="cuda")
+    p, e_p = _softmax(x, F32)[3:]
+    q = torch.zeros_like(x).scatter_(1, t.clamp(min=0)[:, None], (t >= 0).double()[:, None])
+    _check_far(E.linear_cross_entropy(h, w, t, grad_loss=gl), h, w, x, q, gl, 1.0, p, e_p, F32)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols,vocab", [FEW, TILES])
 @pytest.mark.parametrize("power", [-7, -19])
