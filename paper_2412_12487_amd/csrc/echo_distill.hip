@@ -10,28 +10,39 @@ namespace {
 __device__ __forceinline__ TeacherIn teacher_in(const DistillArgs &a) {
     return TeacherIn{a.ids, a.teacher, a.index_type, a.teacher_type, a.top, a.vocab_start, a.vocab_size, 1.0f / a.temperature};
 }
-// The entries with the logits of their columns / T.
+// The entries with the logits of their columns.
 template <class T>
 __device__ __forceinline__ Teacher entries_of(const DistillArgs &a, int64_t row, int first, int cols, Entry *entries) {
     const TeacherIn in = teacher_in(a);
     const Teacher t = teacher_of(in, row, first, cols, a.cols, entries);
     const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
-    take_logits(entries, a.top, [&](int at) ECHO_INLINE { return (float)l[at] * in.inv_t; });
+    take_logits(entries, a.top, [&](int at) ECHO_INLINE { return (float)l[at]; });
     return t;
 }
+// Exponentials of logits / T relative to that of a logit `base`.  Logits' distances are taken before they are divided by T: at logits / T of
+// 10^10, whose last place is 1024, the maximum's own exponential is 1 and the others follow from their distances alone.
+struct Relative {
+    float base, k;      // k: log2(e) / T
+    __device__ __forceinline__ float operator()(float l) const { return __builtin_amdgcn_exp2f((l - base) * k); }
+};
+// Probabilities from a given lse.
+struct Given {
+    float lse, inv_t;
+    __device__ __forceinline__ float operator()(float l) const { return exp_of(l * inv_t - lse); }
+};
 // The gradient where the teacher has a mass, over what its row has there.
-template <class T>
-__device__ __forceinline__ void put_entries(T *grad, const Entry *entries, int top, float base, float scale, float g) {
+template <class T, class X>
+__device__ __forceinline__ void put_entries(T *grad, const Entry *entries, int top, X exp_at, float scale, float g) {
     for (int k = threadIdx.x % kWave; k < top; k += kWave) {
         const Entry e = entries[k];
-        if (e.at >= 0) grad[e.at] = (T)(exp_of(e.x - base) * scale - e.mass * g);
+        if (e.at >= 0) grad[e.at] = (T)(exp_at(e.x) * scale - e.mass * g);
     }
 }
 __device__ __forceinline__ float finish_row(const DistillArgs &a, int64_t row, const Teacher &t, const Entry *entries, float top, float sum) {
-    const float more = logf(sum), lse = top == -kInf ? -kInf : top + more;
+    const float inv_t = 1.0f / a.temperature, more = logf(sum), lse = top == -kInf ? -kInf : top * inv_t + more;
     // the loss takes logits from their maximum on, the target as they are
-    const float cross = a.loss ? cross_of(entries, a.top, lse != -kInf ? top : 0.0f) : 0.0f;
-    const float target = a.target ? cross_of(entries, a.top, 0.0f) : 0.0f;
+    const float cross = a.loss ? cross_of(entries, a.top, top != -kInf ? top : 0.0f) * inv_t : 0.0f;
+    const float target = a.target ? cross_of(entries, a.top, 0.0f) * inv_t : 0.0f;
     if (threadIdx.x % kWave == 0) {
         if (a.lse) a.lse[row] = lse;
         if (a.target) a.target[row] = target;
@@ -62,7 +73,7 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK), (kDistillWaves<T
     extern __shared__ __attribute__((aligned(16))) char space[];
     Entry *entries = reinterpret_cast<Entry *>(space) + q.team * a.top;
     __shared__ float4 lds[2][Q::WAVES];
-    const float inv_t = 1.0f / a.temperature;
+    const float k2 = 1.0f / a.temperature * kLog2e;
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * Q::TEAMS + q.team; row < a.rows; row += (int64_t)gridDim.x * Q::TEAMS) {
         const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
@@ -75,17 +86,17 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK), (kDistillWaves<T
         for (int k = 0; k < P; ++k) {
             const F<N> f = widen<T, N>(x[k]);
 #pragma unroll
-            for (int j = 0; j < N; ++j) top = fmaxf(top, f[j] * inv_t);
+            for (int j = 0; j < N; ++j) top = fmaxf(top, f[j]);
             if constexpr (kDistillWaves<T, THREADS, E> > 1) asm volatile("" : "+v"(top));
         }
         forget<T, N, P>(x);
         top = wave_max(top);
-        const float base = top == -kInf ? 0.0f : top;
+        const Relative from{top == -kInf ? 0.0f : top, k2};
 #pragma unroll
         for (int k = 0; k < P; ++k) {
             const F<N> f = widen<T, N>(x[k]);
 #pragma unroll
-            for (int j = 0; j < N; ++j) sum += exp_of(f[j] * inv_t - base);
+            for (int j = 0; j < N; ++j) sum += from(f[j]);
             if constexpr (kDistillWaves<T, THREADS, E> > 1) asm volatile("" : "+v"(sum));
         }
         forget<T, N, P>(x);
@@ -96,15 +107,15 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK), (kDistillWaves<T
             __syncthreads();      // also: the teacher's logits have been read, and grad may be logits
             const float4 p = lds[turn][q.lane % Q::WAVES];
             top = ring_max<Q::WAVES>(p.x);
-            sum = ring_sum<Q::WAVES>(p.x == -kInf ? p.y : p.y * exp_of(p.x - top));
+            sum = ring_sum<Q::WAVES>(p.x == -kInf ? p.y : p.y * Relative{top, k2}(p.x));
             trained = ring_sum<Q::WAVES>(p.z) > 0.0f;      // the first wavefront's
             turn ^= 1;
         }
         if (sum != sum) top = sum;      // a row of NaN alone has no maximum but a sum
-        float lse = top == -kInf ? -kInf : 0.0f;
         if (q.wave == 0) finish_row(a, row, t, entries, top, sum);
         if (!a.grad) continue;
-        const bool live = trained && lse != -kInf;
+        const bool live = trained && top != -kInf;
+        const Relative share{top, k2};
         const float g = a.grad_loss[row] * a.temperature, scale = g / sum;
 #pragma unroll
         for (int k = 0; k < P; ++k) {
@@ -112,7 +123,7 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK), (kDistillWaves<T
             if (live) {
                 f = widen<T, N>(x[k]);
 #pragma unroll
-                for (int j = 0; j < N; ++j) f[j] = exp_of(f[j] * inv_t - top) * scale;
+                for (int j = 0; j < N; ++j) f[j] = share(f[j]) * scale;
             }
             x[k] = round_to<T, N>(f);
             if constexpr (kDistillWaves<T, THREADS, E> > 1) forget<T, N, 1>(reinterpret_cast<V<T, N>(&)[1]>(x[k]));
@@ -120,7 +131,7 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK), (kDistillWaves<T
         T *d = static_cast<T *>(a.grad) + row * a.grad_stride;
         q.drop(d, x);
         settled<Q::WAVES>();
-        if (q.wave == 0 && live) put_entries(d, entries, a.top, top, scale, g);
+        if (q.wave == 0 && live) put_entries(d, entries, a.top, share, scale, g);
     }
 }
 
@@ -131,7 +142,7 @@ __global__ __launch_bounds__(kWideBlock) void k_distill_wide(DistillArgs a) {
     extern __shared__ __attribute__((aligned(16))) char space[];
     Entry *entries = reinterpret_cast<Entry *>(space);
     __shared__ float4 lds[kWideWaves];
-    const float inv_t = 1.0f / a.temperature;
+    const float k2 = 1.0f / a.temperature * kLog2e;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
         Teacher t{};
@@ -142,16 +153,16 @@ __global__ __launch_bounds__(kWideBlock) void k_distill_wide(DistillArgs a) {
             const F<N> f = widen<T, N>(load<N>(l, c, a.cols, T(-kInf)));
             float m = top;
 #pragma unroll
-            for (int j = 0; j < N; ++j) m = fmaxf(m, f[j] * inv_t);
-            const float base = m == -kInf ? 0.0f : m;
-            sum *= top == -kInf ? 1.0f : exp_of(top - base);
+            for (int j = 0; j < N; ++j) m = fmaxf(m, f[j]);
+            const Relative from{m == -kInf ? 0.0f : m, k2};
+            sum *= top == -kInf ? 1.0f : from(top);
 #pragma unroll
-            for (int j = 0; j < N; ++j) sum += exp_of(f[j] * inv_t - base);
+            for (int j = 0; j < N; ++j) sum += from(f[j]);
             top = m;
         }
         const float mine = top;
         top = wave_max(top);
-        sum = wave_sum(mine == -kInf ? sum : sum * exp_of(mine - top));
+        sum = wave_sum(mine == -kInf ? sum : sum * Relative{top, k2}(mine));
         __syncthreads();      // the last row's readers are done
         if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = make_float4(top, sum, t.trained ? 1.0f : 0.0f, 0.0f);
         __syncthreads();
@@ -161,25 +172,26 @@ __global__ __launch_bounds__(kWideBlock) void k_distill_wide(DistillArgs a) {
 #pragma unroll
         for (int v = 0; v < kWideWaves; ++v) {
             const float4 p = lds[v];
-            sum += p.x == -kInf ? p.y : p.y * exp_of(p.x - top);
+            sum += p.x == -kInf ? p.y : p.y * Relative{top, k2}(p.x);
         }
         const bool live = lds[0].z > 0.0f && (top != -kInf || sum != sum);
         if (sum != sum) top = sum;
         if (threadIdx.x < kWave) finish_row(a, row, t, entries, top, sum);
         if (!a.grad) continue;
         T *d = static_cast<T *>(a.grad) + row * a.grad_stride;
+        const Relative share{top, k2};
         const float g = a.grad_loss[row] * a.temperature, scale = g / sum;
         for (int c = threadIdx.x * N; c < a.cols; c += STEP) {
             F<N> f = 0.0f;
             if (live) {
                 f = widen<T, N>(load<N>(l, c, a.cols));
 #pragma unroll
-                for (int j = 0; j < N; ++j) f[j] = exp_of(f[j] * inv_t - top) * scale;
+                for (int j = 0; j < N; ++j) f[j] = share(f[j]) * scale;
             }
             store<N>(d, c, a.cols, round_to<T, N>(f));
         }
         settled<kWideWaves>();
-        if (threadIdx.x < kWave && live) put_entries(d, entries, a.top, top, scale, g);
+        if (threadIdx.x < kWave && live) put_entries(d, entries, a.top, share, scale, g);
     }
 }
 
@@ -213,6 +225,7 @@ __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
         __syncthreads();      // also: the teacher's logits have been read
         const float lse = a.lse_in[row], g = a.grad_loss[row] * a.temperature;
         const bool live = lds && lse != -kInf;
+        const Given share{lse, inv_t};
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int c = from + k * 256 * N;
@@ -221,12 +234,12 @@ __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
             if (live) {
                 f = widen<T, N>(raw[k]);
 #pragma unroll
-                for (int j = 0; j < N; ++j) f[j] = exp_of(f[j] * inv_t - lse) * g;
+                for (int j = 0; j < N; ++j) f[j] = share(f[j]) * g;
             }
             drop<N>(d, c, a.cols, round_to<T, N>(f));
         }
         settled<4>();
-        if (threadIdx.x < kWave && live) put_entries(d, entries, a.top, lse, g, g);
+        if (threadIdx.x < kWave && live) put_entries(d, entries, a.top, share, g, g);
     }
 }
 

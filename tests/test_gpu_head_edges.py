@@ -249,3 +249,46 @@ def test_small_temperatures(rows, cols, vocab, power, dtype, what):
         p, e_p = _exp(x - full["lse"].double()[:, None])
         alone = E.linear_distillation_grad(h, w, ids, z, full["lse"], gl, temperature=temp)
         _check_far(alone, h, w, x, q, gl, temp, p, e_p + 16 * R.U * p + e_q, dtype)
+
+
+def _distinct(g, rows, top, cols):
+    """Ids of which none comes twice in a row."""
+    return torch.rand(rows, cols, generator=g, device="cuda").argsort(1)[:, :top].contiguous()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("temp", [0.3, 1e-3, 1e-6])
+@pytest.mark.parametrize("cols", [5, 500, 5000, 40000, 70000])
+@pytest.mark.parametrize("what", ["one call"])
+def test_distillation_of_logits_far_from_zero(cols, temp, dtype, what):
+    """Logits of 2^15 and both signs that differ by a few of their last places, over temperatures that are no powers of two: 10^5 to
+    3 * 10^10.  From a given lse, which is a number of 32 bits, logits / T are such numbers too."""
+    rows, top = 6, min(4, cols)
+    g = _gen(cols)
+    k = torch.randint(-8, 9, (rows, cols), generator=g, device="cuda").double()
+    l = (2.0 ** 15 + k * 2.0 ** 15 * torch.finfo(dtype).eps).to(dtype)
+    l[::2] *= -1
+    ids = _distinct(g, rows, top, cols)
+    z = torch.randint(-2, 3, (rows, top), generator=g, device="cuda").float()
+    gl = _normal(g, rows)
+    t32 = float(torch.tensor(temp))      # what the library takes
+    mass, e_mass, prior, e_prior, _ = R.teacher(ids, z, cols, t32)
+    full = E.distillation(l, ids, z, temperature=temp, grad_loss=gl)
+    q, e_q = torch.zeros(rows, cols, dtype=torch.float64, device="cuda").scatter_(1, ids, mass), R.U * 4
+    e_q = torch.zeros_like(q).scatter_(1, ids, e_mass + e_q * mass)
+    if what == "one call":
+        top, total, e_total, p, e_p = _softmax(l.double() / t32, F32)
+        d = l.double() / t32 - top
+        e_p = e_p + 2 * R.U * d.abs() * p      # 1 / T is rounded
+        far = -d.gather(1, ids)
+        e_total = e_total + (2 * R.U * d.abs() * torch.exp(d)).sum(1)
+        more, cross = torch.log(total), (mass * far).sum(1)
+        bound = t32 * t32 * (e_prior + e_total / total + (e_mass * far).sum(1) + 16 * R.U * (prior.abs() + cross + more + 1))
+        R.close(full["loss"], t32 * t32 * (prior + more + cross), bound, "loss")
+        grad = full["grad"]
+    else:
+        x = (l.float() * (1 / torch.tensor(temp))).double()      # rounded to 32 bits, as the lse is
+        p, e_p = _exp(x - full["lse"].double()[:, None])
+        grad = E.distillation_grad(l, ids, z, full["lse"], gl, temperature=temp)
+    scale = (gl.double() * t32)[:, None]
+    R.close(grad, (p - q) * scale, scale.abs() * (e_p + e_q + 8 * R.U * (p + q)), "grad")
