@@ -28,7 +28,7 @@ struct Relative {
 // Probabilities from a given lse.
 struct Given {
     float lse, inv_t;
-    __device__ __forceinline__ float operator()(float l) const { return exp_of(l * inv_t - lse); }
+    __device__ __forceinline__ float operator()(float l) const { return exp_of(scaled(l, inv_t) - lse); }
 };
 // The gradient where the teacher has a mass, over what its row has there.
 template <class T, class X>

@@ -187,7 +187,7 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
             outgoing.flush(static_cast<K *>(a.kept) + n * a.kept_stride + v, a.kept_stride, a.rows - n, a.prob_cols - v);
         }
     } else {
-        // In a loss's own call probabilities are 2^((D - top) k) / sum, from a given lse exp(D / T - lse).  A distance is rounded once.
+        // In a loss's own call probabilities are 2^((D - top) k) / sum, from a given lse exp(D / T - lse).
         const float scale = *a.scale, times = a.whole ? 1.0f : a.inv_t, k2_of = a.whole ? k2 : kLog2e;
 #pragma unroll
         for (int b = 0; b < S::BJ; ++b) {
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
                 F4 d = 0.0f;
                 if (live) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) d[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[k][b][e], times, -base) * k2_of) * each;
+                    for (int e = 0; e < 4; ++e) d[e] = __builtin_amdgcn_exp2f((scaled(acc[k][b][e], times) - base) * k2_of) * each;
                     if (!a.top) {
                         if ((unsigned)(hit - v) < 4u) {
 #pragma unroll
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
     const bool given = a.lse_in, live = trained && (given ? lse != -kInf : sum != 0.0f);
     const float g = live ? a.grad_loss[n] / *a.scale * kUnit<T> : 0.0f;
     const float times = given ? inv_t : 1.0f, base = given ? lse : top, k = given ? kLog2e : k2, part_of_sum = given ? 1.0f : 1.0f / sum;
-    const auto share = [&](float d) ECHO_INLINE { return __builtin_amdgcn_exp2f(__builtin_fmaf(d, times, -base) * k) * part_of_sum; };
+    const auto share = [&](float d) ECHO_INLINE { return __builtin_amdgcn_exp2f((scaled(d, times) - base) * k) * part_of_sum; };
 #pragma unroll 4
     for (int c = threadIdx.x * 4; c < a.cols; c += STEP) {
         F<4> d = 0.0f;

@@ -21,6 +21,12 @@ constexpr float kLog2e = 1.44269504088896341f;
 // makes the result |x| 2^-24 of itself wrong, as does that of x itself.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
+// A logit / T as a number of 32 bits, by itself: an lse that is given is such a number, and above each of them.  Fused with the
+// subtraction of the lse, the product would not be rounded, and the largest logit's probability be up to exp of half its last place.
+__device__ __forceinline__ float scaled(float l, float inv_t) {
+#pragma clang fp contract(off)
+    return l * inv_t;
+}
 __device__ __forceinline__ int64_t index_at(const void *ids, int index_type, int64_t at) {
     return index_type == ECHO_I64 ? id_at<int64_t>(ids, at) : id_at<int32_t>(ids, at);
 }

@@ -259,7 +259,7 @@ def _distinct(g, rows, top, cols):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("temp", [0.3, 1e-3, 1e-6])
 @pytest.mark.parametrize("cols", [5, 500, 5000, 40000, 70000])
-@pytest.mark.parametrize("what", ["one call"])
+@pytest.mark.parametrize("what", ["one call", "given lse"])
 def test_distillation_of_logits_far_from_zero(cols, temp, dtype, what):
     """Logits of 2^15 and both signs that differ by a few of their last places, over temperatures that are no powers of two: 10^5 to
     3 * 10^10.  From a given lse, which is a number of 32 bits, logits / T are such numbers too."""
@@ -292,3 +292,20 @@ def test_distillation_of_logits_far_from_zero(cols, temp, dtype, what):
         grad = E.distillation_grad(l, ids, z, full["lse"], gl, temperature=temp)
     scale = (gl.double() * t32)[:, None]
     R.close(grad, (p - q) * scale, scale.abs() * (e_p + e_q + 8 * R.U * (p + q)), "grad")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,vocab", [FEW, TILES])
+def test_a_given_lse_is_above_every_logit(rows, cols, vocab, dtype):
+    """Logits of 5e6 at a temperature that is no power of two: as numbers of 32 bits none is above the lse, and no probability above 1."""
+    temp = 3e-6
+    h, w, _, x = _far(rows, cols, vocab, dtype, 4, 3)
+    ids, z = torch.arange(rows, device="cuda")[:, None] % vocab, torch.zeros(rows, 1, device="cuda")
+    gl = torch.full((rows,), 1 / rows, device="cuda")
+    lse = E.linear_distillation(h, w, ids, z, temperature=temp)["lse"]
+    x = (x.float() * (1 / torch.tensor(temp))).double()
+    p, e_p = _exp(x - lse.double()[:, None])
+    assert float(p.max()) <= 1
+    q = torch.zeros_like(x).scatter_(1, ids, 1.0)
+    got = E.linear_distillation_grad(h, w, ids, z, lse, gl, temperature=temp)
+    _check_far(got, h, w, x, q, gl, float(torch.tensor(temp)), p, e_p + 16 * R.U * p, dtype)
