@@ -162,7 +162,7 @@ int echo_distillation_grad(const void *logits, int64_t logits_stride, int32_t ty
  * gradient of above:
  *   dhidden = d weight, [rows][cols] of `type`;   dweight = d^T hidden, [vocab][cols] of grad_type (`type` or ECHO_F32),
  *   written, or with accumulate != 0 added to.
- * Of 16-bit types d is rounded to `type` (relative to the largest |grad_loss|, of any row) before these products, as the
+ * Of 16-bit types d is rounded to `type` (relative to the largest finite |grad_loss| of the rows trained on) before these products, as the
  * logits' gradient of echo_cross_entropy is (of up to 64 rows it may be held in twice the bits); of 32 bits it is held in 24.  Rows not trained on have d = 0.  A row whose hidden state
  * has a NaN or an infinity gives NaN to every row of dweight, trained on or not.  Logits beyond 2^127 / T count as infinite, and
  * 32-bit elements beyond the largest of bfloat16, infinities among them, as NaN.

@@ -65,6 +65,7 @@ struct PartsArgs {
     float *parts;                 // [splits][rows][ld]
     int64_t part;
     int ld;
+    TeacherIn in;                 // top is 0 with one target a row: its ids are the targets
     const float *grad_loss;
     float *scale_out;             // one workgroup more writes it, or null
 };

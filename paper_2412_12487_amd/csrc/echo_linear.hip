@@ -57,19 +57,27 @@ struct Cells {
     }
 };
 
-// The largest |grad_loss| of the rows, or 1 where that is 0 or not finite: what the gradient's shares are relative to, so that
-// rows of one weight have it exactly.
-template <int THREADS>
-__device__ __forceinline__ void write_scale(const float *grad_loss, int rows, float *scale, float *lds) {
+// The largest finite |grad_loss| of the rows that are trained on, or 1 where there is none above 0: what the gradient's shares are
+// relative to, so that rows of one weight have it exactly.  What stands in other rows, infinities among it, is not their concern.
+template <int THREADS, class Trained>
+__device__ __forceinline__ void write_scale(const float *grad_loss, int rows, float *scale, float *lds, Trained trained) {
     float top = 0.0f;
 #pragma unroll 4
-    for (int n = threadIdx.x; n < rows; n += THREADS) top = fmaxf(top, fabsf(grad_loss[n]));
+    for (int n = threadIdx.x; n < rows; n += THREADS) {
+        const float g = fabsf(grad_loss[n]);
+        if (trained(n) && g < kInf) top = fmaxf(top, g);
+    }
     top = wave_max(top);
     if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = top;
     __syncthreads();
     if (threadIdx.x) return;
     for (int w = 1; w < THREADS / kWave; ++w) top = fmaxf(top, lds[w]);
-    *scale = top > 0.0f && top < kInf ? top : 1.0f;
+    *scale = top > 0.0f ? top : 1.0f;
+}
+// Whether a row is trained on, once the teacher's entries are prepared.
+__device__ __forceinline__ bool is_trained(const HeadArgs &a, int n) {
+    if (a.top) return a.prior[n].y > 0.0f;
+    return row_of(a, a.wide_index ? id_at<int64_t>(a.targets, n) : id_at<int32_t>(a.targets, n)).trained;
 }
 
 // Tiles of logits, i over the vocabulary and j over the rows.  2048 x 8192 over 49152 ids in wide tiles: 1.21 to 1.31 ms, 1260 to 1360
@@ -84,7 +92,8 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
     __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
     if constexpr (MODE == kKeep)
         if ((int)blockIdx.x == a.m.tiles_i * a.m.tiles_j)
-            return write_scale<S::THREADS>(a.grad_loss, a.rows, a.scale_out, reinterpret_cast<float *>(t0));
+            return write_scale<S::THREADS>(a.grad_loss, a.rows, a.scale_out, reinterpret_cast<float *>(t0),
+                                           [&](int n) ECHO_INLINE { return is_trained(a, n); });
     const Place at = place_of(a.m, blockIdx.x);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wi = wave / S::WJ, wj = wave % S::WJ;
@@ -268,7 +277,9 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS < 256 ? 1 : S::THREADS / 256
     __shared__ __attribute__((aligned(16))) char t0[S::BYTES];
     __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
     if ((int)blockIdx.x == a.m.tiles_i * a.m.tiles_j * a.m.splits)
-        return write_scale<S::THREADS>(a.grad_loss, a.m.nj, a.scale_out, reinterpret_cast<float *>(t0));
+        return write_scale<S::THREADS>(a.grad_loss, a.m.nj, a.scale_out, reinterpret_cast<float *>(t0), [&](int n) ECHO_INLINE {
+            return is_trained(a.in, n);
+        });
     const Place at = place_of(a.m, blockIdx.x);
     F4 acc[S::BI][S::BJ];
     multiply<T, true, true, S>(a.m, at, t0, t1, acc);
@@ -608,9 +619,9 @@ __global__ __launch_bounds__(256) void k_teacher(TeacherArgs a) {
 }
 
 // For a gradient whose loss was another call's; else the loss's launch has a workgroup for it.
-__global__ __launch_bounds__(1024) void k_scale(const float *grad_loss, int rows, float *scale) {
+__global__ __launch_bounds__(1024) void k_scale(HeadArgs a) {
     __shared__ float lds[16];
-    write_scale<1024>(grad_loss, rows, scale, lds);
+    write_scale<1024>(a.grad_loss, a.rows, a.scale_out, lds, [&](int n) ECHO_INLINE { return is_trained(a, n); });
 }
 
 // Rows laid out for the products: PLANES planes of 16 bits, rows filled up with zeros to whole steps.  One launch for both
@@ -678,8 +689,8 @@ hipError_t launch_teacher(const TeacherArgs &a, hipStream_t s) {
     return hipLaunchKernel(reinterpret_cast<const void *>(k_teacher), dim3(grid_of((a.rows + 3) / 4)), dim3(256), args,
                            4 * sizeof(Entry) * a.in.top, s);
 }
-hipError_t launch_scale(const float *grad_loss, int rows, float *scale, hipStream_t s) {
-    return launch(k_scale, dim3(1), dim3(1024), s, grad_loss, rows, scale);
+hipError_t launch_scale(const HeadArgs &a, hipStream_t s) {
+    return launch(k_scale, dim3(1), dim3(1024), s, a);
 }
 hipError_t launch_layout(const LayoutArgs &a, const LayoutArgs &b, int type, hipStream_t s) {
     const dim3 grid(grid_of(((a.rows + b.rows) * (a.width / 8) + 255) / 256));
@@ -979,6 +990,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         c.ld = (int)up(a.vocab, kDepth);
         c.parts = reinterpret_cast<float *>(w + p.sums);
         c.part = a.rows * c.ld;
+        c.in = in;
         c.grad_loss = a.grad_loss;
         c.scale_out = a.grads ? reinterpret_cast<float *>(w + p.scale) : nullptr;
         tile(c.m, a.vocab, h.rows, p.few_shape);
@@ -1001,8 +1013,9 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
     if (!a.grads) return hipSuccess;
     h.whole = a.forward && !p.few ? reinterpret_cast<float2 *>(w + p.whole) : nullptr;
     h.lse = a.lse_in;
+    h.scale_out = reinterpret_cast<float *>(w + p.scale);
+    if (!p.keep && !p.few) ECHO_HIP(launch_scale(h, s));
     h.scale_out = nullptr;
-    if (!p.keep && !p.few) ECHO_HIP(launch_scale(a.grad_loss, h.rows, reinterpret_cast<float *>(w + p.scale), s));
     const Operand prob{h.prob, h.prob_stride, h.prob_plane, p.prob_rows, (int)p.prob_cols};
     const int64_t grad_elem = a.grad_type == ECHO_F32 ? 4 : 2;
     float *parts = p.parts ? reinterpret_cast<float *>(w + p.part) : nullptr, *tail = reinterpret_cast<float *>(w + p.tail);

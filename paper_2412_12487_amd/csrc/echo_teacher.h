@@ -34,6 +34,15 @@ __device__ __forceinline__ float value_at(const void *p, int type, int64_t at) {
     if (type == ECHO_F32) return static_cast<const float *>(p)[at];
     return type == ECHO_F16 ? (float)static_cast<const f16 *>(p)[at] : (float)static_cast<const bf16 *>(p)[at];
 }
+// Whether a row is trained on: its target is in the vocabulary, or an id of the vocabulary has a mass.
+__device__ __forceinline__ bool is_trained(const TeacherIn &t, int64_t row) {
+    const int n = t.top ? t.top : 1;
+    for (int k = 0; k < n; ++k) {
+        const int64_t id = index_at(t.ids, t.index_type, row * n + k);
+        if (id >= 0 && id < t.vocab_size && !(t.top && value_at(t.logits, t.type, row * n + k) * t.inv_t == -kInf)) return true;
+    }
+    return false;
+}
 
 // An entry: its column here (or -1), and the mass of its id, which the first entry of an id that has one holds.  `x` is for
 // the logit of that column.  One wavefront prepares a row's entries in shared memory, and each lane reads again only

@@ -575,7 +575,7 @@ def linear_cross_entropy(hidden, weight, targets, *, vocab_start=0, vocab_size=N
     cross_entropy gives them; linear_cross_entropy_grad then gives each rank its gradients.
 
     16-bit types: the logits' gradient is rounded to hidden's type before the gradients' products, relative to the
-    largest |grad_loss|."""
+    largest |grad_loss| of the rows trained on."""
     head = _head(hidden, weight, vocab_start, vocab_size)
     given = _target_args(targets, head[0], head[1], head[2])
     return _linear_loss("echo_linear_cross_entropy", ("loss", "lse") if vocab_size is None else ("lse", "target"), hidden, weight,

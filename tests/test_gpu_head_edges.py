@@ -309,3 +309,44 @@ def test_a_given_lse_is_above_every_logit(rows, cols, vocab, dtype):
     q = torch.zeros_like(x).scatter_(1, ids, 1.0)
     got = E.linear_distillation_grad(h, w, ids, z, lse, gl, temperature=temp)
     _check_far(got, h, w, x, q, gl, float(torch.tensor(temp)), p, e_p + 16 * R.U * p, dtype)
+
+
+# ---------------------------------------------------------------- rows whose weight is not used
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,vocab", [FEW, TILES])
+@pytest.mark.parametrize("teacher", [False, True])
+@pytest.mark.parametrize("weight", [1e30, math.inf, -math.inf, math.nan])
+def test_weights_of_rows_not_trained_on(rows, cols, vocab, dtype, teacher, weight):
+    """Whatever grad_loss holds for a row that is not trained on, the others have their gradients."""
+    h, w, t, gl = _case(rows, cols, vocab, dtype, 5)
+    gl = gl * 1e4
+    if teacher:
+        ids, z = _teacher(rows, 6, vocab, 3)
+        z[4] = -math.inf
+        dead = R.teacher(ids, z, vocab, 1.0)[4].logical_not()
+        call, grad, given = E.linear_distillation, E.linear_distillation_grad, (ids, z)
+    else:
+        dead = t < 0
+        call, grad, given = E.linear_cross_entropy, E.linear_cross_entropy_grad, (t,)
+    assert dead.any() and not dead.all()
+    gl[dead] = 0
+    want = call(h, w, *given, grad_loss=gl)
+    bad = torch.where(dead, torch.full_like(gl, weight), gl)
+    got = call(h, w, *given, grad_loss=bad)
+    assert all(torch.equal(got[k], want[k]) for k in want)
+    want, got = grad(h, w, *given, want["lse"], gl), grad(h, w, *given, want["lse"], bad)
+    assert all(torch.equal(got[k], want[k]) for k in want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,vocab", [FEW, TILES])
+def test_an_infinite_weight_stays_in_its_row(rows, cols, vocab, dtype):
+    h, w, t, gl = _case(rows, cols, vocab, dtype, 5)
+    gl = gl * 1e7      # half precision holds no share of such a weight as it is
+    want = E.linear_cross_entropy(h, w, t, grad_loss=gl)
+    gl[3] = math.inf
+    got = E.linear_cross_entropy(h, w, t, grad_loss=gl)
+    others = torch.arange(rows, device="cuda") != 3
+    assert t[3] >= 0 and torch.equal(got["dhidden"][others], want["dhidden"][others])
+    assert not torch.isfinite(got["dhidden"][3]).all()
