@@ -350,3 +350,45 @@ def test_an_infinite_weight_stays_in_its_row(rows, cols, vocab, dtype):
     others = torch.arange(rows, device="cuda") != 3
     assert t[3] >= 0 and torch.equal(got["dhidden"][others], want["dhidden"][others])
     assert not torch.isfinite(got["dhidden"][3]).all()
+
+
+# ---------------------------------------------------------------- shards
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,vocab", [(1030, 64, 6000), (2048, 128, 8900)])
+def test_linear_shards_by_tiles(rows, cols, vocab, dtype):
+    """Three ranks whose logits come in tiles: middle ones, and a launch of wide ones with middle ones behind it.  Each rank's statistics
+    and gradients, and the sum of their shares of the hidden states' gradient against the whole vocabulary's."""
+    ranks, temp = 3, 2.0
+    whole = vocab * ranks
+    h, w, t, g = _case(rows, cols, whole, dtype, vocab)
+    ids, z = _teacher(rows, 12, whole, 3)
+    for given, args, more, call, grad, names in (
+            (R.targets(t, whole), (t,), {}, E.linear_cross_entropy, E.linear_cross_entropy_grad, {"lse", "target"}),
+            (R.entries(ids, z, whole, temp), (ids, z), dict(temperature=temp), E.linear_distillation, E.linear_distillation_grad,
+             {"lse", "target", "entropy"})):
+        scale = temp if more else 1.0
+        at = [dict(vocab_start=rank * vocab, vocab_size=whole, **more) for rank in range(ranks)]
+        parts = [w[rank * vocab:(rank + 1) * vocab] for rank in range(ranks)]
+        stats, bounds = [], []
+        for rank in range(ranks):
+            out, ref = call(h, parts[rank], *args, **at[rank]), R.linear(h, parts[rank], given, rank * vocab, whole, scale)
+            assert set(out) == names
+            _close(out, ref)
+            stats.append(out)
+            bounds.append({k: ref[k][1] + R.U * (ref[k][0].abs() + ref[k][1]) for k in names})
+        lse = torch.logsumexp(torch.stack([s["lse"] for s in stats]), 0)
+        dh = bound = 0
+        for rank in range(ranks):
+            out = grad(h, parts[rank], *args, lse, g, **at[rank])
+            ref = R.linear(h, parts[rank], given, rank * vocab, whole, scale, lse=lse, grad_loss=g)
+            _close(out, ref)
+            dh, bound = dh + out["dhidden"].double(), bound + ref["dhidden"][1] + R.UNIT[dtype] * (ref["dhidden"][0].abs() + ref["dhidden"][1])
+        value = R.linear(h, w, given, 0, whole, scale, lse=lse, grad_loss=g)["dhidden"][0]
+        assert ((dh - value).abs() <= bound + R.SMALL[dtype] * ranks).all()
+        # the joined loss is the whole vocabulary's; the join itself is a few roundings of its result
+        joined = lse.double() - sum(s["target"].double() for s in stats) - (stats[0]["entropy"].double() if more else 0)
+        e = torch.stack([b["lse"] for b in bounds]).max(0).values + 16 * R.U * (lse.double().abs() + 1)
+        e = e + sum(b["target"] for b in bounds) + (bounds[0]["entropy"] if more else 0)
+        value, trained = R.linear(h, w, given, 0, whole, scale)["loss"][0], given[5]
+        assert trained.any() and ((scale * scale * joined - value).abs() <= scale * scale * e)[trained].all()
