@@ -1,5 +1,5 @@
 """The output head's losses and distillation at the calls that tests/test_gpu_head.py does not make, against 64 bits: every
-statistic asked for together, shards by tiles."""
+statistic asked for together, logits far from zero, weights of rows not trained on, shards by tiles, few rows, repeated ids."""
 from __future__ import annotations
 
 import math
@@ -392,3 +392,47 @@ def test_linear_shards_by_tiles(rows, cols, vocab, dtype):
         e = e + sum(b["target"] for b in bounds) + (bounds[0]["entropy"] if more else 0)
         value, trained = R.linear(h, w, given, 0, whole, scale)["loss"][0], given[5]
         assert trained.any() and ((scale * scale * joined - value).abs() <= scale * scale * e)[trained].all()
+
+
+# ---------------------------------------------------------------- few rows, repeated ids
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("rows", [1, 2, 64])
+def test_shares_of_few_rows_have_two_planes(rows, dtype):
+    """Of up to 64 rows the logits' gradient is held in twice the bits: with the table's gradient in 32 bits nothing is off by a
+    rounding to the type.  Products of small whole numbers, so that the logits are exact; half precision's smallest step is 2^-39 of the
+    largest weight."""
+    cols, vocab = 64, 300
+    g = _gen(rows)
+    h = torch.randint(-2, 3, (rows, cols), generator=g, device="cuda").to(dtype)
+    w = (torch.randint(-2, 3, (vocab, cols), generator=g, device="cuda") / 16).to(dtype)
+    t = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    gl = torch.linspace(1, 2, rows, device="cuda")
+    rel, least = R.SHARE[dtype]
+    out = E.linear_cross_entropy(h, w, t, grad_loss=gl, dtype=F32)
+    got = {"one call": out["dweight"], "from lse": E.linear_cross_entropy_grad(h, w, t, out["lse"], gl, dtype=F32)["dweight"]}
+    x = h.double() @ w.double().t()
+    for name, lse in (("one call", None), ("from lse", out["lse"])):
+        d, e_d = R.loss(x, torch.zeros_like(x), *R.targets(t, vocab), 0, vocab, 1.0, lse, gl)["grad"]
+        e_d = e_d + (d.abs() + e_d) * (rel * rel + 8 * R.U) + least * float(gl.max())
+        v, e = R.product(d.t(), h.double(), dtype, e_d.t())
+        e = e + e * 0.01 + 4 * R.U * v.abs()      # the second plane's own sum is 2^-8 of the first's at most
+        R.close(got[name], v, e, name)
+        # one plane alone would be off by more
+        one = (d / gl.max().double()).float().to(dtype).double() * gl.max().double()
+        assert ((one.t() @ h.double() - v).abs() > 2 * (e + R.U * v.abs())).any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_repeated_ids_in_tiles(dtype):
+    """1024 entries a row whose ids come several times, where a tile's entries are in cells."""
+    rows, cols, vocab = TILES
+    h, w, _, g = _case(rows, cols, vocab, dtype, 2)
+    gen = _gen(9)
+    ids = torch.randint(0, vocab, (rows, 1024), generator=gen, device="cuda")
+    z = _normal(gen, rows, 1024)
+    ids[0] = 7
+    ids[1::4, 1::2] = ids[1::4, 0::2]
+    ids[2::4, 512:] = ids[2::4, :1]
+    z[2::4, 0] = -math.inf
+    _close(E.linear_distillation(h, w, ids, z, grad_loss=g), R.linear(h, w, R.entries(ids, z, vocab, 1.0), 0, vocab, grad_loss=g))
