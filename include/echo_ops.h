@@ -126,16 +126,20 @@ int echo_cross_entropy_grad(const void *logits, int64_t logits_stride, int32_t t
 /*
  * Distillation of rows of logits over the ids [vocab_start, vocab_start + cols) of a vocabulary of vocab_size ids from a
  * teacher's top logits: `top` ids a row and their logits, ids [rows][top] and teacher [rows][top] of teacher_type (`type` or
- * ECHO_F32), 1 <= top <= 1024.  Ids outside [0, vocab_size) are padding, and an id may come more than once (its masses add
- * up).  With T the temperature (1e-6 to 1e6), q the softmax of teacher / T over the row's ids in the vocabulary and p that of
- * logits / T over the vocabulary, per row (any of lse, target, entropy, loss may be NULL; 32 bits):
+ * ECHO_F32), 1 <= top <= 1024.  Ids outside [0, vocab_size) are padding.  With T the temperature (1e-6 to 1e6), q the softmax of
+ * teacher / T over the row's entries whose ids are in the vocabulary, one q an entry, and p that of logits / T over the
+ * vocabulary, per row (any of lse, target, entropy, loss may be NULL; 32 bits):
  *   lse      log of the sum of exp(logits / T): -inf where every logit is -inf, NaN where the row has a NaN or +inf
- *   target   sum of q * logit / T over the ids held here
- *   entropy  -sum of q log q over all ids of the row
- *   loss     T^2 * sum of q (log q - log p); 0 for a row without an id whose logit is above -inf, which is not trained on, +inf
- *            where q is not 0 and the logit is -inf (whole vocabulary only)
+ *   target   sum of q * logit / T over the entries whose ids are held here
+ *   entropy  -sum of q log q over all entries of the row
+ *   loss     T^2 * sum over the entries of q (log q - log p of its id); 0 for a row without an id whose logit is above -inf, which
+ *            is not trained on, +inf where q is not 0 and the logit is -inf (whole vocabulary only)
  *   grad     T (p - q) * grad_loss[row], [rows][cols] of `type` (whole vocabulary only), in the same pass.  Rows not
  *            trained on and rows without a finite logit get zeros.  May be logits itself.
+ * Where a row's ids are all different, loss is T^2 times the divergence of p from q.  An id may come more than once: in grad and
+ * target its entries' q add up, while entropy and loss stay sums over the entries, each with its own log q.  Two entries q1 and q2
+ * of one id have a loss below that of one entry q1 + q2, by T^2 ((q1 + q2) log(q1 + q2) - q1 log q1 - q2 log q2), a
+ * constant of the student; the loss of such a row may be below 0.
  * For a vocabulary over several ranks, every rank is given all of a row's ids; the whole lse is log(sum over ranks of
  * exp(lse)), loss = T^2 * (lse - sum over ranks of target - entropy), and echo_distillation_grad gives each rank its gradient.
  */

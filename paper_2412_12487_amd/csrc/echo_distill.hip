@@ -1,7 +1,8 @@
 // echo_distill.hip -- distillation from a teacher's top logits over a vocabulary or a shard of one, on gfx950.
 //
-// Per row, at temperature T: q = softmax of the teacher's logits / T over its ids in the vocabulary, p = softmax of the
-// logits / T over the vocabulary, loss = T^2 sum q (log q - log p), and the logits' gradient T (p - q) grad_loss.
+// Per row, at temperature T: q = softmax of the teacher's logits / T over its entries in the vocabulary, p = softmax of the
+// logits / T over the vocabulary, loss = T^2 sum over entries of q (log q - log p), and the logits' gradient T (p - q) grad_loss,
+// in which the q of one id add up.
 #include "echo_teacher.h"
 
 namespace echo {

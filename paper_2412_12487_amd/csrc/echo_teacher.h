@@ -53,7 +53,7 @@ struct Entry {
 };
 struct Teacher {
     bool trained;      // an id of the vocabulary has a mass
-    float prior;       // sum of q log q
+    float prior;       // sum of q log q over the entries, also of those that name an id together
 };
 // The row's entries whose columns are in [first, first + cols).
 //

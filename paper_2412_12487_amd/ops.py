@@ -442,15 +442,19 @@ def _stats(res, names, like, dev, shape):
 def distillation(logits, ids, teacher, *, temperature=1.0, vocab_start=0, vocab_size=None, grad_loss=None, out=None):
     """Distillation of rows of logits from a teacher's top logits: ids and teacher have the leading shape of logits and up to
     1024 entries a row, teacher logits' type or float32.  Ids outside the vocabulary are padding; a row of padding alone is not
-    trained on; an id may come more than once.  With q the softmax of teacher / temperature over a row's ids and p
-    that of logits / temperature over the vocabulary, loss = temperature^2 * sum of q (log q - log p).
+    trained on.  With q the softmax of teacher / temperature over a row's entries and p
+    that of logits / temperature over the vocabulary, loss = temperature^2 * sum over the entries of q (log q - log p of its id).
+
+    An id may come more than once.  Its entries' q add up in the gradient and in 'target'; the loss and 'entropy' are sums over the
+    entries, each with its own log q, so that the loss is lower than that of the merged entry by a constant of the student (two equal
+    entries alone in a row: temperature^2 log 2) and may be below 0.
 
     Whole vocabulary (vocab_size not given): a dict with 'loss', 'lse' (log of the sum of exp(logits / temperature)),
     float32, and, if grad_loss is given, 'grad': that of the logits, in the same pass.  `out` may supply tensors
     of those names; 'grad' may be logits itself.
 
     A shard of it, as in cross_entropy: a dict with 'lse' over these rows, 'target' (sum of q * logit / temperature over the
-    ids held here) and 'entropy' (-sum of q log q over all of a row's ids, the same on every rank).  loss =
+    ids held here) and 'entropy' (-sum of q log q over all of a row's entries, the same on every rank).  loss =
     temperature^2 * (whole lse - sum over ranks of target - entropy); distillation_grad gives each rank its gradient."""
     dev = _gpu(logits, "logits")
     rows, cols, ls = _matrix(logits, "logits", dev, _TYPES)

@@ -436,3 +436,35 @@ def test_repeated_ids_in_tiles(dtype):
     ids[2::4, 512:] = ids[2::4, :1]
     z[2::4, 0] = -math.inf
     _close(E.linear_distillation(h, w, ids, z, grad_loss=g), R.linear(h, w, R.entries(ids, z, vocab, 1.0), 0, vocab, grad_loss=g))
+
+
+def test_an_id_named_twice():
+    """Masses of an id add up in the gradient, in the cross term and in a shard's target; sum of q log q is over the entries, each with
+    its own mass.  A student certain of an id that is named twice with equal logits has a loss of -T^2 log 2, and one that is merged
+    into a single entry 0; their gradients are the same."""
+    temp, ln2 = 2.0, math.log(2.0)
+    for cols in (5, 700, 40000, 70000):
+        l = torch.full((2, cols), -math.inf, device="cuda")
+        l[:, 3] = 1.0
+        ids = torch.tensor([[3, 3], [3, -1]], device="cuda")
+        z = torch.tensor([[0.5, 0.5], [0.5 + temp * ln2, 0.0]], device="cuda")
+        gl = torch.ones(2, device="cuda")
+        out = E.distillation(l, ids, z, temperature=temp, grad_loss=gl)
+        assert abs(float(out["loss"][0]) + temp * temp * ln2) < 1e-5 and abs(float(out["loss"][1])) < 1e-5
+        assert float(out["grad"].abs().max()) < 1e-6
+        shard = E.distillation(l, ids, z, temperature=temp, vocab_start=0, vocab_size=cols + 7)
+        assert abs(float(shard["entropy"][0]) - ln2) < 1e-6 and float(shard["entropy"][1]) == 0
+        assert torch.allclose(shard["target"], torch.full((2,), 0.5, device="cuda"), atol=1e-6)
+        away = E.distillation(l, ids, z, temperature=temp, vocab_start=9, vocab_size=cols + 9)      # the id is another rank's
+        assert torch.equal(away["entropy"], shard["entropy"]) and not away["target"].any()
+    for rows, cols, vocab in (FEW, TILES):
+        h, w, _, gl = _case(rows, cols, vocab, F32, 4)
+        ids, z = _teacher(rows, 4, vocab // 4, 3)
+        ids = torch.where(ids < 0, ids, ids * 4 + torch.arange(4, device="cuda"))      # no id twice
+        split, halves = torch.cat([ids, ids], 1), torch.cat([z, z], 1)
+        one = E.linear_distillation(h, w, ids, z, temperature=temp, grad_loss=gl)
+        two = E.linear_distillation(h, w, split, halves, temperature=temp, grad_loss=gl)
+        trained = (ids >= 0).any(1)
+        assert torch.allclose(two["loss"], torch.where(trained, one["loss"] - temp * temp * ln2, 0.0), atol=1e-4)
+        for k in ("dhidden", "dweight"):
+            assert float((two[k] - one[k]).abs().max()) <= 1e-5 * float(one[k].abs().max()), k
