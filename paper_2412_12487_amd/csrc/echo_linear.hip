@@ -60,13 +60,17 @@ struct Cells {
 // The largest finite |grad_loss| of the rows that are trained on, or 1 where there is none above 0: what the gradient's shares are
 // relative to, so that rows of one weight have it exactly.  What stands in other rows, infinities among it, is not their concern.
 template <int THREADS, class Trained>
-__device__ __forceinline__ void write_scale(const float *grad_loss, int rows, float *scale, float *lds, Trained trained) {
+__device__ __forceinline__ float largest_of(const float *grad_loss, int rows, Trained trained) {
     float top = 0.0f;
 #pragma unroll 4
-    for (int n = threadIdx.x; n < rows; n += THREADS) {
+    for (int n = threadIdx.x; n < rows; n += THREADS) {      // without branches, so that four rows are on their way
         const float g = fabsf(grad_loss[n]);
-        if (trained(n) && g < kInf) top = fmaxf(top, g);
+        top = fmaxf(top, (trained(n) & (g < kInf)) ? g : 0.0f);
     }
+    return top;
+}
+template <int THREADS>
+__device__ __forceinline__ void write_scale(float top, float *scale, float *lds) {
     top = wave_max(top);
     if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = top;
     __syncthreads();
@@ -74,10 +78,18 @@ __device__ __forceinline__ void write_scale(const float *grad_loss, int rows, fl
     for (int w = 1; w < THREADS / kWave; ++w) top = fmaxf(top, lds[w]);
     *scale = top > 0.0f ? top : 1.0f;
 }
-// Whether a row is trained on, once the teacher's entries are prepared.
-__device__ __forceinline__ bool is_trained(const HeadArgs &a, int n) {
-    if (a.top) return a.prior[n].y > 0.0f;
-    return row_of(a, a.wide_index ? id_at<int64_t>(a.targets, n) : id_at<int32_t>(a.targets, n)).trained;
+template <int THREADS, class I>
+__device__ __forceinline__ float largest_of(const float *grad_loss, int rows, const void *targets, int64_t vocab_size) {
+    return largest_of<THREADS>(grad_loss, rows, [=](int n) ECHO_INLINE { return (uint64_t)id_at<I>(targets, n) < (uint64_t)vocab_size; });
+}
+// Once the teacher's entries are prepared.
+template <int THREADS>
+__device__ __forceinline__ void write_scale(const HeadArgs &a, float *lds) {
+    const float2 *prior = a.prior;
+    const float top = a.top          ? largest_of<THREADS>(a.grad_loss, a.rows, [=](int n) ECHO_INLINE { return prior[n].y > 0.0f; })
+                      : a.wide_index ? largest_of<THREADS, int64_t>(a.grad_loss, a.rows, a.targets, a.vocab_size)
+                                     : largest_of<THREADS, int32_t>(a.grad_loss, a.rows, a.targets, a.vocab_size);
+    write_scale<THREADS>(top, a.scale_out, lds);
 }
 
 // Tiles of logits, i over the vocabulary and j over the rows.  2048 x 8192 over 49152 ids in wide tiles: 1.21 to 1.31 ms, 1260 to 1360
@@ -92,8 +104,7 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArg
     __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
     if constexpr (MODE == kKeep)
         if ((int)blockIdx.x == a.m.tiles_i * a.m.tiles_j)
-            return write_scale<S::THREADS>(a.grad_loss, a.rows, a.scale_out, reinterpret_cast<float *>(t0),
-                                           [&](int n) ECHO_INLINE { return is_trained(a, n); });
+            return write_scale<S::THREADS>(a, reinterpret_cast<float *>(t0));
     const Place at = place_of(a.m, blockIdx.x);
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wi = wave / S::WJ, wj = wave % S::WJ;
@@ -276,10 +287,13 @@ template <class T, class S>
 __global__ __launch_bounds__(S::THREADS, S::THREADS < 256 ? 1 : S::THREADS / 256) void k_parts(PartsArgs a) {
     __shared__ __attribute__((aligned(16))) char t0[S::BYTES];
     __shared__ __attribute__((aligned(16))) char t1[S::BYTES];
-    if ((int)blockIdx.x == a.m.tiles_i * a.m.tiles_j * a.m.splits)
-        return write_scale<S::THREADS>(a.grad_loss, a.m.nj, a.scale_out, reinterpret_cast<float *>(t0), [&](int n) ECHO_INLINE {
-            return is_trained(a.in, n);
-        });
+    if ((int)blockIdx.x == a.m.tiles_i * a.m.tiles_j * a.m.splits) {
+        const TeacherIn &in = a.in;
+        const float top = in.top ? largest_of<S::THREADS>(a.grad_loss, a.m.nj, [&](int n) ECHO_INLINE { return has_mass(in, n); })
+                          : in.index_type == ECHO_I64 ? largest_of<S::THREADS, int64_t>(a.grad_loss, a.m.nj, in.ids, in.vocab_size)
+                                                      : largest_of<S::THREADS, int32_t>(a.grad_loss, a.m.nj, in.ids, in.vocab_size);
+        return write_scale<S::THREADS>(top, a.scale_out, reinterpret_cast<float *>(t0));
+    }
     const Place at = place_of(a.m, blockIdx.x);
     F4 acc[S::BI][S::BJ];
     multiply<T, true, true, S>(a.m, at, t0, t1, acc);
@@ -621,7 +635,7 @@ __global__ __launch_bounds__(256) void k_teacher(TeacherArgs a) {
 // For a gradient whose loss was another call's; else the loss's launch has a workgroup for it.
 __global__ __launch_bounds__(1024) void k_scale(HeadArgs a) {
     __shared__ float lds[16];
-    write_scale<1024>(a.grad_loss, a.rows, a.scale_out, lds, [&](int n) ECHO_INLINE { return is_trained(a, n); });
+    write_scale<1024>(a, lds);
 }
 
 // Rows laid out for the products: PLANES planes of 16 bits, rows filled up with zeros to whole steps.  One launch for both

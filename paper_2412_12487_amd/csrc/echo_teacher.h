@@ -34,12 +34,11 @@ __device__ __forceinline__ float value_at(const void *p, int type, int64_t at) {
     if (type == ECHO_F32) return static_cast<const float *>(p)[at];
     return type == ECHO_F16 ? (float)static_cast<const f16 *>(p)[at] : (float)static_cast<const bf16 *>(p)[at];
 }
-// Whether a row is trained on: its target is in the vocabulary, or an id of the vocabulary has a mass.
-__device__ __forceinline__ bool is_trained(const TeacherIn &t, int64_t row) {
-    const int n = t.top ? t.top : 1;
-    for (int k = 0; k < n; ++k) {
-        const int64_t id = index_at(t.ids, t.index_type, row * n + k);
-        if (id >= 0 && id < t.vocab_size && !(t.top && value_at(t.logits, t.type, row * n + k) * t.inv_t == -kInf)) return true;
+// Whether an id of a row has a mass, where its entries are not prepared: its first entry tells that of most rows.
+__device__ __forceinline__ bool has_mass(const TeacherIn &t, int64_t row) {
+    for (int k = 0; k < t.top; ++k) {
+        const int64_t id = index_at(t.ids, t.index_type, row * t.top + k);
+        if (id >= 0 && id < t.vocab_size && value_at(t.logits, t.type, row * t.top + k) * t.inv_t != -kInf) return true;
     }
     return false;
 }
