@@ -160,18 +160,20 @@ int echo_distillation_grad(const void *logits, int64_t logits_stride, int32_t ty
 
 /*
  * The same losses straight from hidden states [rows][cols] and an output table, `vocab` rows of cols elements for the ids
- * [vocab_start, vocab_start + vocab): logits = hidden weight^T, which are not kept.  hidden and weight are of `type`; the
+ * [vocab_start, vocab_start + vocab): logits = hidden weight^T, which are not returned.  hidden and weight are of `type`; the
  * products are of 16-bit elements (three of them for one of 32 bits) with sums in 32 bits, and logits, statistics and losses
  * are in 32 bits.  Gradients (both or neither), of the loss sum over rows of grad_loss * loss, with d the logits'
  * gradient of above:
  *   dhidden = d weight, [rows][cols] of `type`;   dweight = d^T hidden, [vocab][cols] of grad_type (`type` or ECHO_F32),
  *   written, or with accumulate != 0 added to.
- * Of 16-bit types d is rounded to `type` (relative to the largest finite |grad_loss| of the rows trained on) before these products, as the
- * logits' gradient of echo_cross_entropy is (of up to 64 rows it may be held in twice the bits); of 32 bits it is held in 24.  Rows not trained on have d = 0.  A row whose hidden state
- * has a NaN or an infinity gives NaN to every row of dweight, trained on or not.  Logits beyond 2^127 / T count as infinite, and
- * 32-bit elements beyond the largest of bfloat16, infinities among them, as NaN.
- * echo_linear_cross_entropy gives loss and gradients with the whole vocabulary, or a shard's lse and target;
- * echo_linear_cross_entropy_grad is given the whole vocabulary's lse.  The distillations are their counterparts.
+ * Of 16-bit types d is rounded to `type` (relative to the largest finite |grad_loss| of the rows trained on) before these
+ * products, as the logits' gradient of echo_cross_entropy is (of up to 64 rows it may be held in twice the bits); of 32 bits it
+ * is held in 24.  Rows not trained on have d = 0.  A row whose hidden state has a NaN or an infinity gives NaN to every row of
+ * dweight, trained on or not.  Logits / T beyond the largest number of 32 bits make lse infinite, and 32-bit elements beyond the
+ * largest of bfloat16, infinities among them, count as NaN.
+ * echo_linear_cross_entropy gives loss and gradients with the whole vocabulary (gradients together with lse), or a shard's lse
+ * and target; echo_linear_cross_entropy_grad is given the whole vocabulary's lse: of ECHO_F16 one that is more than 1.38 below a
+ * logit / T may overflow the gradients.  The distillations are their counterparts.
  * rows, vocab <= 2^24, cols <= 2^20, and the product of any two <= 2^38 (else ECHO_ERR_RANGE).
  * workspace: at least echo_linear_workspace(...) bytes for the same matrices, aligned to 16; top is 0 for the cross entropies,
  * loss and grads say which of the two the call computes.  It holds at most about 1 GiB of the logits' gradient at a time (256 columns

@@ -92,11 +92,11 @@ __device__ __forceinline__ void write_scale(const HeadArgs &a, float *lds) {
     write_scale<THREADS>(top, a.scale_out, lds);
 }
 
-// Tiles of logits, i over the vocabulary and j over the rows.  2048 x 8192 over 49152 ids in wide tiles: 1.21 to 1.31 ms, 1260 to 1360
+// Tiles of logits, i over the vocabulary and j over the rows.  2048 x 8192 over 49152 ids in wide tiles: 1.21 to 1.34 ms, 1230 to 1360
 // TFLOP/s (a library product alone: 1340); the last rounding, maxima and exponentials of a tile take 13 us of a round's 205.
 //   kLoss: each row's maximum and sum of exponentials over a wavefront's columns, and the logits of its target or entries.
 //   kKeep: the same, and the exponentials, relative to that maximum.
-//   kGrad: the gradient's share of each logit, (exp(x / T - lse) - q) * grad_loss / scale, rounded to T.
+//   kGrad: the gradient's share of each logit, (p - q) * grad_loss / scale, rounded to the elements' type.
 enum { kLoss, kKeep, kGrad };
 template <class T, class S, int MODE, int PLANES>
 __global__ __launch_bounds__(S::THREADS, S::THREADS / 256) void k_logits(HeadArgs a) {

@@ -7,7 +7,7 @@ stage outside its layers' matrix products, on the GPU at hand (`workloads.measur
     y = layer_norm(x, weight, bias)["y"]
     h = embedding(ids, table, scale)
     r = cross_entropy(logits, targets, grad_loss=g)          # loss, lse and the logits' gradient
-    r = linear_cross_entropy(h, table, targets, grad_loss=g) # loss, lse, dhidden and dweight: logits are not kept
+    r = linear_cross_entropy(h, table, targets, grad_loss=g) # loss, lse, dhidden and dweight; no logits
     r = distillation(logits, ids, teacher, temperature=2.0, grad_loss=g)
 
 Activations are float32, float16 or bfloat16 matrices whose rows are contiguous (leading dimensions in
@@ -570,8 +570,11 @@ def _target_args(targets, dev, rows, shape):
 
 def linear_cross_entropy(hidden, weight, targets, *, vocab_start=0, vocab_size=None, grad_loss=None, dtype=None, out=None,
                          accumulate=False, workspace=None):
-    """cross_entropy of the logits hidden @ weight.t(), which are not kept: weight is a matrix of the vocabulary's rows, of
+    """cross_entropy of the logits hidden @ weight.t(), which are not returned: weight is a matrix of the vocabulary's rows, of
     hidden's type.
+
+    Without gradients the workspace holds statistics alone.  With them it holds the logits' gradient, rows * vocabulary elements of 16
+    bits (three times that for float32), up to about 1 GiB at a time; in one call of float16 and float32 as many of 32 bits again.
 
     Whole vocabulary: a dict with 'loss' and 'lse' and, if grad_loss (float32, the gradient of each row's loss) is given,
     'dhidden' like hidden and 'dweight' like weight or of `dtype` (float32).  `out` may supply tensors of those names;
@@ -598,7 +601,7 @@ def linear_cross_entropy_grad(hidden, weight, targets, lse, grad_loss, *, vocab_
 
 def linear_distillation(hidden, weight, ids, teacher, *, temperature=1.0, vocab_start=0, vocab_size=None, grad_loss=None,
                         dtype=None, out=None, accumulate=False, workspace=None):
-    """distillation of the logits hidden @ weight.t(), which are not kept; tensors and gradients as in
+    """distillation of the logits hidden @ weight.t(), which are not returned; tensors, workspace and gradients as in
     linear_cross_entropy, ids, teacher and the statistics of a shard as in distillation."""
     head = _head(hidden, weight, vocab_start, vocab_size)
     given, top, temp = _teacher_args(ids, teacher, temperature, head[0], head[1], head[2], hidden.dtype)

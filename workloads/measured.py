@@ -28,7 +28,7 @@ def training_step(ids, targets, table, norms, *, scale=1.0, eps=1e-5, fused=Fals
     logits' use is rounded to the table's type first) and 'norms', a list of (weight gradient, bias gradient), float32.
     Nothing waits for the GPU.
 
-    fused: the head and its loss are one operator, which keeps no logits; the logits' use is then added up in 32 bits.
+    fused: the head and its loss are one operator, which returns no logits; the logits' use is then added up in 32 bits.
     teacher, with fused: (ids [tokens, top], logits, temperature) of a teacher whose mean distillation loss is added."""
     if teacher is not None and not fused:
         raise ValueError("a teacher needs the fused head")
