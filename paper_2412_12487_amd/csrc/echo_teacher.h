@@ -38,7 +38,7 @@ __device__ __forceinline__ float value_at(const void *p, int type, int64_t at) {
 __device__ __forceinline__ bool has_mass(const TeacherIn &t, int64_t row) {
     for (int k = 0; k < t.top; ++k) {
         const int64_t id = index_at(t.ids, t.index_type, row * t.top + k);
-        if (id >= 0 && id < t.vocab_size && value_at(t.logits, t.type, row * t.top + k) * t.inv_t != -kInf) return true;
+        if (id >= 0 && id < t.vocab_size && value_at(t.logits, t.type, row * t.top + k) != -kInf) return true;
     }
     return false;
 }
@@ -65,7 +65,7 @@ __device__ __forceinline__ Teacher teacher_of(const TeacherIn &t, int64_t row, i
     const auto logit = [&](int k) ECHO_INLINE {
         const int64_t id = index_at(t.ids, t.index_type, from + k);
         const float z = value_at(t.logits, t.type, from + k);      // beside the id, not behind it
-        return id >= 0 && id < t.vocab_size ? z * t.inv_t : -kInf;
+        return id >= 0 && id < t.vocab_size ? z : -kInf;
     };
     float top = -kInf, sum = 0.0f, prior = 0.0f;
     for (int k = lane; k < t.top; k += kWave) {
@@ -74,13 +74,15 @@ __device__ __forceinline__ Teacher teacher_of(const TeacherIn &t, int64_t row, i
         top = fmaxf(top, z);
     }
     top = wave_max(top);
+    // distances from the largest logit, before they are divided by T: of logits far from 0 they are exact
     const float base = top == -kInf ? 0.0f : top;
-    for (int k = lane; k < t.top; k += kWave) sum += expf(entries[k].x - base);
+    const auto distance = [&](int k) ECHO_INLINE { return (entries[k].x - base) * t.inv_t; };
+    for (int k = lane; k < t.top; k += kWave) sum += expf(distance(k));
     sum = wave_sum(sum);
     const bool live = sum != 0.0f;      // NaN too
     const float log_sum = logf(sum);
     for (int k = lane; k < t.top; k += kWave) {
-        const float d = entries[k].x - base, q = live ? expf(d) / sum : 0.0f;
+        const float d = distance(k), q = live ? expf(d) / sum : 0.0f;
         if (q != 0.0f) prior += q * (d - log_sum);
         int at = q != 0.0f ? shard_row(index_at(t.ids, t.index_type, from + k), t.vocab_start, vocab) : -1;
         if ((unsigned)(at - first) >= (unsigned)cols) at = -1;
@@ -108,7 +110,7 @@ __device__ __forceinline__ Teacher teacher_of(const TeacherIn &t, int64_t row, i
         if (mine >= 0) {
             for (int o = 0; o < t.top; ++o) {
                 if (entries[o].at != mine) continue;
-                mass += expf(entries[o].x - base) / sum;
+                mass += expf(distance(o)) / sum;
                 later |= o < k;
             }
         }

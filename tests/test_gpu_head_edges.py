@@ -311,6 +311,47 @@ def test_a_given_lse_is_above_every_logit(rows, cols, vocab, dtype):
     _check_far(got, h, w, x, q, gl, float(torch.tensor(temp)), p, e_p + 16 * R.U * p, dtype)
 
 
+@pytest.mark.parametrize("temp", [0.3, 1e-3, 1e-6])
+@pytest.mark.parametrize("size", [2.0 ** 10, 2.0 ** 20])
+@pytest.mark.parametrize("where", ["logits", "rows of parts", "tiles"])
+def test_teachers_logits_far_from_zero(where, size, temp):
+    """A teacher whose logits differ by a few of their last places: its distribution follows from their distances.  The student's is even."""
+    rows, cols, vocab = TILES if where == "tiles" else FEW
+    g = _gen(3)
+    ids = _distinct(g, rows, 5, vocab)
+    z = size + torch.randint(0, 9, (rows, 5), generator=g, device="cuda") * (size * 2.0 ** -23)
+    z[::2] *= -1
+    ids[3, 2] = -1
+    z[4, 1] = -math.inf
+    gl = torch.full((rows,), 1 / rows, device="cuda")
+    t32 = float(torch.tensor(temp))
+    x = torch.where(ids >= 0, z.double(), -math.inf)
+    d = (x - x.max(1, keepdim=True).values) / t32
+    q = torch.softmax(d, 1)
+    far = torch.where(q > 0, d.abs(), 0.0)
+    e_q = q * R.U * (4 * far.max(1, keepdim=True).values + 64)
+    plogp = torch.special.xlogy(q, q)
+    e_prior = (e_q * (1 + torch.where(q > 0, torch.log(q).abs(), 0.0))).sum(1) + 16 * R.U * (plogp.abs().sum(1) + 1)
+    dense = torch.zeros(rows, vocab, dtype=torch.float64, device="cuda").scatter_add_(1, ids.clamp(min=0), torch.where(ids >= 0, q, 0.0))
+    e_dense = torch.zeros_like(dense).scatter_add_(1, ids.clamp(min=0), torch.where(ids >= 0, e_q, 0.0))
+    loss = t32 * t32 * (plogp.sum(1) + math.log(vocab))
+    e_loss = t32 * t32 * (e_prior + 64 * R.U * math.log(vocab))
+    if where == "logits":
+        l = torch.zeros(rows, vocab, device="cuda")
+        out = E.distillation(l, ids, z, temperature=temp, grad_loss=gl)
+        scale = gl.double()[:, None] * t32
+        R.close(out["grad"], (1 / vocab - dense) * scale, scale * (e_dense + 64 * R.U / vocab + 8 * R.U * dense), "grad")
+        entropy = E.distillation(l, ids, z, temperature=temp, vocab_start=0, vocab_size=vocab)["entropy"]
+    else:
+        h, w = torch.zeros(rows, cols, device="cuda"), torch.randint(-2, 3, (vocab, cols), generator=g, device="cuda").float()
+        out = E.linear_distillation(h, w, ids, z, temperature=temp, grad_loss=gl)
+        zero = torch.full_like(dense, 1 / vocab)
+        _check_far(out, h, w, None, dense, gl, t32, zero, e_dense + 64 * R.U * zero, F32)
+        entropy = E.linear_distillation(h, w, ids, z, temperature=temp, vocab_start=0, vocab_size=vocab)["entropy"]
+    R.close(entropy, -plogp.sum(1), e_prior, "entropy")
+    R.close(out["loss"], loss, e_loss, "loss")
+
+
 # ---------------------------------------------------------------- rows whose weight is not used
 
 @pytest.mark.parametrize("dtype", TYPES)
