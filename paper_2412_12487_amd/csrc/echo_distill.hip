@@ -9,7 +9,7 @@ namespace echo {
 namespace {
 
 __device__ __forceinline__ TeacherIn teacher_in(const DistillArgs &a) {
-    return TeacherIn{a.ids, a.teacher, a.index_type, a.teacher_type, a.top, a.vocab_start, a.vocab_size, 1.0f / a.temperature};
+    return TeacherIn{a.ids, a.teacher, a.index_type, a.teacher_type, a.top, a.vocab_start, a.vocab_size, a.inv_t};
 }
 // The entries with the logits of their columns.
 template <class T>
@@ -22,6 +22,7 @@ __device__ __forceinline__ Teacher entries_of(const DistillArgs &a, int64_t row,
 }
 // Exponentials of logits / T relative to that of a logit `base`.  Logits' distances are taken before they are divided by T: at logits / T of
 // 10^10, whose last place is 1024, the maximum's own exponential is 1 and the others follow from their distances alone.
+// 1 / T and log2(e) / T are arguments: made by every lane they cost a row of 51201 of bf16 two registers more than there are, 126 us and not 111.
 struct Relative {
     float base, k;      // k: log2(e) / T
     __device__ __forceinline__ float operator()(float l) const { return __builtin_amdgcn_exp2f((l - base) * k); }
@@ -40,7 +41,7 @@ __device__ __forceinline__ void put_entries(T *grad, const Entry *entries, int t
     }
 }
 __device__ __forceinline__ float finish_row(const DistillArgs &a, int64_t row, const Teacher &t, const Entry *entries, float top, float sum) {
-    const float inv_t = 1.0f / a.temperature, more = logf(sum), lse = top == -kInf ? -kInf : top * inv_t + more;
+    const float inv_t = a.inv_t, more = logf(sum), lse = top == -kInf ? -kInf : top * inv_t + more;
     // the loss takes logits from their maximum on, the target as they are
     const float cross = a.loss ? cross_of(entries, a.top, top != -kInf ? top : 0.0f) * inv_t : 0.0f;
     const float target = a.target ? cross_of(entries, a.top, 0.0f) * inv_t : 0.0f;
@@ -74,7 +75,7 @@ __global__ __launch_bounds__((Team<T, THREADS, E, CUT>::BLOCK), (kDistillWaves<T
     extern __shared__ __attribute__((aligned(16))) char space[];
     Entry *entries = reinterpret_cast<Entry *>(space) + q.team * a.top;
     __shared__ float4 lds[2][Q::WAVES];
-    const float k2 = 1.0f / a.temperature * kLog2e;
+    const float k2 = a.k2;
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * Q::TEAMS + q.team; row < a.rows; row += (int64_t)gridDim.x * Q::TEAMS) {
         const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
@@ -143,7 +144,7 @@ __global__ __launch_bounds__(kWideBlock) void k_distill_wide(DistillArgs a) {
     extern __shared__ __attribute__((aligned(16))) char space[];
     Entry *entries = reinterpret_cast<Entry *>(space);
     __shared__ float4 lds[kWideWaves];
-    const float k2 = 1.0f / a.temperature * kLog2e;
+    const float k2 = a.k2;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *l = static_cast<const T *>(a.logits) + row * a.logits_stride;
         Teacher t{};
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {
     extern __shared__ __attribute__((aligned(16))) char space[];
     Entry *entries = reinterpret_cast<Entry *>(space);
     __shared__ int lds;
-    const float inv_t = 1.0f / a.temperature;
+    const float inv_t = a.inv_t;
     const int spans = (a.cols + SPAN - 1) / SPAN;
     const int64_t n = a.rows * spans;
     for (int64_t id = blockIdx.x; id < n; id += gridDim.x) {

@@ -397,6 +397,8 @@ int distill(DistillArgs a, int32_t type, int32_t index_type, int32_t teacher_typ
     if (!a.rows) return ECHO_OK;
     a.cols = (int)cols;
     a.top = (int)top;
+    a.inv_t = 1.0f / a.temperature;
+    a.k2 = a.inv_t * 1.44269504088896341f;
     return on_device(hip_device, what, [&] {
         return launch_distill(a, type, static_cast<hipStream_t>(hip_stream));
     });

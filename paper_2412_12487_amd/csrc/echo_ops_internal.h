@@ -80,6 +80,7 @@ struct DistillArgs {
     const float *lse_in, *grad_loss;
     void *grad;
     int64_t grad_stride;
+    float inv_t, k2;          // 1 / temperature, and log2(e) of it: scalar operands, not divisions of every lane
 };
 
 // Row partitions of the weight-gradient reduction, and bytes of scratch.
