@@ -63,7 +63,7 @@ __device__ __forceinline__ void settled() {
 }
 
 // A team a row, as in cross entropy: the row is read once and its gradient written from registers.  The gradient is then
-// written over at the teacher's ids.  Memory bounds it: 2048 x 51200 of bf16 with 64 ids a row takes 83 us with its gradient, 5.1 TB/s, on new
+// written over at the teacher's ids.  Memory bounds it: 2048 x 51200 of bf16 with 64 ids a row takes 85 us with its gradient, 4.9 TB/s, on new
 // logits (cross entropy 79); while one wavefront prepares the teacher's entries, the others take their maxima and sums.
 template <class T, int THREADS, int E>
 constexpr int kDistillWaves = THREADS == 1024 && E * sizeof(T) <= 128 ? 8 : 1;
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(kWideBlock) void k_distill_wide(DistillArgs a) {
 }
 
 // The gradient alone, from the whole vocabulary's lse: a workgroup takes a stretch of one row, and the teacher's entries in it.
-// 1000 x 12801 of half precision with 33 ids a row: 14.5 us, 3.5 TB/s, since each of a row's two workgroups prepares its entries.
+// 1000 x 12801 of half precision with 33 ids a row: 15.3 us, 3.3 TB/s, since each of a row's two workgroups prepares its entries.
 constexpr int kGradPieces = 4;
 template <class T>
 __global__ __launch_bounds__(256) void k_distill_grad(DistillArgs a) {

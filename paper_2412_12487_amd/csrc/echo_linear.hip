@@ -475,7 +475,7 @@ __global__ __launch_bounds__(BLOCK) void k_rows(RowsArgs a) {
 
 // The gradient's shares from the exponentials that the loss's pass kept, in place where they are of 16 bits; where the target
 // is or the teacher has a mass, from the logit itself.  A workgroup takes a stretch of one row.
-// Memory bounds it: 2048 x 51200 of bfloat16 in 68 us, 6.2 TB/s, where the logits' second product would take 1.4 ms at hidden
+// Memory bounds it: 2048 x 51200 of bfloat16 in 70 us, 6.0 TB/s, where the logits' second product would take 1.4 ms at hidden
 // size 8192 (19 us and 80 us for 512 rows at 1024).
 constexpr int kSpan = 256 * 8 * 2;
 template <class T, int PLANES>
