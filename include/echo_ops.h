@@ -139,7 +139,8 @@ int echo_cross_entropy_grad(const void *logits, int64_t logits_stride, int32_t t
  * Where a row's ids are all different, loss is T^2 times the divergence of p from q.  An id may come more than once: in grad and
  * target its entries' q add up, while entropy and loss stay sums over the entries, each with its own log q.  Two entries q1 and q2
  * of one id have a loss below that of one entry q1 + q2, by T^2 ((q1 + q2) log(q1 + q2) - q1 log q1 - q2 log q2), a
- * constant of the student; the loss of such a row may be below 0.
+ * constant of the student; the loss of such a row may be below 0.  Who wants the divergence there gives one entry an id, of
+ * logit T log(sum of exp(teacher / T) over its entries).
  * For a vocabulary over several ranks, every rank is given all of a row's ids; the whole lse is log(sum over ranks of
  * exp(lse)), loss = T^2 * (lse - sum over ranks of target - entropy), and echo_distillation_grad gives each rank its gradient.
  */
@@ -150,8 +151,8 @@ int echo_distillation(const void *logits, int64_t logits_stride, int32_t type, c
                       int hip_device, void *hip_stream);
 
 /*
- * grad = T (exp(logits / T - lse) - q) * grad_loss for the columns held here, lse [rows] that of the whole vocabulary, taken as
- * it is given.  Rows not trained on and rows with lse = -inf get zeros.  grad may be logits itself.
+ * grad = T (exp(logits / T - lse) - q) * grad_loss for the columns held here, logits / T as numbers of 32 bits and lse [rows]
+ * that of the whole vocabulary, taken as it is given.  Rows not trained on and rows with lse = -inf get zeros.  grad may be logits itself.
  */
 int echo_distillation_grad(const void *logits, int64_t logits_stride, int32_t type, const void *ids, int32_t index_type,
                            const void *teacher, int32_t teacher_type, int64_t rows, int64_t cols, int64_t top,

@@ -447,7 +447,8 @@ def distillation(logits, ids, teacher, *, temperature=1.0, vocab_start=0, vocab_
 
     An id may come more than once.  Its entries' q add up in the gradient and in 'target'; the loss and 'entropy' are sums over the
     entries, each with its own log q, so that the loss is lower than that of the merged entry by a constant of the student (two equal
-    entries alone in a row: temperature^2 log 2) and may be below 0.
+    entries alone in a row: temperature^2 log 2) and may be below 0.  For the divergence give one entry an id, of logit
+    temperature * logsumexp(teacher / temperature) over its entries.
 
     Whole vocabulary (vocab_size not given): a dict with 'loss', 'lse' (log of the sum of exp(logits / temperature)),
     float32, and, if grad_loss is given, 'grad': that of the logits, in the same pass.  `out` may supply tensors
